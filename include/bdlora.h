@@ -445,6 +445,131 @@ int bdlora_profile_end(bdlora_pool_t pool, float* ms, int32_t* n);
 #define BDLORA_PATH_LARGE  4
 int bdlora_last_path(bdlora_pool_t pool, int32_t* path);
 
+/* ------------------------------------------------------------------------
+ * Key-value cache: what stands between a layer's qkv and o projections in
+ * decoder serving (the attention of the Llama models of Sec. 4; its heads
+ * are sharded like the projections, so one GPU caches its own kv heads).
+ *
+ * A cache belongs to one decoder layer on one shard.  Its memory is the
+ * caller's and lies in pages:
+ *     k, v:         [n_pages][n_kv_heads][page_size][head_dim]
+ *     weight, pos:  [n_pages][n_kv_heads][page_size], fp32 and int32
+ * A sequence's entries 0 .. len - 1 lie in the pages that its row of the page
+ * table names: entry i in place i mod page_size of page table[row][i /
+ * page_size].  Places of a row from ceil(len / page_size) on are never read,
+ * and what pages hold from entry len on, or before the first entry attended
+ * to, affects no result (it may be anything, NaN as well).  Page tables, and
+ * lens, starts, seqs, index and positions, are int32 device arrays: calls can
+ * be captured in a HIP graph and replayed over changed contents.
+ *
+ * Query head h reads kv head h / (n_q_heads / n_kv_heads).  Keys are cached
+ * after their rotation, so the order of a sequence's entries means nothing to
+ * attention, only to starts.
+ *
+ * weight is the attention probability that an entry's key got, summed over
+ * the query heads that read it and over the calls that accumulate; pos is its
+ * token's position.  A cache without them (both null) attends but does not
+ * accumulate or evict.  A page may be named by several sequences (a shared
+ * prefix) where it is only attended to; a call that accumulates, appends or
+ * evicts writes pages, which only one of its sequences may name.
+ *
+ * Device-side errors (a page number outside 0 .. n_pages - 1 under an entry
+ * that is used, a length or index beyond the table's row, a position outside
+ * the tables, a seq outside the table) raise the cache's sticky error flag
+ * (bdlora_kv_get_device_error); nothing outside the arrays is read or
+ * written: the entry counts as not there, the length is cut to what the row
+ * can name, the token is not stored.
+ *
+ * All calls only enqueue on `stream` and allocate nothing; calls on one cache
+ * share its workspace and must be issued on one stream. */
+typedef struct bdlora_kv* bdlora_kv_t;
+
+/* Cache formats: bf16, or 8 bits (e4m3) that stand for k_scale (v_scale)
+ * times their value.  Queries, inputs and outputs are bf16 either way, and
+ * all sums and the softmax fp32. */
+#define BDLORA_KV_BF16     0
+#define BDLORA_KV_FP8_E4M3 1
+
+/* n_q_heads: 1..1024, a multiple of n_kv_heads (the shard's own heads).
+ * head_dim: 64 or 128.  page_size: a power of two, 16..65536.  max_seqs:
+ * 1..65535, the most sequences of a call.  k_scale, v_scale: positive (1 for
+ * a bf16 cache). */
+typedef struct {
+    int32_t n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs;
+    int32_t format;
+    float k_scale, v_scale;
+} bdlora_kv_desc;
+
+/* A cache over the caller's device memory (16-byte aligned, kept for the
+ * cache's life, contents as they are); weight and pos: both, or both null.
+ * Allocates the workspace.  Errors: INVALID_ARG, SHAPE, OOM, HIP,
+ * UNSUPPORTED. */
+int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight, int32_t* pos, int32_t device,
+                     bdlora_kv_t* out);
+
+/* Free the workspace (waits for the device's work). */
+int bdlora_kv_destroy(bdlora_kv_t cache);
+
+/* Bytes of one page (k and v, with `weights` weight and pos too) and of the
+ * workspace.  Pure host function; either pointer may be null. */
+int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_bytes, int64_t* workspace_bytes);
+
+/* Rotary embedding of T new tokens and their entry into the cache.
+ * qkv: device bf16 [T rows, qkv_stride elements apart], each the shard's
+ * output of the qkv projection: query heads, key heads, value heads side by
+ * side.  cos, sin: fp32 [n_positions][head_dim / 2].  With pairs (x1, x2) =
+ * elements (i, i + head_dim / 2), or (2i, 2i + 1) with interleaved != 0, of a
+ * query or key row of a token at position p:
+ *     y1 = x1 cos[p][i] - x2 sin[p][i],  y2 = x2 cos[p][i] + x1 sin[p][i]
+ * in fp32, each product and sum rounded by itself, then to bf16 (to the
+ * cache's format: times 1 / scale, clamped to +-448, to nearest even).
+ * q_out: bf16 [T rows, q_stride apart], the rotated queries (it may be the
+ * query part of qkv itself).  Token t becomes entry index[t] of table row
+ * seqs[t] (0..n_seqs - 1; -1: it is not stored, its query is rotated all the
+ * same), with weight 0 and pos positions[t]; lens (int32 [n_seqs], may be
+ * null): lens[seqs[t]] = max(lens[seqs[t]], index[t] + 1).  No two tokens of
+ * a call may become the same entry.  A token whose position is outside the
+ * tables is not stored and its query row is zero.  Strides: multiples of 8;
+ * qkv, q_out, cos, sin 16-byte aligned.
+ * Errors: INVALID_ARG, SHAPE, HIP. */
+int bdlora_kv_append(bdlora_kv_t cache, const void* qkv, int64_t qkv_stride, const float* cos, const float* sin,
+                     int32_t n_positions, int32_t interleaved, const int32_t* seqs, const int32_t* index,
+                     const int32_t* positions, int32_t T, const int32_t* table, int64_t table_stride, int32_t table_width,
+                     int32_t n_seqs, int32_t* lens, void* q_out, int64_t q_stride, void* stream);
+
+/* Attention of one new token for each of B sequences (0..max_seqs): row b of
+ * q (bf16, rows q_stride elements apart, heads side by side) over entries
+ * max(starts[b], 0) .. lens[b] - 1 (starts null: all) of table row b:
+ *     s_j = scale <q, k_j>,  p = softmax(s),  out = sum_j p_j v_j,
+ *     lse = log sum_j exp(s_j)
+ * out: bf16 rows like q's (not overlapping what the call reads); lse: fp32
+ * [B][n_q_heads], may be null.  Where no entry is left, or all scores are
+ * -infinity, out is 0 and lse -infinity.  accumulate != 0 adds each entry's
+ * p_j, summed over the query heads of its kv head, to its weight.  Results
+ * do not depend on timing (bitwise equal from call to call).
+ * q, out 16-byte aligned, strides multiples of 8.
+ * Errors: INVALID_ARG (accumulate on a cache without weights, too), SHAPE,
+ * HIP. */
+int bdlora_kv_attend(bdlora_kv_t cache, const void* q, int64_t q_stride, int32_t B, const int32_t* table,
+                     int64_t table_stride, int32_t table_width, const int32_t* lens, const int32_t* starts, float scale,
+                     int32_t accumulate, void* out, int64_t out_stride, float* lse, void* stream);
+
+/* Cut each of B sequences (table rows 0..B - 1) to at most `budget` >= 1
+ * entries, in place, for each kv head by itself: first in rank are the
+ * entries whose pos exceeds the sequence's largest pos (in that head) minus
+ * `recent` (0..budget), then the others by weight, largest first (NaN last);
+ * equal ranks go by the lower entry.  The first `budget` stay.  Those of them
+ * that are entries >= budget move, in ascending order, into the places below
+ * budget that became free, in ascending order (k, v, weight and pos move;
+ * the others are left alone).  lens[b] = min(lens[b], budget).  Sequences
+ * within the budget stay as they are.
+ * Errors: INVALID_ARG (a cache without weights, too), SHAPE, HIP. */
+int bdlora_kv_evict(bdlora_kv_t cache, int32_t B, const int32_t* table, int64_t table_stride, int32_t table_width,
+                    int32_t* lens, int32_t budget, int32_t recent, void* stream);
+
+/* As bdlora_get_device_error, for the cache's flag. */
+int bdlora_kv_get_device_error(bdlora_kv_t cache, void* stream, int32_t* flag);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* bdlora_last_error(void);
 

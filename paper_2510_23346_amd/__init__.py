@@ -21,6 +21,7 @@ __all__ = [
     "DECODE_PLAN_IN_MAIN_BYTES", "decode_plans_in_main",
     "ACT_NONE", "ACT_SILU_MUL", "WEIGHT_BF16", "WEIGHT_INT4_G128", "pack_weight_int4",
     "packed_weight_bytes", "MAX_SEGMENTS", "Segments", "layout_slot_bytes", "pack_adapter_layout",
+    "KVCache", "KVDesc", "KV_BF16", "KV_FP8_E4M3", "kv_bytes",
 ]
 
 COLUMN, ROW = 0, 1
@@ -42,6 +43,7 @@ ACT_NONE, ACT_SILU_MUL = 0, 1   # BDLORA_ACT_*: activation between the MLP's pro
 # BDLORA_PATH_*: launch sequence of a forward (0: none yet)
 PATHS = {0: "", 1: "decode", 2: "tile64", 3: "medium", 4: "large"}
 WEIGHT_BF16, WEIGHT_INT4_G128 = 0, 1   # BDLORA_WEIGHT_*: base weight formats
+KV_BF16, KV_FP8_E4M3 = 0, 1   # BDLORA_KV_*: key-value cache formats
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libbdlora.so")
 _LIB = None
@@ -66,7 +68,14 @@ class _Segs(ctypes.Structure):
     _fields_ = [("n_seg", _c.c_int32), ("start", _IP), ("len", _IP), ("slot", _IP)]
 
 
+class KVDesc(ctypes.Structure):
+    _fields_ = [("n_q_heads", _c.c_int32), ("n_kv_heads", _c.c_int32), ("head_dim", _c.c_int32),
+                ("page_size", _c.c_int32), ("n_pages", _c.c_int32), ("max_seqs", _c.c_int32), ("format", _c.c_int32),
+                ("k_scale", _c.c_float), ("v_scale", _c.c_float)]
+
+
 _SP = _c.POINTER(_Segs)
+_L = _c.c_int64
 
 _SIGS = {
     "bdlora_create_pool": (_I, [_c.POINTER(ProjDesc), _I, _I, _I, _I, _c.c_int64, _I, _c.POINTER(_P)]),
@@ -97,6 +106,13 @@ _SIGS = {
     "bdlora_profile_begin": (_I, [_P, _I]),
     "bdlora_profile_end": (_I, [_P, _c.POINTER(_c.c_float), _IP]),
     "bdlora_last_path": (_I, [_P, _IP]),
+    "bdlora_kv_create": (_I, [_c.POINTER(KVDesc), _P, _P, _P, _P, _I, _c.POINTER(_P)]),
+    "bdlora_kv_destroy": (_I, [_P]),
+    "bdlora_kv_bytes": (_I, [_c.POINTER(KVDesc), _I, _LP, _LP]),
+    "bdlora_kv_append": (_I, [_P, _P, _L, _P, _P, _I, _I, _P, _P, _P, _I, _P, _L, _I, _I, _P, _P, _L, _P]),
+    "bdlora_kv_attend": (_I, [_P, _P, _L, _I, _P, _L, _I, _P, _P, _c.c_float, _I, _P, _L, _P, _P]),
+    "bdlora_kv_evict": (_I, [_P, _I, _P, _L, _I, _P, _I, _I, _P]),
+    "bdlora_kv_get_device_error": (_I, [_P, _P, _IP]),
     "bdlora_last_error": (_c.c_char_p, []),
 }
 HEADER_FUNCTIONS = tuple(_SIGS)
@@ -568,3 +584,6 @@ class Pool:
         v = _c.c_int32(0)
         _check(lib().bdlora_last_path(self._h, _c.byref(v)))
         return PATHS[v.value]
+
+
+from .kvcache import KVCache, kv_bytes  # noqa: E402  (it uses the binding above)

@@ -12,6 +12,8 @@
 
 #include "bdl_launch.h"
 
+#include "bdl_kv.h"
+
 namespace {
 
 thread_local std::string g_err;
@@ -330,6 +332,8 @@ int pack_adapter_slab(const Layout& L, int rank, const uint16_t* const* A_host, 
 }
 
 }  // namespace
+
+int bdl::api_fail(int code, const std::string& msg) { return fail(code, msg); }
 
 extern "C" {
 

@@ -1,0 +1,183 @@
+"""The key-value cache of one decoder layer on one shard (``bdlora_kv_*``).
+
+:class:`KVCache` stands between the qkv and the o projection of a layer:
+``append`` rotates the new tokens' queries and keys and stores keys and
+values, ``attend`` is the attention of one new token per sequence, ``evict``
+cuts sequences to a budget by the attention their entries got.  As in the rest
+of the binding, only arguments are checked and marshalled here.
+"""
+from __future__ import annotations
+
+import ctypes as _c
+import math
+from typing import Tuple
+
+from . import KV_BF16, KV_FP8_E4M3, KVDesc, _check, _stream_handle, lib
+
+__all__ = ["KVCache", "kv_bytes"]
+
+
+def kv_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, max_seqs: int, *,
+             fmt: int = KV_BF16, weights: bool = False) -> Tuple[int, int]:
+    """Bytes of one page (k and v; with ``weights`` weight and pos too) and of
+    a cache's workspace (pure host)."""
+    d = KVDesc(int(n_q_heads), int(n_kv_heads), int(head_dim), int(page_size), int(n_pages), int(max_seqs), int(fmt), 1.0, 1.0)
+    a, b = _c.c_int64(), _c.c_int64()
+    _check(lib().bdlora_kv_bytes(_c.byref(d), int(weights), _c.byref(a), _c.byref(b)))
+    return a.value, b.value
+
+
+class KVCache:
+    """A paged key-value cache.
+
+    ``k`` and ``v`` are device tensors ``[n_pages, n_kv_heads, page_size,
+    head_dim]`` (bf16, or ``torch.float8_e4m3fn`` standing for ``k_scale`` or
+    ``v_scale`` times their values), ``weight`` (fp32) and ``pos`` (int32)
+    ``[n_pages, n_kv_heads, page_size]``.  They are allocated (zeroed) where
+    they are not given; weight and pos only with ``weights=True``, and a cache
+    without them cannot accumulate or evict.
+
+    ``table`` arguments are int32 device tensors ``[sequences, width]``:
+    entry i of a sequence lies in place ``i % page_size`` of page ``table[row,
+    i // page_size]``.  Calls enqueue on ``stream`` (the current one).
+    """
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, page_size: int, max_seqs: int, *,
+                 fmt: int = KV_BF16, k_scale: float = 1.0, v_scale: float = 1.0, weights: bool = False, device: int = 0,
+                 k=None, v=None, weight=None, pos=None):
+        import torch
+        self._h = None
+        self.n_q_heads, self.n_kv_heads, self.head_dim = int(n_q_heads), int(n_kv_heads), int(head_dim)
+        self.n_pages, self.page_size, self.max_seqs, self.fmt = int(n_pages), int(page_size), int(max_seqs), int(fmt)
+        self.device = int(device)
+        d = KVDesc(self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, self.max_seqs, self.fmt,
+                   float(k_scale), float(v_scale))
+        _check(lib().bdlora_kv_bytes(_c.byref(d), 0, None, None))       # refuses a bad description before any allocation
+        self._bf16, self._i32, self._f32 = torch.bfloat16, torch.int32, torch.float32
+        shape = (self.n_pages, self.n_kv_heads, self.page_size)
+        kind = torch.float8_e4m3fn if self.fmt == KV_FP8_E4M3 else torch.bfloat16
+        weights = weights or weight is not None or pos is not None
+
+        def buffer(name, t, shape, kind):
+            if t is None:
+                return torch.zeros(shape, dtype=kind, device=f"cuda:{self.device}")
+            if tuple(t.shape) != shape or t.dtype != kind or not t.is_contiguous() or t.get_device() != self.device:
+                raise ValueError(f"{name} must be a contiguous {kind} tensor {shape} on cuda:{self.device}")
+            return t
+
+        self.k = buffer("k", k, shape + (self.head_dim,), kind)
+        self.v = buffer("v", v, shape + (self.head_dim,), kind)
+        self.weight = buffer("weight", weight, shape, torch.float32) if weights else None
+        self.pos = buffer("pos", pos, shape, torch.int32) if weights else None
+        h = _c.c_void_p()
+        _check(lib().bdlora_kv_create(_c.byref(d), self.k.data_ptr(), self.v.data_ptr(),
+                                      self.weight.data_ptr() if weights else None, self.pos.data_ptr() if weights else None,
+                                      self.device, _c.byref(h)))
+        self._h = h
+        self._scale = 1.0 / math.sqrt(self.head_dim)
+        self._qw = self.n_q_heads * self.head_dim
+        self._qkvw = self._qw + 2 * self.n_kv_heads * self.head_dim
+        L = lib()
+        self._append, self._attend, self._evict = L.bdlora_kv_append, L.bdlora_kv_attend, L.bdlora_kv_evict
+
+    # -- lifetime ---------------------------------------------------------
+    def close(self):
+        if getattr(self, "_h", None):
+            _check(lib().bdlora_kv_destroy(self._h))
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    # -- arguments --------------------------------------------------------
+    def _rows(self, name, t, n, width):
+        """Row stride of a bf16 tensor of n rows: [n, width], or [n, heads, head_dim]."""
+        sh, st = t.shape, t.stride()
+        ok = t.dtype == self._bf16 and t.get_device() == self.device and sh[0] == n
+        if len(sh) == 2:
+            ok = ok and sh[1] == width and st[1] == 1
+        else:
+            ok = ok and len(sh) == 3 and sh[2] == self.head_dim and sh[1] * sh[2] == width and st[2] == 1 and \
+                (st[1] == self.head_dim or sh[1] == 1)
+        if not ok:
+            raise ValueError(f"{name} must be a bf16 tensor [{n}, {width}] on cuda:{self.device} with contiguous rows")
+        return st[0] if n > 1 else width
+
+    def _ints(self, name, t, n):
+        if t.dtype != self._i32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != self.device:
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values on cuda:{self.device}")
+        return t.data_ptr()
+
+    def _table(self, t):
+        st = t.stride()
+        if t.dtype != self._i32 or t.dim() != 2 or st[1] != 1 and t.shape[1] > 1 or t.get_device() != self.device:
+            raise ValueError(f"table must be an int32 tensor [sequences, width] on cuda:{self.device} with contiguous rows")
+        return t.data_ptr(), (st[0] if t.shape[0] > 1 else t.shape[1]), t.shape[1]
+
+    # -- operators --------------------------------------------------------
+    def append(self, qkv, cos, sin, seqs, index, positions, table, lens, q_out, interleaved: bool = False, stream=None):
+        """Rotate the queries and keys of ``qkv [T, (n_q_heads + 2
+        n_kv_heads) head_dim]`` (the qkv projection's output), store keys and
+        values as entries ``index`` of table rows ``seqs`` (-1: not stored),
+        raise ``lens`` (may be None) to cover them, and write the rotated
+        queries to ``q_out`` (it may be qkv's own query columns).  ``cos`` and
+        ``sin``: fp32 ``[positions, head_dim / 2]``."""
+        T = qkv.shape[0]
+        qs = self._rows("qkv", qkv, T, self._qkvw)
+        os_ = self._rows("q_out", q_out, T, self._qw)
+        for t in (cos, sin):
+            if t.dtype != self._f32 or t.shape != cos.shape or t.dim() != 2 or t.shape[1] * 2 != self.head_dim or \
+                    not t.is_contiguous() or t.get_device() != self.device:
+                raise ValueError(f"cos and sin must be contiguous fp32 tensors [positions, {self.head_dim // 2}] on "
+                                 f"cuda:{self.device}")
+        tp, ts, tw = self._table(table)
+        n = table.shape[0]
+        _check(self._append(self._h, qkv.data_ptr(), qs, cos.data_ptr(), sin.data_ptr(), cos.shape[0], int(interleaved),
+                            self._ints("seqs", seqs, T), self._ints("index", index, T),
+                            self._ints("positions", positions, T), T, tp, ts, tw, n,
+                            None if lens is None else self._ints("lens", lens, n), q_out.data_ptr(), os_,
+                            _stream_handle(stream)))
+
+    def attend(self, q, table, lens, out, starts=None, scale=None, lse=None, accumulate: bool = False, stream=None):
+        """Attention of row b of ``q [B, n_q_heads head_dim]`` over entries
+        ``starts[b]`` (0) to ``lens[b]`` of table row b, into ``out``;
+        ``scale`` defaults to ``head_dim ** -0.5``.  ``lse``: fp32 ``[B,
+        n_q_heads]``, receives the log of the sum of the scores'
+        exponentials.  ``accumulate`` adds the entries' probabilities to
+        ``weight``."""
+        B = q.shape[0]
+        qs = self._rows("q", q, B, self._qw)
+        os_ = self._rows("out", out, B, self._qw)
+        tp, ts, tw = self._table(table)
+        if table.shape[0] < B:
+            raise ValueError(f"table has {table.shape[0]} rows for {B} sequences")
+        if lse is not None and (lse.dtype != self._f32 or tuple(lse.shape) != (B, self.n_q_heads) or
+                                not lse.is_contiguous() or lse.get_device() != self.device):
+            raise ValueError(f"lse must be a contiguous fp32 tensor [{B}, {self.n_q_heads}] on cuda:{self.device}")
+        _check(self._attend(self._h, q.data_ptr(), qs, B, tp, ts, tw, self._ints("lens", lens, B),
+                            None if starts is None else self._ints("starts", starts, B),
+                            self._scale if scale is None else scale, int(accumulate), out.data_ptr(), os_,
+                            None if lse is None else lse.data_ptr(), _stream_handle(stream)))
+
+    def evict(self, table, lens, budget: int, recent: int = 0, stream=None):
+        """Cut the sequences of ``table`` to ``budget`` entries per kv head:
+        the last ``recent`` positions stay, then the largest weights; kept
+        entries from behind the budget move into the freed places."""
+        tp, ts, tw = self._table(table)
+        B = table.shape[0]
+        _check(self._evict(self._h, B, tp, ts, tw, self._ints("lens", lens, B), int(budget), int(recent),
+                           _stream_handle(stream)))
+
+    def device_error(self, stream=None) -> int:
+        f = _c.c_int32(0)
+        _check(lib().bdlora_kv_get_device_error(self._h, _stream_handle(stream), _c.byref(f)))
+        return f.value
