@@ -15,6 +15,12 @@ int api_fail(int code, const std::string& msg);
 constexpr int kKvMaxHeads = 1024;      // query heads
 constexpr int kKvMinPage = 16, kKvMaxPage = 65536;
 
+// attend: the most workgroups of a launch, heads a workgroup takes at once,
+// and what one leaves for a sequence that it shares with others: unnormalised
+// sums [heads][D], then each head's maximum and sum
+constexpr int kKvAttendGrid = 512, kKvHeads = 16;
+constexpr int kv_part_floats(int D) { return kKvHeads * (D + 2); }
+
 // What every kernel knows of the cache and of the call's page table.  Pages
 // are [n_pages][hkv][1 << ps_shift] entries: K and V of D elements each,
 // weight and pos (null when the cache does not track weights) of one.
@@ -48,7 +54,11 @@ struct KvAttendArgs {
     long long q_stride, out_stride;
     const int *lens, *starts;   // starts may be null
     float* lse;                 // may be null
-    int B;
+    int B, n_cu;
+    float* part;                // [2 kKvAttendGrid][kv_part_floats(D)]
+    unsigned* count;            // [B][hkv][head tiles]: zero between calls
+    float* logits;              // accumulating: [n_pages][hq][page], scores in units of log 2
+    float* lse2;                // accumulating: [B][hq], lse in those units
     float score_scale;    // times the product of raw values: scores in units of log 2
     float v_scale;
 };

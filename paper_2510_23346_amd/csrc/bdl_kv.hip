@@ -1,40 +1,7 @@
-// Key-value cache of decoder serving: append, attention of one new token,
-// eviction (gfx950, wave64).
-#include "bdl_device.h"
-#include "bdl_kv.h"
+// Key-value cache of decoder serving: append and eviction (gfx950, wave64).
+#include "bdl_kv_device.h"
 
 namespace bdl {
-
-__device__ __forceinline__ float bf2f(uint32_t b) { return __uint_as_float(b << 16); }
-
-// e4m3 bits, round to nearest even, clamped to the largest number (NaN stays)
-__device__ __forceinline__ uint32_t f2e4m3(float f) {
-    const float c = f != f ? f : fminf(fmaxf(f, -448.f), 448.f);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, c, 0, false) & 0xffu;
-}
-
-__device__ __forceinline__ void kv_error(const KvCache& c) {
-    __hip_atomic_store(c.err, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// the entry (index i of sequence row b, kv head h) as an index into the
-// pages' entries; -1 (and the error flag) where the table names no page
-__device__ __forceinline__ long long kv_entry(const KvCache& c, int b, int h, int i) {
-    const int p = c.table[(long long)b * c.tstride + (i >> c.ps_shift)];
-    if ((unsigned)p >= (unsigned)c.n_pages) {
-        kv_error(c);
-        return -1;
-    }
-    return (((long long)p * c.hkv + h) << c.ps_shift) + (i & ((1 << c.ps_shift) - 1));
-}
-
-// length of row b, limited to what its table row can name
-__device__ __forceinline__ int kv_len(const KvCache& c, const int* lens, int b) {
-    const int n = lens[b];
-    const long long most = (long long)c.width << c.ps_shift;
-    if (n < 0 || n > most) kv_error(c);
-    return n < 0 ? 0 : (int)min((long long)n, most);
-}
 
 // ------------------------------------------------------------------ append
 // One thread per pair of a q or k row, or per two elements of a v row.
@@ -93,95 +60,6 @@ hipError_t launch_kv_append(const KvAppendArgs& a, int head_dim, bool fp8, hipSt
         fp8 ? kv_append_kernel<64, true><<<a.T, 256, 0, s>>>(a) : kv_append_kernel<64, false><<<a.T, 256, 0, s>>>(a);
     else
         fp8 ? kv_append_kernel<128, true><<<a.T, 256, 0, s>>>(a) : kv_append_kernel<128, false><<<a.T, 256, 0, s>>>(a);
-    return hipGetLastError();
-}
-
-// ------------------------------------------------------------------ attend
-template <bool FP8>
-__device__ __forceinline__ float kv_get(const char* base, long long i) {
-    if (FP8) {
-        const uint32_t b = reinterpret_cast<const uint8_t*>(base)[i];
-        return (float)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false)[0];
-    }
-    return bf2f(reinterpret_cast<const uint16_t*>(base)[i]);
-}
-
-__device__ __forceinline__ float wave_sum(float v) {
-    for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k);
-    return v;
-}
-
-// One workgroup per (sequence, kv head), one query head after the other; a
-// wave takes every fourth entry with a running maximum and sum.
-template <int D, bool FP8>
-__global__ void kv_attend_kernel(const KvAttendArgs a, const bool accumulate) {
-    constexpr int E = D / 64;
-    __shared__ float red[4][D + 2], stat[2];
-    const int b = blockIdx.x, h = blockIdx.y, w = wave_id(), l = threadIdx.x & 63, G = a.c.hq / a.c.hkv;
-    const int n = kv_len(a.c, a.lens, b), i0 = a.starts ? max(a.starts[b], 0) : 0;
-    auto score = [&](const float* q, long long e) {
-        float s = 0.f;
-        for (int k = 0; k < E; ++k) s += q[k] * kv_get<FP8>(a.c.K, e * D + l + 64 * k);
-        return wave_sum(s) * a.score_scale;
-    };
-    for (int pass = 0; pass < (accumulate ? 2 * G : G); ++pass) {
-        const int hq = h * G + pass % G;
-        float q[E], o[E], m = -INFINITY, sum = 0.f;
-        for (int k = 0; k < E; ++k) {
-            q[k] = bf2f(a.q[b * a.q_stride + hq * D + l + 64 * k]);
-            o[k] = 0.f;
-        }
-        if (pass >= G) {      // weights, head by head
-            const float lse = a.lse[(long long)b * a.c.hq + hq] * 1.44269504f;
-            for (int i = i0 + w; i < n; i += 4) {
-                const long long e = kv_entry(a.c, b, h, i);
-                if (e < 0) continue;
-                const float p = exp2f(score(q, e) - lse);
-                if (l == 0) a.c.weight[e] += p;
-            }
-            continue;
-        }
-        for (int i = i0 + w; i < n; i += 4) {
-            const long long e = kv_entry(a.c, b, h, i);
-            if (e < 0) continue;
-            const float s = score(q, e), mn = fmaxf(m, s);
-            const float f = m == -INFINITY ? 0.f : exp2f(m - mn), p = s == -INFINITY ? 0.f : exp2f(s - mn);
-            m = mn;
-            sum = sum * f + p;
-            for (int k = 0; k < E; ++k) o[k] = o[k] * f + p * kv_get<FP8>(a.c.V, e * D + l + 64 * k);
-        }
-        __syncthreads();
-        for (int k = 0; k < E; ++k) red[w][l + 64 * k] = o[k];
-        if (l == 0) {
-            red[w][D] = m;
-            red[w][D + 1] = sum;
-        }
-        __syncthreads();
-        const float top = fmaxf(fmaxf(red[0][D], red[1][D]), fmaxf(red[2][D], red[3][D]));
-        float total = 0.f, f[4];
-        for (int k = 0; k < 4; ++k) {
-            f[k] = red[k][D] == -INFINITY ? 0.f : exp2f(red[k][D] - top);
-            total += red[k][D + 1] * f[k];
-        }
-        if (threadIdx.x < D) {
-            float v = 0.f;
-            for (int k = 0; k < 4; ++k) v += red[k][threadIdx.x] * f[k];
-            a.out[b * a.out_stride + hq * D + threadIdx.x] = f2bf(total == 0.f ? 0.f : v / total * a.v_scale);
-        }
-        if (threadIdx.x == 0 && a.lse)
-            a.lse[(long long)b * a.c.hq + hq] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.693147181f;
-        __syncthreads();
-    }
-}
-
-hipError_t launch_kv_attend(const KvAttendArgs& a, int head_dim, bool fp8, bool accumulate, hipStream_t s) {
-    const dim3 grid(a.B, a.c.hkv);
-    if (head_dim == 64)
-        fp8 ? kv_attend_kernel<64, true><<<grid, 256, 0, s>>>(a, accumulate)
-            : kv_attend_kernel<64, false><<<grid, 256, 0, s>>>(a, accumulate);
-    else
-        fp8 ? kv_attend_kernel<128, true><<<grid, 256, 0, s>>>(a, accumulate)
-            : kv_attend_kernel<128, false><<<grid, 256, 0, s>>>(a, accumulate);
     return hipGetLastError();
 }
 

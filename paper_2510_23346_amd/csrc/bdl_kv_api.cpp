@@ -20,9 +20,13 @@ struct bdlora_kv {
     char* ws = nullptr;            // the workspace, one allocation
     long long bytes = 0;
     int* err = nullptr;
-    float* lse = nullptr;          // [max_seqs][n_q_heads]
+    int n_cu = 0;
+    float* lse2 = nullptr;         // [max_seqs][n_q_heads]
+    float* part = nullptr;         // attend's shares of sequences
+    unsigned* count = nullptr;     // [max_seqs][n_kv_heads][head tiles]
+    float* logits = nullptr;       // [n_pages][n_q_heads][page_size]
     int* moves = nullptr;          // [max_seqs][n_kv_heads]
-    int* scratch = nullptr;        // [n_pages][n_kv_heads][page_size]
+    int* scratch = nullptr;        // [n_pages][n_kv_heads][page_size], where logits lie too
 };
 
 namespace {
@@ -77,7 +81,7 @@ int check_desc(const bdlora_kv_desc* d) {
 }
 
 struct Parts {
-    long long err, lse, moves, scratch, total;
+    long long clear, err, count, part, lse2, moves, logits, total;   // (what starts at zero lies below clear)
 };
 
 Parts layout(const bdlora_kv_desc& d, bool weights) {
@@ -88,10 +92,14 @@ Parts layout(const bdlora_kv_desc& d, bool weights) {
         at += (bytes + 255) / 256 * 256;
         return r;
     };
+    const long long group = d.n_q_heads / d.n_kv_heads;
     p.err = take(4);
-    p.lse = take(4LL * d.max_seqs * d.n_q_heads);
+    p.count = take(4LL * d.max_seqs * d.n_kv_heads * ((group + bdl::kKvHeads - 1) / bdl::kKvHeads));
+    p.clear = at;
+    p.part = take(2LL * bdl::kKvAttendGrid * bdl::kv_part_floats(d.head_dim) * 4);
+    p.lse2 = take(weights ? 4LL * d.max_seqs * d.n_q_heads : 0);
     p.moves = take(weights ? 4LL * d.max_seqs * d.n_kv_heads : 0);
-    p.scratch = take(weights ? 4LL * d.n_pages * d.n_kv_heads * d.page_size : 0);
+    p.logits = take(weights ? 4LL * d.n_pages * d.n_q_heads * d.page_size : 0);
     p.total = at;
     return p;
 }
@@ -160,7 +168,7 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
         const Parts p = layout(*desc, weight != nullptr);
         char* ws = nullptr;
         if (hipError_t e = hipMalloc((void**)&ws, (size_t)p.total)) return hip_fail("hipMalloc of the cache's workspace", e);
-        hipError_t e = hipMemset(ws + p.err, 0, 4);
+        hipError_t e = hipMemset(ws, 0, (size_t)p.clear);
         if (!e) e = hipStreamSynchronize(nullptr);
         if (e) {
             (void)hipFree(ws);
@@ -180,9 +188,13 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
         c->ws = ws;
         c->bytes = p.total;
         c->err = (int*)(ws + p.err);
-        c->lse = (float*)(ws + p.lse);
+        c->n_cu = std::max(1, prop.multiProcessorCount);
+        c->count = (unsigned*)(ws + p.count);
+        c->part = (float*)(ws + p.part);
+        c->lse2 = (float*)(ws + p.lse2);
+        c->logits = (float*)(ws + p.logits);
         c->moves = (int*)(ws + p.moves);
-        c->scratch = (int*)(ws + p.scratch);
+        c->scratch = (int*)(ws + p.logits);
         *out = c;
         return BDLORA_OK;
     });
@@ -278,8 +290,13 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         a.out_stride = out_stride;
         a.lens = lens;
         a.starts = starts;
-        a.lse = lse ? lse : c->lse;
+        a.lse = lse;
         a.B = B;
+        a.n_cu = c->n_cu;
+        a.part = c->part;
+        a.count = c->count;
+        a.logits = c->logits;
+        a.lse2 = c->lse2;
         a.score_scale = (float)((double)scale * c->d.k_scale * 1.4426950408889634);
         a.v_scale = c->d.v_scale;
         if (hipError_t e = bdl::launch_kv_attend(a, c->d.head_dim, c->d.format == BDLORA_KV_FP8_E4M3, accumulate != 0, (hipStream_t)stream))
