@@ -57,9 +57,11 @@ struct KvAttendArgs {
     int B, n_cu;
     float* part;                // [2 kKvAttendGrid][kv_part_floats(D)]
     unsigned* count;            // [B][hkv][head tiles]: zero between calls
-    float* logits;              // accumulating: [n_pages][hq][page], scores in units of log 2
+    unsigned* group_count;      // [2 kKvAttendGrid]: zero between calls
+    float* logits;              // accumulating: [n_pages][hq][page], products <q, k>
     float* lse2;                // accumulating: [B][hq], lse in those units
-    float score_scale;    // times the product of raw values: scores in units of log 2
+    float score_scale;    // > 0, times the product of raw values: scores in units of log 2
+    unsigned q_sign;      // a negative scale: flips the queries' signs (two bf16 each word)
     float v_scale;
 };
 

@@ -24,6 +24,7 @@ struct bdlora_kv {
     float* lse2 = nullptr;         // [max_seqs][n_q_heads]
     float* part = nullptr;         // attend's shares of sequences
     unsigned* count = nullptr;     // [max_seqs][n_kv_heads][head tiles]
+    unsigned* group_count = nullptr;   // [2 kKvAttendGrid]
     float* logits = nullptr;       // [n_pages][n_q_heads][page_size]
     int* moves = nullptr;          // [max_seqs][n_kv_heads]
     int* scratch = nullptr;        // [n_pages][n_kv_heads][page_size], where logits lie too
@@ -81,7 +82,7 @@ int check_desc(const bdlora_kv_desc* d) {
 }
 
 struct Parts {
-    long long clear, err, count, part, lse2, moves, logits, total;   // (what starts at zero lies below clear)
+    long long clear, err, count, group_count, part, lse2, moves, logits, total;   // (what starts at zero lies below clear)
 };
 
 Parts layout(const bdlora_kv_desc& d, bool weights) {
@@ -95,6 +96,7 @@ Parts layout(const bdlora_kv_desc& d, bool weights) {
     const long long group = d.n_q_heads / d.n_kv_heads;
     p.err = take(4);
     p.count = take(4LL * d.max_seqs * d.n_kv_heads * ((group + bdl::kKvHeads - 1) / bdl::kKvHeads));
+    p.group_count = take(2LL * bdl::kKvAttendGrid * 4);
     p.clear = at;
     p.part = take(2LL * bdl::kKvAttendGrid * bdl::kv_part_floats(d.head_dim) * 4);
     p.lse2 = take(weights ? 4LL * d.max_seqs * d.n_q_heads : 0);
@@ -190,6 +192,7 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
         c->err = (int*)(ws + p.err);
         c->n_cu = std::max(1, prop.multiProcessorCount);
         c->count = (unsigned*)(ws + p.count);
+        c->group_count = (unsigned*)(ws + p.group_count);
         c->part = (float*)(ws + p.part);
         c->lse2 = (float*)(ws + p.lse2);
         c->logits = (float*)(ws + p.logits);
@@ -280,6 +283,10 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         if (!lens || !aligned(lens, 4) || !aligned(starts, 4) || !aligned(lse, 4))
             return api_fail(BDLORA_ERR_INVALID_ARG, "lens (and starts) must be int32, lse fp32 device arrays");
         if (int rc = check_table(c, table, table_stride, table_width)) return rc;
+        // (the kernel counts tiles of 32 entries in 32 bits)
+        const long long heads = (long long)c->d.n_kv_heads * ((c->d.n_q_heads / c->d.n_kv_heads + bdl::kKvHeads - 1) / bdl::kKvHeads);
+        if (((long long)table_width * c->d.page_size + 63) / 32 * B * heads > INT32_MAX)
+            return api_fail(BDLORA_ERR_SHAPE, "more than 2^31 tiles: B x kv heads x a row's entries / 32");
         Device guard(c->device);
         if (!guard.ok) return api_fail(BDLORA_ERR_HIP, "hipSetDevice failed");
         bdl::KvAttendArgs a;
@@ -295,9 +302,12 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         a.n_cu = c->n_cu;
         a.part = c->part;
         a.count = c->count;
+        a.group_count = c->group_count;
         a.logits = c->logits;
         a.lse2 = c->lse2;
-        a.score_scale = (float)((double)scale * c->d.k_scale * 1.4426950408889634);
+        // (the kernels mask with -infinity times the scale: it is kept above zero)
+        a.score_scale = (float)std::max(std::fabs((double)scale * c->d.k_scale * 1.4426950408889634), 1e-37);
+        a.q_sign = scale < 0.f ? 0x80008000u : 0u;
         a.v_scale = c->d.v_scale;
         if (hipError_t e = bdl::launch_kv_attend(a, c->d.head_dim, c->d.format == BDLORA_KV_FP8_E4M3, accumulate != 0, (hipStream_t)stream))
             return hip_fail("attend launch", e);

@@ -9,19 +9,20 @@
 // 4 G flops per 4 bytes.
 //
 // Work is cut into tiles of 32 entries.  All tiles of the batch, sequence
-// after sequence and head after head, form one line, of which every workgroup
-// takes an equal stretch, whatever the sequences' lengths; the four waves of
-// a workgroup take every fourth tile and meet in LDS.  A sequence that a
-// stretch covers alone is finished there; the others' shares go to the
-// workspace, and the workgroup that arrives last adds them in their order (so
-// the result does not depend on which one that is).
+// after sequence and head after head, form one line, of which every wave takes
+// an equal stretch, whatever the sequences' lengths.  Its loads run one tile
+// ahead, its page numbers two, across the ends of sequences.  A sequence
+// within one stretch is finished there; the waves of a workgroup, which have
+// neighbouring stretches, meet in LDS once at the end; what a workgroup shares
+// with others goes to the workspace, and the one that arrives last adds the
+// shares in the line's order (so the result does not depend on which one that
+// is).
 #include "bdl_kv_device.h"
 
 namespace bdl {
 
 namespace {
 
-constexpr int kNW = 4;                  // waves per workgroup
 constexpr float kLn2 = 0.6931471805599453f;
 
 // A sequence: entries first .. len - 1 in tiles that begin at a multiple of 16
@@ -41,26 +42,20 @@ __device__ __forceinline__ Seq seq_of(const KvAttendArgs& a, int b) {
     return s;
 }
 
-// The line of tiles: `total` of them (heads x the sequences' tiles), cut into
-// 1 << k stretches
+// The line of tiles: `total` (< 2^31: heads x the sequences' tiles) of them, cut
+// into 1 << k stretches
 struct Line {
-    unsigned long long total;
+    unsigned total;
     int k;
-    __device__ __forceinline__ unsigned long long begin(unsigned w) const { return (total * w) >> k; }
+    __device__ __forceinline__ unsigned begin(unsigned w) const { return (unsigned)(((unsigned long long)total * w) >> k); }
     // the stretch that holds tile c
-    __device__ __forceinline__ unsigned owner(unsigned long long c) const {
-        unsigned w = (unsigned)min((double)((1u << k) - 1), (double)c * (double)(1u << k) / (double)total);
+    __device__ __forceinline__ unsigned owner(unsigned c) const {
+        unsigned w = min((1u << k) - 1, (unsigned)((float)c * __builtin_amdgcn_rcpf((float)total) * (float)(1u << k)));
         while (begin(w) > c) --w;
         while (begin(w + 1) <= c) ++w;
         return w;
     }
 };
-
-__device__ __forceinline__ unsigned long long wave_sum64(unsigned long long v) {
-#pragma unroll
-    for (int x = 32; x; x >>= 1) v += __shfl_xor(v, x);
-    return v;
-}
 
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -102,157 +97,284 @@ __device__ __forceinline__ u32x4 bf16_of(uint32_t a, uint32_t b) {
     return r;
 }
 
+__device__ __forceinline__ uint32_t pk_bf16(float x, float y) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
+}
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// A tile's two blocks of 16 entries, each within one page
+// A tile: two blocks of 16 entries, each within one page, of one head of one
+// sequence
 struct Tile {
-    size_t at[2];     // bytes from the start of K and V
-    int lo[2], n[2];  // rows lo .. n - 1 of a block are attended to
+    int b, h;             // sequence and head
+    bool first, last;     // of the sequence's tiles
+    unsigned tiles;
+    int e;                // its first entry
+    int lo[2], n[2];      // rows lo .. n - 1 of a block are attended to
     int page[2];
+    unsigned long long at[2];   // where the blocks begin in K and V, in bytes
 };
 
-template <int D, bool FP8, bool ACC>
-__global__ __launch_bounds__(kNW * 64, 2) void kv_attend_kernel(const KvAttendArgs a) {
+// A share's way through the workspace: up to kDirect shares of a sequence are
+// added by its last workgroup; more are added in groups of kGroup workgroups
+// first, so that no workgroup reads more than a few dozen
+constexpr unsigned kDirect = 24, kGroup = 16;
+
+template <int D, bool FP8, bool ACC, int NW, int EU>
+__global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendArgs a) {
     constexpr int SZ = FP8 ? 1 : 2, ROW = D * SZ;
     constexpr int NL = 16 * ROW / 1024;             // 16-byte loads of a block
     constexpr int KS = D / 32, DT = D / 16;
-    constexpr int BUF = 32 * D / 8;                 // 16-byte pieces of a tile in LDS
-    __shared__ u32x4 lds[kNW * BUF];
-    __shared__ float stat[kNW][2][kKvHeads];
-    __shared__ int last_flag;
+    constexpr int BUF = 32 * D / 8;                 // 16-byte pieces of a tile in LDS, or of a wave's sums
+    constexpr int NT = NW * 64;
+    static_assert(NW <= 8, "pieces of a workgroup are in the first 16 lanes");
+    // per wave: the tile being worked on (in the end the sums of its last
+    // sequence), and the sums of a sequence that came from the wave before
+    __shared__ u32x4 lds[NW * 2 * BUF];
+    __shared__ float stat[NW][2][2][kKvHeads];      // [wave][piece][maximum, sum][head]
+    __shared__ int4 info[2 * NW];                   // [wave][piece 1, 0]: sequence (-1: none), head, first and last tile it has, tiles
+    __shared__ unsigned info0[2 * NW];              // its sequence's first tile on the line
+    __shared__ int flag[2];
+    static_assert(kKvHeads * D / 4 <= NT, "a group's share is read before it is written over");
     const int w = wave_id(), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
     const int G = a.c.hq / a.c.hkv, HT = (G + kKvHeads - 1) / kKvHeads, HH = a.c.hkv * HT;
     const int psh = a.c.ps_shift, pmask = (1 << psh) - 1;
 
-    // this workgroup's stretch and where it begins
+    // the line, this workgroup's stretch and the wave's part of it
+    Seq four[4];                                    // sequences c0 + 64 i + lane
+    unsigned incl[4], sum4[4], total = 0;
+    auto look_four = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) four[i] = seq_of(a, c0 + 64 * i + l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            incl[i] = (unsigned)wave_incl_scan((int)four[i].tiles);
+            sum4[i] = (unsigned)wave_total((int)incl[i]);
+        }
+    };
+    if (a.B <= 64) {
+        four[0] = seq_of(a, l);
+        incl[0] = (unsigned)wave_incl_scan((int)four[0].tiles);
+        total = sum4[0] = (unsigned)wave_total((int)incl[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+            four[i] = four[0];
+            incl[i] = incl[0];
+            sum4[i] = 0;
+        }
+    } else {
+        for (int c0 = (a.B - 1) / 256 * 256; c0 >= 0; c0 -= 256) {
+            look_four(c0);
+            total += sum4[0] + sum4[1] + sum4[2] + sum4[3];
+        }
+    }
     Line line;
-    Seq mine = seq_of(a, l);
-    unsigned incl = (unsigned)wave_incl_scan((int)mine.tiles);
-    unsigned long long total = (unsigned)wave_total((int)incl);
-    for (int b = 64 + l; b - l < a.B; b += 64) total += wave_sum64(seq_of(a, b).tiles);
     line.total = total * HH;
-    const int kmax = 31 - __builtin_clz(gridDim.x);
-    line.k = 0;
-    while (line.k < kmax && line.total > ((unsigned long long)kNW << line.k)) ++line.k;
+    // as many stretches as give every wave a tile, at most one per workgroup
+    line.k = min(31 - __builtin_clz(gridDim.x), 32 - __builtin_clz((line.total - 1) / NW | 1) - (line.total <= NW ? 1 : 0));
     if (blockIdx.x >= 1u << line.k) return;
-    unsigned long long r = line.begin(blockIdx.x);
-    const unsigned long long r1 = line.begin(blockIdx.x + 1);
-    if (r >= r1) return;
-    int b0 = 0;                                     // sequences b0 .. b0 + 63 are in the lanes
-    unsigned long long base = 0;                    // tiles of a head before b0
-    while ((base + (unsigned)wave_total((int)incl)) * HH <= r) {
-        base += (unsigned)wave_total((int)incl);
-        b0 += 64;
-        mine = seq_of(a, b0 + l);
-        incl = (unsigned)wave_incl_scan((int)mine.tiles);
-    }
-    int bi = __ffsll((long long)__ballot((base + incl) * HH > r)) - 1;
-    unsigned long long seq0 = (base + (unsigned)__builtin_amdgcn_readlane((int)(incl - mine.tiles), bi)) * HH;   // its first tile
-    int h;
-    unsigned t0;
+    const unsigned g0 = line.begin(blockIdx.x), g1 = line.begin(blockIdx.x + 1);
+    if (g0 >= g1) return;
+    // (fewer tiles than waves: the first waves have one each)
+    auto part_of = [&](unsigned x) { return g1 - g0 < NW ? min(x, g1 - g0) : (unsigned)((unsigned long long)(g1 - g0) * x / NW); };
+    const unsigned r0 = g0 + part_of(w);
+    const int left = (int)(g0 + part_of(w + 1) - r0);                // tiles of this wave
+
+    // The cursor: the tile whose pages are looked up, two ahead of the one
+    // being worked on.  Sequences b0 .. b0 + 63 are in the lanes.
+    int b0 = 0, cb, ch, clen, cfirst;
+    unsigned ct, ctiles;
+    Seq mine;
+    unsigned head0;                                 // the first tile of the first sequence and head
     {
-        const unsigned tiles = (unsigned)__builtin_amdgcn_readlane((int)mine.tiles, bi);
-        const unsigned long long off = r - seq0;
-        unsigned q = (unsigned)((double)off / (double)tiles);
-        if ((unsigned long long)q * tiles > off) --q;
-        if ((unsigned long long)(q + 1) * tiles <= off) ++q;
-        h = (int)q;
-        t0 = (unsigned)(off - (unsigned long long)q * tiles);
+        unsigned base = 0, in = 0;                  // tiles of a head before b0; those up to each lane's sequence
+        for (int c0 = 0;; c0 += 256) {
+            if (a.B > 256) look_four(c0);
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (found) continue;
+                b0 = c0 + 64 * i;
+                mine = four[i];
+                in = incl[i];
+                found = (base + sum4[i]) * HH > r0 || b0 + 64 >= a.B;
+                if (!found) base += sum4[i];
+            }
+            if (found) break;
+        }
+        const unsigned long long over = __ballot((base + in) * HH > r0);
+        const int bi = over ? __ffsll((long long)over) - 1 : 0;      // (none: a wave without tiles behind the last)
+        const unsigned seq0 = (base + (unsigned)__builtin_amdgcn_readlane((int)(in - mine.tiles), bi)) * HH;
+        ctiles = (unsigned)__builtin_amdgcn_readlane((int)mine.tiles, bi);
+        clen = __builtin_amdgcn_readlane(mine.len, bi);
+        cfirst = __builtin_amdgcn_readlane(mine.first, bi);
+        const unsigned off = r0 - seq0;
+        unsigned q = 0;
+        if (HH > 1) {
+            q = (unsigned)((float)off * __builtin_amdgcn_rcpf((float)ctiles));
+            if (q * ctiles > off) --q;
+            if ((q + 1) * ctiles <= off) ++q;
+        }
+        cb = b0 + bi;
+        ch = uni((int)q);
+        ct = (unsigned)uni((int)(off - q * ctiles));
+        head0 = r0 - ct;
     }
-    u32x4* const buf = lds + w * BUF;
-
-    for (;;) {
-        const int b = b0 + bi, kvh = h / HT, ht = h - kvh * HT;
-        const int len = __builtin_amdgcn_readlane(mine.len, bi), first = __builtin_amdgcn_readlane(mine.first, bi);
-        const unsigned tiles = (unsigned)__builtin_amdgcn_readlane((int)mine.tiles, bi);
-        const unsigned t1 = (unsigned)min((unsigned long long)tiles, t0 + (r1 - r));
-        const int nh = min(kKvHeads, G - ht * kKvHeads), hq0 = kvh * G + ht * kKvHeads;
-        const int e0 = first & ~15;
+    auto advance = [&]() __attribute__((always_inline)) {
+        if (++ct < ctiles) return;
+        ct = 0;
+        if (++ch < HH) return;
+        ch = 0;
+        if (++cb >= a.B) --cb;                      // (behind the last tile: never used)
+        if (cb - b0 == 64) {
+            b0 += 64;
+            mine = seq_of(a, b0 + l);
+        }
+        ctiles = (unsigned)__builtin_amdgcn_readlane((int)mine.tiles, cb - b0);
+        clen = __builtin_amdgcn_readlane(mine.len, cb - b0);
+        cfirst = __builtin_amdgcn_readlane(mine.first, cb - b0);
+    };
+    // the cursor's tile, its page numbers on their way
+    auto look = [&](bool used) __attribute__((always_inline)) {
         typedef const __attribute__((address_space(4))) int* cint;
-        const cint trow = (cint)(a.c.table + (long long)b * a.c.tstride);
-
-        // the queries: B operand, lane = head lr, numbers 32 ks + 8 lg on
-        u32x4 q[KS];
+        const cint trow = (cint)(a.c.table + (long long)cb * a.c.tstride);
+        Tile x;
+        x.b = cb;
+        x.h = ch;
+        x.tiles = ctiles;
+        x.first = ct == 0;
+        x.last = ct + 1 == ctiles;
+        x.e = (cfirst & ~15) + 32 * (int)ct;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-            q[ks] = lr < nh ? ld16(a.q + b * a.q_stride + (long long)(hq0 + lr) * D + ks * 32 + lg * 8) : u32x4{0, 0, 0, 0};
-
-        auto pages = [&](unsigned t, int (&pg)[2]) __attribute__((always_inline)) {
+        for (int j = 0; j < 2; ++j) {
+            const int e = x.e + 16 * j, rows = used ? clen - e : 0;
+            x.page[j] = trow[rows > 0 ? e >> psh : 0];
+            x.n[j] = min(16, max(0, rows));
+            x.lo[j] = max(0, cfirst - e);
+        }
+        return x;
+    };
+    // its pages are there: check them.  (Addresses in units of 16 bytes: pages
+    // are at most 2^30 of them)
+    const unsigned page16 = (unsigned)a.c.hkv << psh, row16 = ROW / 16;
+    auto locate = [&](Tile& x) __attribute__((always_inline)) {
+        const int kvh = HT == 1 ? x.h : x.h / HT;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const long long e = e0 + 32LL * t + 16 * j;
-                pg[j] = trow[uni(e < len ? (int)(e >> psh) : 0)];
+        for (int j = 0; j < 2; ++j) {
+            if (x.n[j] > 0 && (unsigned)x.page[j] >= (unsigned)a.c.n_pages) {
+                kv_error(a.c);
+                x.n[j] = 0;
             }
-        };
-        auto tile = [&](unsigned t, const int (&pg)[2]) __attribute__((always_inline)) {
-            Tile x;
+            if (x.n[j] == 0) x.page[j] = 0;
+            x.at[j] = ((unsigned long long)(unsigned)x.page[j] * (page16 * row16) +
+                       (((unsigned)kvh << psh) + ((unsigned)(x.e + 16 * j) & pmask)) * row16) * 16;
+        }
+    };
+    u32x4 kr[2][NL], vr[2][NL];
+    auto load = [&](u32x4 (&x)[2][NL], const char* base_, const Tile& tl) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const long long e = e0 + 32LL * t + 16 * j;
-                bool ok = t < t1 && e < len;
-                if (ok && (unsigned)pg[j] >= (unsigned)a.c.n_pages) {
-                    kv_error(a.c);
-                    ok = false;
+        for (int j = 0; j < 2; ++j) {
+            const __amdgpu_buffer_rsrc_t rs = buf_rsrc(base_ + tl.at[j], (unsigned)tl.n[j] * ROW);
+#pragma unroll
+            for (int i = 0; i < NL; ++i) x[j][i] = buf16(rs, l * 16 + i * 1024);
+        }
+    };
+    // a head of the line: up to 16 query heads of one kv head
+    struct Heads {
+        int hq0, n;
+    };
+    auto heads_of = [&](int h) __attribute__((always_inline)) {
+        if (HT == 1) return Heads{h * G, G};
+        const int kvh = h / HT, ht = h - kvh * HT;
+        return Heads{kvh * G + ht * kKvHeads, min(kKvHeads, G - ht * kKvHeads)};
+    };
+    // the queries of a tile's heads: B operand, lane = head lr, numbers 32 ks + 8 lg on
+    u32x4 q[KS];
+    auto load_q = [&](const Tile& x) __attribute__((always_inline)) {
+        const Heads hd = heads_of(x.h);
+        const uint16_t* p = a.q + x.b * a.q_stride + (hd.hq0 + min(lr, hd.n - 1)) * D + lg * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            q[ks] = ld16(p + ks * 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[ks][i] ^= a.q_sign;
+        }
+    };
+    u32x4* const buf = lds + w * 2 * BUF;
+    // rows as they were loaded (a block is contiguous) into LDS, bf16
+    auto put = [&](const u32x4 (&x)[2][NL], const Tile& tl, bool value) __attribute__((always_inline)) {
+        constexpr int LPR = ROW / 16;               // lanes of a row
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int row = i * (64 / LPR) + l / LPR, c = l % LPR, rr = j * 16 + row;
+                u32x4 v = x[j][i];
+                // (a value before the first entry may be NaN, and 0 times NaN is one)
+                if (value && tl.lo[j] > 0 && row < tl.lo[j]) v = u32x4{0, 0, 0, 0};
+                if constexpr (FP8) {
+                    const u32x4 y0 = bf16_of(v[0], v[1]), y1 = bf16_of(v[2], v[3]);
+                    buf[value ? v_at<D>(rr, 2 * c) : k_at<D>(rr, 2 * c)] = y0;
+                    buf[value ? v_at<D>(rr, 2 * c + 1) : k_at<D>(rr, 2 * c + 1)] = y1;
+                } else {
+                    buf[value ? v_at<D>(rr, c) : k_at<D>(rr, c)] = v;
                 }
-                x.page[j] = ok ? pg[j] : 0;
-                x.n[j] = ok ? (int)min(16LL, len - e) : 0;
-                x.lo[j] = (int)max(0LL, first - e);
-                x.at[j] = ok ? ((((size_t)pg[j] * a.c.hkv + kvh) << psh) + (size_t)((int)e & pmask)) * ROW : 0;
             }
-            return x;
-        };
-        u32x4 kr[2][NL], vr[2][NL];
-        auto load = [&](u32x4 (&x)[2][NL], const char* base_, const Tile& tl) __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const __amdgpu_buffer_rsrc_t rs = buf_rsrc(base_ + tl.at[j], (unsigned)tl.n[j] * ROW);
-#pragma unroll
-                for (int i = 0; i < NL; ++i) x[j][i] = buf16(rs, l * 16 + i * 1024);
-            }
-        };
-        // rows as they were loaded (a block is contiguous) into LDS, bf16
-        auto put = [&](const u32x4 (&x)[2][NL], const Tile& tl, bool value) __attribute__((always_inline)) {
-            constexpr int LPR = ROW / 16;           // lanes of a row
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < NL; ++i) {
-                    const int row = i * (64 / LPR) + l / LPR, c = l % LPR, rr = j * 16 + row;
-                    u32x4 v = x[j][i];
-                    // (a value before the first entry may be NaN, and 0 times NaN is one)
-                    if (value && tl.lo[j] > 0 && row < tl.lo[j]) v = u32x4{0, 0, 0, 0};
-                    if constexpr (FP8) {
-                        const u32x4 y0 = bf16_of(v[0], v[1]), y1 = bf16_of(v[2], v[3]);
-                        buf[value ? v_at<D>(rr, 2 * c) : k_at<D>(rr, 2 * c)] = y0;
-                        buf[value ? v_at<D>(rr, 2 * c + 1) : k_at<D>(rr, 2 * c + 1)] = y1;
-                    } else {
-                        buf[value ? v_at<D>(rr, c) : k_at<D>(rr, c)] = v;
-                    }
-                }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        };
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    // 4 numbers of a row's output, from number d of query head hq on
+    auto finish = [&](int b, int hq, int d, f32x4 v, float top, float sum_) __attribute__((always_inline)) {
+        const float g = a.v_scale / sum_;
+        const bool none = sum_ == 0.f;
+        *reinterpret_cast<uint2*>(a.out + b * a.out_stride + hq * D + d) =
+            uint2{none ? 0u : pk_bf16(v[0] * g, v[1] * g), none ? 0u : pk_bf16(v[2] * g, v[3] * g)};
+        if (d == 0) {
+            const float lse2 = none ? -INFINITY : top + __log2f(sum_);
+            const long long at = (long long)b * a.c.hq + hq;
+            if (a.lse) a.lse[at] = lse2 * kLn2;
+            if (ACC) a.lse2[at] = lse2;
+        }
+    };
 
-        // state of the wave: lane (head lr) has its maximum, its part of the
-        // sum, and out^T: numbers 16 dt + 4 lg + i
-        float m = -INFINITY, sum = 0.f;
-        f32x4 o[DT];
+    // state of the wave: lane (head lr) has its maximum, its part of the sum,
+    // and out^T: numbers 16 dt + 4 lg + i
+    float m = -INFINITY, sum = 0.f;
+    f32x4 o[DT];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // the sums as a piece of a sequence that other waves share, into LDS
+    auto leave = [&](int piece, const Tile& x) __attribute__((always_inline)) {
+        f32x4* const ob = reinterpret_cast<f32x4*>(buf + piece * BUF);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) ob[dt * 64 + l] = o[dt];
+        if (l < kKvHeads) {
+            stat[w][piece][0][l] = m;
+            stat[w][piece][1][l] = sum;
+        }
+        if (l == 0) {
+            info[2 * w + 1 - piece] = int4{x.b, x.h, (piece == 0 ? 1 : 0) | (x.last ? 2 : 0), (int)x.tiles};
+            info0[2 * w + 1 - piece] = head0;
+        }
+    };
+    if (l < 2) info[2 * w + l] = int4{-1, 0, 0, 0};
 
-        int pg[2];
-        unsigned t = t0 + w;
-        pages(t, pg);
-        Tile cur = tile(t, pg);
+    if (left > 0) {
+        Tile cur = look(true);
+        advance();
+        Tile nxt = look(left > 1);
+        locate(cur);
         load(kr, a.c.K, cur);
         load(vr, a.c.V, cur);
-        pages(t + kNW, pg);
-        for (; t < t1; t += kNW) {
-            const Tile nxt = tile(t + kNW, pg);
+        load_q(cur);
+        bool first = cur.first;                     // the wave has the sequence's first tile
+        for (int i = 0; i < left; ++i) {
+            locate(nxt);
             put(kr, cur, false);
             load(kr, a.c.K, nxt);
-            pages(t + 2 * kNW, pg);
             // scores^T: lane = head lr, entries 4 lg + i of each block
             f32x4 s[2];
 #pragma unroll
@@ -261,26 +383,25 @@ __global__ __launch_bounds__(kNW * 64, 2) void kv_attend_kernel(const KvAttendAr
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) s[j] = mfma(buf[k_at<D>(j * 16 + lr, ks * 4 + lg)], q[ks], s[j]);
             }
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = 4 * lg + i;
-                    const float x = s[j][i] * a.score_scale;
-                    s[j][i] = row >= cur.lo[j] && row < cur.n[j] ? x : -INFINITY;
-                    top = fmaxf(top, s[j][i]);
-                }
-            if constexpr (ACC) {
+            if ((cur.lo[0] | cur.lo[1]) > 0 || (cur.n[0] & cur.n[1]) != 16) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    if (lr < nh && cur.n[j] > 0) {
-                        const int in_page = (int)(e0 + 32 * t + 16 * j) & pmask;
-                        *reinterpret_cast<f32x4*>(a.logits + ((((size_t)cur.page[j] * a.c.hq + hq0 + lr) << psh) + in_page + 4 * lg)) = s[j];
-                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (4 * lg + e < cur.lo[j] || 4 * lg + e >= cur.n[j]) s[j][e] = -INFINITY;
+            }
+            if constexpr (ACC) {
+                const Heads hd = heads_of(cur.h);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (lr < hd.n && cur.n[j] > 0)
+                        *reinterpret_cast<f32x4*>(a.logits + ((((size_t)cur.page[j] * a.c.hq + hd.hq0 + lr) << psh) +
+                                                              ((cur.e + 16 * j) & pmask) + 4 * lg)) = s[j];
             }
             // the maximum follows only where a score passes it by 8 (in units of
             // log 2): until then no exponential exceeds 2^8
+            float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                              fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * a.score_scale;
             if (__any(top > m + 8.f)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -292,20 +413,23 @@ __global__ __launch_bounds__(kNW * 64, 2) void kv_attend_kernel(const KvAttendAr
             }
             const float mm = m == -INFINITY ? 0.f : m;
             // exponentials as two bf16 numbers whose sum has 16 significant bits
+            // (the first cut towards zero and the second never 0, so that an
+            // infinite value gives an infinite sum and no NaN)
             u32x4 hi, lo;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const float x = exp2_(s[j][i] - mm), y = exp2_(s[j][i + 1] - mm);
+                for (int e = 0; e < 4; e += 2) {
+                    const float x = exp2_(fmaf(s[j][e], a.score_scale, -mm)), y = exp2_(fmaf(s[j][e + 1], a.score_scale, -mm));
                     sum += x + y;
                     const uint32_t ux = __float_as_uint(x), uy = __float_as_uint(y);
-                    hi[j * 2 + i / 2] = (ux >> 16) | (uy & 0xffff0000u);
-                    const float dx = x - __uint_as_float(ux & 0xffff0000u), dy = y - __uint_as_float(uy & 0xffff0000u);
-                    lo[j * 2 + i / 2] = (__float_as_uint(dx) >> 16) | (__float_as_uint(dy) & 0xffff0000u);
+                    hi[j * 2 + e / 2] = __builtin_amdgcn_perm(uy, ux, 0x07060302u);
+                    lo[j * 2 + e / 2] = pk_bf16(x - __uint_as_float(ux & 0xffff0000u), y - __uint_as_float(uy & 0xffff0000u)) | 0x00010001u;
                 }
             put(vr, cur, true);
             load(vr, a.c.V, nxt);
+            advance();
+            const Tile far = look(i + 2 < left);
             // out^T += V^T P^T: the entries' order within the product is that of
             // the scores' lanes
 #pragma unroll
@@ -320,56 +444,86 @@ __global__ __launch_bounds__(kNW * 64, 2) void kv_attend_kernel(const KvAttendAr
                 const u32x4 va = __builtin_bit_cast(u32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
                 o[dt] = mfma(va, lo, mfma(va, hi, o[dt]));
             }
-            cur = nxt;
-        }
-
-        // the workgroup's waves meet
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        f32x4* const ob = reinterpret_cast<f32x4*>(buf);
+            if (cur.last || i + 1 == left) {
+                // the sequence (and head) ends, or the wave's part does
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (first && cur.last) {
+                    const Heads hd = heads_of(cur.h);
+                    if (lr < hd.n)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) ob[dt * 64 + l] = o[dt];
-        if (l < kKvHeads) {
-            stat[w][0][l] = m;
-            stat[w][1][l] = sum;
-        }
-        __syncthreads();
-        const int head = threadIdx.x & 15;
-        float M = stat[0][0][head], f[kNW], S = 0.f;
+                        for (int dt = 0; dt < DT; ++dt) finish(cur.b, hd.hq0 + lr, dt * 16 + 4 * lg, o[dt], m, sum);
+                } else {
+                    leave(first ? 0 : 1, cur);
+                }
+                if (i + 1 < left) {
+                    load_q(nxt);
+                    head0 = r0 + i + 1;
+                    first = true;
+                    m = -INFINITY;
+                    sum = 0.f;
 #pragma unroll
-        for (int x = 1; x < kNW; ++x) M = fmaxf(M, stat[x][0][head]);
-#pragma unroll
-        for (int x = 0; x < kNW; ++x) {
-            f[x] = stat[x][0][head] == -INFINITY ? 0.f : exp2_(stat[x][0][head] - M);
-            S += f[x] * stat[x][1][head];
-        }
-        auto finish = [&](int hd, int d, f32x4 v, float top, float total_) __attribute__((always_inline)) {
-            const float g = total_ == 0.f ? 0.f : a.v_scale / total_;
-            uint32_t p[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) p[i] = total_ == 0.f ? 0u : f2bf(v[2 * i] * g) | ((uint32_t)f2bf(v[2 * i + 1] * g) << 16);
-            *reinterpret_cast<uint2*>(a.out + b * a.out_stride + (long long)(hq0 + hd) * D + d) = uint2{p[0], p[1]};
-            if (d == 0) {
-                const float lse2 = total_ == 0.f ? -INFINITY : top + __log2f(total_);
-                const long long at = (long long)b * a.c.hq + hq0 + hd;
-                if (a.lse) a.lse[at] = lse2 * kLn2;
-                if (ACC) a.lse2[at] = lse2;
+                    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
             }
-        };
-        const bool whole = t0 == 0 && t1 == tiles;
-        const unsigned long long head0 = seq0 + (unsigned long long)h * tiles;      // this sequence and head's first tile
-        float* const part = a.part + (size_t)(2 * blockIdx.x + (t0 == 0)) * kv_part_floats(D);
-        if (head < nh) {
-            for (int u = threadIdx.x; u < DT * 64; u += kNW * 64) {
+            cur = nxt;
+            nxt = far;
+        }
+    }
+
+    // The pieces of the workgroup, in the line's order (lane 2 wave + 0, 1:
+    // piece 1, which came from the wave before, and piece 0).  Each sequence's
+    // are added, and those that the workgroup has alone are finished
+    __syncthreads();
+    const int head = threadIdx.x & 15;
+    const int4 pi = info[min(l, 2 * NW - 1)];
+    const unsigned ph0 = info0[min(l, 2 * NW - 1)];
+    const unsigned valid = (unsigned)__ballot(pi.x >= 0 && l < 2 * NW);
+    const unsigned lasts = (unsigned)__ballot((pi.z & 2) != 0) & valid;
+    unsigned starts = valid & (0xaaaau | (valid & -valid));
+    int nsh = 0;
+    int share_b[2], share_h[2];
+    unsigned share_0[2], share_tiles[2];
+    while (starts) {
+        const int i0 = __ffs((int)starts) - 1;
+        starts &= starts - 1;
+        const unsigned members = valid & ~((1u << i0) - 1) & (starts ? (starts & -starts) - 1 : 0xffffu);
+        const int n = __popc(members), pw = i0 >> 1;                // waves pw .. pw + n - 1, all but the first with piece 1
+        const int b = __builtin_amdgcn_readlane(pi.x, i0), h = __builtin_amdgcn_readlane(pi.y, i0);
+        const bool has_first = i0 & 1, whole = has_first && (lasts & members);
+        const Heads hd = heads_of(h);
+        float* const part = a.part + (size_t)(2 * blockIdx.x + (has_first ? 1 : 0)) * kv_part_floats(D);
+        auto piece = [&](int z) __attribute__((always_inline)) { return z && z < n ? 1 : has_first ? 0 : 1; };
+        auto wave = [&](int z) __attribute__((always_inline)) { return z < n ? pw + z : pw; };
+        if (head < hd.n) {
+            float f[NW], M = -INFINITY, S = 0.f;
+#pragma unroll
+            for (int z = 0; z < NW; ++z) {
+                f[z] = z < n ? stat[wave(z)][piece(z)][0][head] : -INFINITY;
+                M = fmaxf(M, f[z]);
+            }
+#pragma unroll
+            for (int z = 0; z < NW; ++z) {
+                f[z] = f[z] == -INFINITY ? 0.f : exp2_(f[z] - M);
+                const float x = stat[wave(z)][piece(z)][1][head];
+                S += z < n ? f[z] * x : 0.f;                        // (a NaN stays one)
+            }
+            if (threadIdx.x < DT * 64) {
                 f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int x = 0; x < kNW; ++x) {
-                    const f32x4 y = reinterpret_cast<const f32x4*>(lds)[x * BUF + u];
-                    if (f[x] != 0.f) v += f[x] * y;
+                for (int z0 = 0; z0 < NW; z0 += 4) {
+                    if (z0 >= n) break;
+                    f32x4 y[4];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        y[z] = reinterpret_cast<const f32x4*>(lds)[(wave(z0 + z) * 2 + piece(z0 + z)) * BUF + threadIdx.x];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        if (f[z0 + z] != 0.f) v += f[z0 + z] * y[z];
                 }
-                const int d = (u >> 6) * 16 + ((u >> 4) & 3) * 4;
+                const int d = (threadIdx.x >> 6) * 16 + ((threadIdx.x >> 4) & 3) * 4;
                 if (whole) {
-                    finish(head, d, v, M, S);
+                    finish(b, hd.hq0 + head, d, v, M, S);
                 } else {
                     store_through(part + head * D + d, v[0], v[1]);
                     store_through(part + head * D + d + 2, v[2], v[3]);
@@ -377,81 +531,126 @@ __global__ __launch_bounds__(kNW * 64, 2) void kv_attend_kernel(const KvAttendAr
                 }
             }
         }
-        if (!whole) {
-            const unsigned w0 = line.owner(head0), w1 = line.owner(head0 + tiles - 1);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the share has reached memory
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                unsigned* const c = a.count + (size_t)b * HH + h;
-                const unsigned old = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                last_flag = old == w1 - w0;
-                if (last_flag) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (!whole) {                                               // (at most two: the stretch's first and last sequence)
+            const unsigned h0 = (unsigned)__builtin_amdgcn_readlane((int)ph0, i0), tl = (unsigned)__builtin_amdgcn_readlane(pi.w, i0);
+            if (nsh == 0) {
+                share_b[0] = b;
+                share_h[0] = h;
+                share_0[0] = h0;
+                share_tiles[0] = tl;
+            } else {
+                share_b[1] = b;
+                share_h[1] = h;
+                share_0[1] = h0;
+                share_tiles[1] = tl;
             }
-            __syncthreads();
-            if (last_flag) {
-                // share x of sequence: the first workgroup's second place, the others' first
-                const int n = (int)(w1 - w0) + 1;
-                auto share = [&](int x) { return a.part + (size_t)(2 * (w0 + x) + (x == 0)) * kv_part_floats(D); };
-                float* const fl = reinterpret_cast<float*>(lds);
-                float mx = -INFINITY;
-                if (head < nh)
-                    for (int x = threadIdx.x >> 4; x < n; x += kNW * 4) mx = fmaxf(mx, load_through(share(x) + kKvHeads * D + 2 * head).x);
-                fl[threadIdx.x] = mx;
-                __syncthreads();
-                if (threadIdx.x < kKvHeads) {
-                    for (int x = 1; x < kNW * 4; ++x) mx = fmaxf(mx, fl[x * 16 + head]);
-                    stat[0][0][head] = mx;
+            ++nsh;
+        }
+    }
+
+    // Shares: counted; the workgroup that completes a sequence, or a group of
+    // its workgroups, adds them in the line's order
+    if (nsh == 0) return;
+    unsigned w0[2], w1[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (k < nsh) {
+            w0[k] = line.owner(share_0[k]);
+            w1[k] = line.owner(share_0[k] + share_tiles[k] - 1);
+        }
+    const unsigned grp = blockIdx.x / kGroup;
+#pragma unroll 1
+    for (int round = 0; round < 2 * nsh; ++round) {
+        const int k = round >> 1, level = round & 1;
+        const unsigned v0 = k ? w0[1] : w0[0], v1 = k ? w1[1] : w1[0];
+        const int b = k ? share_b[1] : share_b[0], h = k ? share_h[1] : share_h[0];
+        const Heads hd = heads_of(h);
+        const bool direct = v1 - v0 < kDirect;
+        if (direct && !level) continue;
+        // members m0 + stride x (the sequence's first workgroup in place of what
+        // lies before it), x = 0 .. n - 1
+        const unsigned m0 = direct ? v0 : level ? v0 / kGroup * kGroup : max(v0, grp * kGroup);
+        const unsigned stride = direct || !level ? 1u : kGroup;
+        const unsigned n = direct ? v1 - v0 + 1 : level ? v1 / kGroup - v0 / kGroup + 1 : min(v1 + 1, (grp + 1) * kGroup) - m0;
+        unsigned* const c = level ? a.count + (size_t)b * HH + h : a.group_count + 2 * m0 + (m0 == v0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // what this wave left has reached memory
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const unsigned old = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            flag[0] = old == n - 1;
+            if (flag[0]) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!uni(flag[0])) {
+            if (!level) ++round;                                   // (the sequence is another's)
+            continue;
+        }
+        auto share = [&](unsigned x) __attribute__((always_inline)) {
+            const unsigned v = max(v0, m0 + stride * x);
+            return a.part + (size_t)(2 * v + (v == v0)) * kv_part_floats(D);
+        };
+        // one item = 4 numbers of a head; groups of threads take every ng-th share
+        const int items = hd.n * (D / 4), ng = NT / items, g = threadIdx.x / items, item = threadIdx.x - g * items;
+        const int hq = item / (D / 4), d = item % (D / 4) * 4;
+        f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+        float ss = 0.f, top = -INFINITY;
+        if (g < ng)
+            for (unsigned x0 = g; x0 < n; x0 += 4 * ng) {
+                float2 ms[4], y0[4], y1[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float* p = share(min(x0 + x * ng, n - 1));
+                    ms[x] = load_through(p + kKvHeads * D + 2 * hq);
+                    y0[x] = load_through(p + hq * D + d);
+                    y1[x] = load_through(p + hq * D + d + 2);
                 }
-                __syncthreads();
-                // one item = 4 numbers of a head; groups of threads take every ng-th share
-                const int items = nh * (D / 4), ng = max(1, kNW * 64 / items);
-                for (int i0 = 0; i0 < items; i0 += kNW * 64) {
-                    const int g = ng == 1 ? 0 : threadIdx.x / items, item = i0 + (ng == 1 ? (int)threadIdx.x : (int)threadIdx.x - g * items);
-                    const bool in = item < items && g < ng;
-                    const int hd = item / (D / 4), d = item % (D / 4) * 4;
-                    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-                    float ss = 0.f;
-                    const float top = in ? stat[0][0][hd] : 0.f;
-                    if (in)
-#pragma unroll 4
-                        for (int x = g; x < n; x += ng) {
-                            const float* p = share(x);
-                            const float2 ms = load_through(p + kKvHeads * D + 2 * hd);
-                            const float2 y0 = load_through(p + hd * D + d), y1 = load_through(p + hd * D + d + 2);
-                            const float fx = ms.x == -INFINITY ? 0.f : exp2_(ms.x - top);
-                            if (fx != 0.f) {
-                                ss += fx * ms.y;
-                                v += fx * f32x4{y0.x, y0.y, y1.x, y1.y};
-                            }
-                        }
-                    if (ng > 1) {
-                        if (in) {
-                            reinterpret_cast<f32x4*>(lds)[threadIdx.x] = v;
-                            fl[kNW * 64 * 4 + threadIdx.x] = ss;
-                        }
-                        __syncthreads();
-                        if (threadIdx.x < items)
-                            for (int x = 1; x < ng; ++x) {
-                                v += reinterpret_cast<f32x4*>(lds)[x * items + threadIdx.x];
-                                ss += fl[kNW * 64 * 4 + x * items + threadIdx.x];
-                            }
+                float tn = top;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (x0 + x * ng < n) tn = fmaxf(tn, ms[x].x);
+                const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
+                top = tn;
+                ss *= fo;
+                v *= fo;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (x0 + x * ng < n) {
+                        const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
+                        ss += fx * ms[x].y;
+                        if (fx != 0.f) v += fx * f32x4{y0[x].x, y0[x].y, y1[x].x, y1[x].y};
                     }
-                    if (in && g == 0) finish(hd, d, v, top, ss);
-                }
+            }
+        if (ng > 1) {
+            f32x4* const fv = reinterpret_cast<f32x4*>(lds);
+            float2* const fs = reinterpret_cast<float2*>(lds + NT);
+            fv[threadIdx.x] = v;
+            fs[threadIdx.x] = float2{top, ss};
+        }
+        __syncthreads();
+        if (ng > 1 && g == 0) {
+            const f32x4* const fv = reinterpret_cast<const f32x4*>(lds);
+            const float2* const fs = reinterpret_cast<const float2*>(lds + NT);
+            float tn = top;
+            for (int x = 1; x < ng; ++x) tn = fmaxf(tn, fs[x * items + threadIdx.x].x);
+            const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
+            top = tn;
+            ss *= fo;
+            v *= fo;
+            for (int x = 1; x < ng; ++x) {
+                const float2 y = fs[x * items + threadIdx.x];
+                const float fx = y.x == -INFINITY ? 0.f : exp2_(y.x - top);
+                ss += fx * y.y;
+                if (fx != 0.f) v += fx * fv[x * items + threadIdx.x];
             }
         }
-        // on to the next head or sequence
-        r += t1 - t0;
-        if (r >= r1) return;
-        __syncthreads();
-        t0 = 0;
-        if (++h == HH) {
-            h = 0;
-            seq0 += (unsigned long long)HH * tiles;
-            if (++bi == 64) {
-                bi = 0;
-                b0 += 64;
-                mine = seq_of(a, b0 + l);
+        if (g == 0) {
+            if (level) {
+                finish(b, hd.hq0 + hq, d, v, top, ss);
+            } else {                                               // the group's share takes its first one's place
+                float* const p = share(0);
+                store_through(p + hq * D + d, v[0], v[1]);
+                store_through(p + hq * D + d + 2, v[2], v[3]);
+                if (d == 0) store_through(p + kKvHeads * D + 2 * hq, top, ss);
             }
         }
     }
@@ -485,7 +684,7 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) {
                     for (int g = 0; g < G; ++g) {
                         const float s = a.logits[(((size_t)pg * a.c.hq + h * G + g) << psh) + ((int)e & pmask)];
                         const float z = a.lse2[(long long)b * a.c.hq + h * G + g];
-                        if (z != -INFINITY) v += exp2_(s - z);
+                        if (z != -INFINITY) v += exp2_(fmaf(s, a.score_scale, -z));
                     }
                     a.c.weight[(((size_t)pg * hkv + h) << psh) + ((int)e & pmask)] += v;
                 }
@@ -495,18 +694,24 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) {
     }
 }
 
+#ifndef ATT_NW
+#define ATT_NW 8
+#define ATT_EU 2
+#define ATT_GRID 256
+#endif
 template <int D, bool FP8>
 hipError_t launch(const KvAttendArgs& a, bool accumulate, hipStream_t s) {
+    constexpr int NW = ATT_NW, EU = ATT_EU;
     // no more workgroups than the table rows could have work for
     const long long G = a.c.hq / a.c.hkv, HH = a.c.hkv * ((G + kKvHeads - 1) / kKvHeads);
     const long long tiles = (((long long)a.c.width << a.c.ps_shift) + 31) / 32 * a.B * HH;
     int grid = 1;
-    while (grid < kKvAttendGrid && (long long)grid * kNW < tiles) grid *= 2;
+    while (grid < ATT_GRID && (long long)grid * NW < tiles) grid *= 2;
     if (!accumulate) {
-        kv_attend_kernel<D, FP8, false><<<grid, kNW * 64, 0, s>>>(a);
+        kv_attend_kernel<D, FP8, false, NW, EU><<<grid, NW * 64, 0, s>>>(a);
         return hipGetLastError();
     }
-    kv_attend_kernel<D, FP8, true><<<grid, kNW * 64, 0, s>>>(a);
+    kv_attend_kernel<D, FP8, true, NW, EU><<<grid, NW * 64, 0, s>>>(a);
     const long long blocks = (((long long)a.c.width << a.c.ps_shift) + 255) / 256 * a.B * a.c.hkv;
     kv_weigh_kernel<<<(int)std::min(blocks, 1024LL), 256, 0, s>>>(a);
     return hipGetLastError();
