@@ -33,12 +33,12 @@ struct Seq {
 };
 
 __device__ __forceinline__ Seq seq_of(const KvAttendArgs& a, int b) {
-    Seq s{0, 0, 0u};
-    if (b >= a.B) return s;
-    s.len = kv_len(a.c, a.lens, b);
-    s.first = a.starts ? max(a.starts[b], 0) : 0;
+    const int at = min(b, a.B - 1), cap = a.c.width << a.c.ps_shift;     // (at most 2^30)
+    Seq s;
+    s.len = min(max(a.lens[at], 0), cap);
+    s.first = a.starts ? max(a.starts[at], 0) : 0;
     if (s.first >= s.len) s.len = s.first = 0;
-    s.tiles = max(1u, (unsigned)(s.len - (s.first & ~15) + 31) >> 5);
+    s.tiles = b < a.B ? max(1u, (unsigned)(s.len - (s.first & ~15) + 31) >> 5) : 0u;
     return s;
 }
 
@@ -144,6 +144,8 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     const int psh = a.c.ps_shift, pmask = (1 << psh) - 1;
 
     // the line, this workgroup's stretch and the wave's part of it
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b < a.B; b += NT) (void)kv_len(a.c, a.lens, b);     // (flags lengths that are none)
     Seq four[4];                                    // sequences c0 + 64 i + lane
     unsigned incl[4], sum4[4], total = 0;
     auto look_four = [&](int c0) __attribute__((always_inline)) {
@@ -240,7 +242,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     // the cursor's tile, its page numbers on their way
     auto look = [&](bool used) __attribute__((always_inline)) {
         typedef const __attribute__((address_space(4))) int* cint;
-        const cint trow = (cint)(a.c.table + (long long)cb * a.c.tstride);
+        const cint trow = (cint)(a.c.table + (long long)uni(cb) * a.c.tstride);
         Tile x;
         x.b = cb;
         x.h = ch;
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int e = x.e + 16 * j, rows = used ? clen - e : 0;
-            x.page[j] = trow[rows > 0 ? e >> psh : 0];
+            x.page[j] = trow[uni(rows > 0 ? e >> psh : 0)];
             x.n[j] = min(16, max(0, rows));
             x.lo[j] = max(0, cfirst - e);
         }
@@ -277,7 +279,10 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     auto load = [&](u32x4 (&x)[2][NL], const char* base_, const Tile& tl) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const __amdgpu_buffer_rsrc_t rs = buf_rsrc(base_ + tl.at[j], (unsigned)tl.n[j] * ROW);
+            // (the compiler does not see that these are the same in all lanes)
+            const unsigned lo = (unsigned)uni((int)(unsigned)tl.at[j]), hi = (unsigned)uni((int)(unsigned)(tl.at[j] >> 32));
+            const __amdgpu_buffer_rsrc_t rs =
+                buf_rsrc(base_ + ((unsigned long long)hi << 32 | lo), (unsigned)uni(tl.n[j]) * ROW);
 #pragma unroll
             for (int i = 0; i < NL; ++i) x[j][i] = buf16(rs, l * 16 + i * 1024);
         }
@@ -305,7 +310,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     };
     u32x4* const buf = lds + w * 2 * BUF;
     // rows as they were loaded (a block is contiguous) into LDS, bf16
-    auto put = [&](const u32x4 (&x)[2][NL], const Tile& tl, bool value) __attribute__((always_inline)) {
+    auto put = [&](const u32x4 (&x)[2][NL], bool value) __attribute__((always_inline)) {
         constexpr int LPR = ROW / 16;               // lanes of a row
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
@@ -313,9 +318,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
                 const int row = i * (64 / LPR) + l / LPR, c = l % LPR, rr = j * 16 + row;
-                u32x4 v = x[j][i];
-                // (a value before the first entry may be NaN, and 0 times NaN is one)
-                if (value && tl.lo[j] > 0 && row < tl.lo[j]) v = u32x4{0, 0, 0, 0};
+                const u32x4 v = x[j][i];
                 if constexpr (FP8) {
                     const u32x4 y0 = bf16_of(v[0], v[1]), y1 = bf16_of(v[2], v[3]);
                     buf[value ? v_at<D>(rr, 2 * c) : k_at<D>(rr, 2 * c)] = y0;
@@ -373,7 +376,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
         bool first = cur.first;                     // the wave has the sequence's first tile
         for (int i = 0; i < left; ++i) {
             locate(nxt);
-            put(kr, cur, false);
+            put(kr, false);
             load(kr, a.c.K, nxt);
             // scores^T: lane = head lr, entries 4 lg + i of each block
             f32x4 s[2];
@@ -426,7 +429,15 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
                     hi[j * 2 + e / 2] = __builtin_amdgcn_perm(uy, ux, 0x07060302u);
                     lo[j * 2 + e / 2] = pk_bf16(x - __uint_as_float(ux & 0xffff0000u), y - __uint_as_float(uy & 0xffff0000u)) | 0x00010001u;
                 }
-            put(vr, cur, true);
+            // (a value before the first entry may be NaN, and 0 times NaN is one)
+            if ((cur.lo[0] | cur.lo[1]) > 0) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int n = 0; n < NL; ++n)
+                        if (n * (1024 / ROW) + l / (ROW / 16) < cur.lo[j]) vr[j][n] = u32x4{0, 0, 0, 0};
+            }
+            put(vr, true);
             load(vr, a.c.V, nxt);
             advance();
             const Tile far = look(i + 2 < left);
@@ -493,20 +504,25 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
         const bool has_first = i0 & 1, whole = has_first && (lasts & members);
         const Heads hd = heads_of(h);
         float* const part = a.part + (size_t)(2 * blockIdx.x + (has_first ? 1 : 0)) * kv_part_floats(D);
-        auto piece = [&](int z) __attribute__((always_inline)) { return z && z < n ? 1 : has_first ? 0 : 1; };
-        auto wave = [&](int z) __attribute__((always_inline)) { return z < n ? pw + z : pw; };
+        auto piece = [&](int z) __attribute__((always_inline)) { return (z && z < n) | !has_first; };
+        auto wave = [&](int z) __attribute__((always_inline)) { return pw + (z < n ? z : 0); };
         if (head < hd.n) {
-            float f[NW], M = -INFINITY, S = 0.f;
+            float f[NW], s[NW], M = -INFINITY, S = 0.f;
 #pragma unroll
             for (int z = 0; z < NW; ++z) {
-                f[z] = z < n ? stat[wave(z)][piece(z)][0][head] : -INFINITY;
+                f[z] = stat[wave(z)][piece(z)][0][head];
+                s[z] = stat[wave(z)][piece(z)][1][head];
+            }
+#pragma unroll
+            for (int z = 0; z < NW; ++z) {
+                f[z] = z < n ? f[z] : -INFINITY;
+                s[z] = z < n ? s[z] : 0.f;
                 M = fmaxf(M, f[z]);
             }
 #pragma unroll
             for (int z = 0; z < NW; ++z) {
                 f[z] = f[z] == -INFINITY ? 0.f : exp2_(f[z] - M);
-                const float x = stat[wave(z)][piece(z)][1][head];
-                S += z < n ? f[z] * x : 0.f;                        // (a NaN stays one)
+                S += f[z] * s[z];                                   // (a NaN stays one)
             }
             if (threadIdx.x < DT * 64) {
                 f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
