@@ -68,9 +68,9 @@ struct KvAttendArgs {
 struct KvEvictArgs {
     KvCache c;
     int* lens;
-    int B, budget, recent;
+    int B, budget, recent, n_cu;
     int* scratch;         // [n_pages][hkv][page]: the places to fill and what fills them
-    int* moves;           // [B][hkv] how many
+    unsigned* count;      // [B][hkv], then [B]: zero between calls
 };
 
 hipError_t launch_kv_append(const KvAppendArgs& a, int head_dim, bool fp8, hipStream_t s);

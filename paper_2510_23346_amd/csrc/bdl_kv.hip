@@ -3,69 +3,156 @@
 
 namespace bdl {
 
+namespace {
+
 // ------------------------------------------------------------------ append
-// One thread per pair of a q or k row, or per two elements of a v row.
 // Rotation: y1 = x1 c - x2 s, y2 = x2 c + x1 s in fp32, every product and sum
 // rounded by itself (no fused multiply-add), so that the result is that of
 // the two lines as written.
-template <bool FP8>
-__device__ __forceinline__ void kv_put(char* base, long long entry, int D, int d, float x, float inv) {
-    if (FP8)
-        reinterpret_cast<uint8_t*>(base)[entry * D + d] = (uint8_t)f2e4m3(x * inv);
-    else
-        reinterpret_cast<uint16_t*>(base)[entry * D + d] = f2bf(x);
+//
+// Bound by its memory traffic.  A thread takes 16 numbers of one head of one
+// token, those whose pairs it needs: two 16-byte loads, two 16-byte stores (8
+// bytes each into an 8-bit cache).  A workgroup's threads are units x tokens
+// (x, y), so that no index needs a division by the number of heads.
+__device__ __forceinline__ void unpack8(u32x4 v, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(v[i] << 16);
+        x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+}
+
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pk_bf16(x[2 * i], x[2 * i + 1]);
+    return v;
+}
+
+__device__ __forceinline__ uint2 pack8_e4m3(const float (&x)[8], float inv) {
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float c[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c[k] = clamp_e4m3(x[4 * i + k] * inv);
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
+        w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], r, true);
+    }
+    return uint2{w[0], w[1]};
 }
 
 template <int D, bool FP8>
-__global__ void kv_append_kernel(const KvAppendArgs a) {
+__global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
 #pragma clang fp contract(off)
-    const int t = blockIdx.x, H = a.c.hq + 2 * a.c.hkv;
+    const int t = blockIdx.x * blockDim.y + threadIdx.y, u = blockIdx.y * blockDim.x + threadIdx.x;
+    const int H = a.c.hq + 2 * a.c.hkv, h = u / (D / 16), j = u % (D / 16);
+    if (t >= a.T || h >= H) return;
+    const bool v = h >= a.c.hq + a.c.hkv, pairs = v || a.interleaved;
+    const int d0 = pairs ? 16 * j : 8 * j, d1 = pairs ? 16 * j + 8 : D / 2 + 8 * j;
+    const uint16_t* x = a.qkv + t * a.qkv_stride + h * D;
+    const u32x4 x0 = ld16(x + d0), x1 = ld16(x + d1);
     const int seq = a.seqs[t], i = a.index[t], pos = a.positions[t];
-    const bool pad = seq == -1, pos_ok = pos >= 0 && pos < a.n_positions;
-    const bool at_ok = seq >= 0 && seq < a.n_seqs && i >= 0 && (long long)i < ((long long)a.c.width << a.c.ps_shift);
-    if (threadIdx.x == 0 && (!pos_ok || (!pad && !at_ok))) kv_error(a.c);
-    for (int u = threadIdx.x; u < H * (D / 2); u += blockDim.x) {
-        const int h = u / (D / 2), j = u % (D / 2);
-        const bool v = h >= a.c.hq + a.c.hkv;
-        const int d0 = v || a.interleaved ? 2 * j : j, d1 = v || a.interleaved ? 2 * j + 1 : j + D / 2;
-        const uint16_t* x = a.qkv + t * a.qkv_stride + h * D;
-        float y0 = bf2f(x[d0]), y1 = bf2f(x[d1]);
-        if (!v) {
-            const float c = pos_ok ? a.cos[(long long)pos * (D / 2) + j] : 0.f, s = pos_ok ? a.sin[(long long)pos * (D / 2) + j] : 0.f;
-            const float z0 = y0 * c - y1 * s, z1 = y1 * c + y0 * s;
-            y0 = pos_ok ? z0 : 0.f;
-            y1 = pos_ok ? z1 : 0.f;
+    const int cap = a.c.width << a.c.ps_shift;
+    const bool pos_ok = pos >= 0 && pos < a.n_positions, at_ok = seq >= 0 && seq < a.n_seqs && i >= 0 && i < cap;
+    float y0[8], y1[8];
+    unpack8(x0, y0);
+    unpack8(x1, y1);
+    if (!v) {
+        const long long at = (long long)(pos_ok ? pos : 0) * (D / 2) + 8 * j;
+        float c[8], s[8];
+#pragma unroll
+        for (int k = 0; k < 8; k += 4) {
+            const float4 cc = *reinterpret_cast<const float4*>(a.cos + at + k), ss = *reinterpret_cast<const float4*>(a.sin + at + k);
+            c[k] = cc.x, c[k + 1] = cc.y, c[k + 2] = cc.z, c[k + 3] = cc.w;
+            s[k] = ss.x, s[k + 1] = ss.y, s[k + 2] = ss.z, s[k + 3] = ss.w;
         }
-        if (h < a.c.hq) {
-            uint16_t* q = a.q_out + t * a.q_stride + h * D;
-            q[d0] = f2bf(y0);
-            q[d1] = f2bf(y1);
-        } else if (at_ok && pos_ok) {
-            const int kh = (h - a.c.hq) % a.c.hkv;
-            const long long e = kv_entry(a.c, seq, kh, i);
-            if (e < 0) continue;
-            kv_put<FP8>(v ? a.c.V : a.c.K, e, D, d0, y0, v ? a.v_inv : a.k_inv);
-            kv_put<FP8>(v ? a.c.V : a.c.K, e, D, d1, y1, v ? a.v_inv : a.k_inv);
-            if (v && j == 0 && a.c.weight) {
-                a.c.weight[e] = 0.f;
-                a.c.pos[e] = pos;
+        if (a.interleaved) {
+            // pairs (2k, 2k + 1): y0 holds pairs 0..3, y1 pairs 4..7
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float a0 = y0[2 * k], b0 = y0[2 * k + 1], a1 = y1[2 * k], b1 = y1[2 * k + 1];
+                y0[2 * k] = a0 * c[k] - b0 * s[k];
+                y0[2 * k + 1] = b0 * c[k] + a0 * s[k];
+                y1[2 * k] = a1 * c[k + 4] - b1 * s[k + 4];
+                y1[2 * k + 1] = b1 * c[k + 4] + a1 * s[k + 4];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float a0 = y0[k], b0 = y1[k];
+                y0[k] = a0 * c[k] - b0 * s[k];
+                y1[k] = b0 * c[k] + a0 * s[k];
             }
         }
+        if (!pos_ok)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y0[k] = y1[k] = 0.f;
     }
-    if (threadIdx.x == 0 && a.lens && at_ok && pos_ok && kv_entry(a.c, seq, 0, i) >= 0) atomicMax(a.lens + seq, i + 1);
+    if (h < a.c.hq) {
+        uint16_t* q = a.q_out + t * a.q_stride + h * D;
+        *reinterpret_cast<u32x4*>(q + d0) = pack8(y0);
+        *reinterpret_cast<u32x4*>(q + d1) = pack8(y1);
+        if (u == 0) {
+            if (!pos_ok || (seq != -1 && !at_ok)) kv_error(a.c);
+            if (a.lens && at_ok && pos_ok && kv_entry(a.c, seq, 0, i) >= 0) {
+                // (a prompt's tokens would all raise one number: only the last
+                // of a run does)
+                bool covered = false;
+                if (t + 1 < a.T && a.seqs[t + 1] == seq) {
+                    const int i1 = a.index[t + 1], p1 = a.positions[t + 1];
+                    covered = i1 > i && i1 < cap && p1 >= 0 && p1 < a.n_positions && kv_entry(a.c, seq, 0, i1) >= 0;
+                }
+                if (!covered) atomicMax(a.lens + seq, i + 1);
+            }
+        }
+        return;
+    }
+    if (!at_ok || !pos_ok) return;
+    const int kh = h - a.c.hq - (v ? a.c.hkv : 0);
+    const long long e = kv_entry(a.c, seq, kh, i);
+    if (e < 0) return;
+    char* const base = (v ? a.c.V : a.c.K) + e * (D * (FP8 ? 1 : 2));
+    if constexpr (FP8) {
+        const float inv = v ? a.v_inv : a.k_inv;
+        *reinterpret_cast<uint2*>(base + d0) = pack8_e4m3(y0, inv);
+        *reinterpret_cast<uint2*>(base + d1) = pack8_e4m3(y1, inv);
+    } else {
+        *reinterpret_cast<u32x4*>(base + 2 * d0) = v ? x0 : pack8(y0);
+        *reinterpret_cast<u32x4*>(base + 2 * d1) = v ? x1 : pack8(y1);
+    }
+    if (v && j == 0 && a.c.weight) {
+        a.c.weight[e] = 0.f;
+        a.c.pos[e] = pos;
+    }
 }
 
-hipError_t launch_kv_append(const KvAppendArgs& a, int head_dim, bool fp8, hipStream_t s) {
-    if (head_dim == 64)
-        fp8 ? kv_append_kernel<64, true><<<a.T, 256, 0, s>>>(a) : kv_append_kernel<64, false><<<a.T, 256, 0, s>>>(a);
-    else
-        fp8 ? kv_append_kernel<128, true><<<a.T, 256, 0, s>>>(a) : kv_append_kernel<128, false><<<a.T, 256, 0, s>>>(a);
+template <int D, bool FP8>
+hipError_t append(const KvAppendArgs& a, hipStream_t s) {
+    const int units = (a.c.hq + 2 * a.c.hkv) * (D / 16), x = std::min(units, 256), y = 256 / x;
+    kv_append_kernel<D, FP8><<<dim3((a.T + y - 1) / y, (units + x - 1) / x), dim3(x, y), 0, s>>>(a);
     return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ evict
+// One launch.  The workgroups (sequence, kv head, z) of one sequence and head
+// all select the entries that stay (it reads 8 bytes an entry, what an
+// exchange between them would cost more than), and each moves its share of the
+// keys and values.  Weights and positions, which the selection reads, are moved
+// by the workgroup that is the last of its head to have selected; the length is
+// set by the last of its sequence.
+//
+// Selection: the rank key of the last entry that stays, found in three passes
+// over the keys (11, 11 and 10 bits; histograms in LDS), then places and
+// sources by prefix sums.  A thread owns consecutive entries.  Their keys are
+// kept in registers (4096 entries of a sequence) or LDS (28672), and read
+// again in each pass above that.
+constexpr int kET = 1024, kEW = kET / 64;
+constexpr int kRegEntries = 4 * kET, kLdsEntries = 28 * kET;
+constexpr int kListCap = 4096;          // moves whose lists fit LDS; more go through a.scratch
+
 // An entry's rank key: the protected ones above all, then the weights in
-// their order, a NaN below all.
+// their order, a NaN below all
 __device__ __forceinline__ unsigned kv_key(float w, bool prot) {
     const unsigned u = __float_as_uint(w);
     if (prot) return 0xffffffffu;
@@ -74,101 +161,276 @@ __device__ __forceinline__ unsigned kv_key(float w, bool prot) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ int block_sum(int v, int* red) {
-    v = wave_total(wave_incl_scan(v));
+struct EvictLds {
+    unsigned hist[2048];
+    int freed[kListCap], moved[kListCap];
+    int wave[2][kEW];
+    unsigned digit, need;
+    int last;
+};
+
+// exclusive prefix sum over the workgroup; total in *total
+__device__ __forceinline__ int block_scan(int v, int* total, int* waves) {
+    const int incl = wave_incl_scan(v), l = threadIdx.x & 63;
+    if (l == 63) waves[threadIdx.x >> 6] = incl;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return red[0] + red[1] + red[2] + red[3];
+    const int s = wave_incl_scan(l < kEW ? waves[l] : 0), w = wave_id();
+    *total = __builtin_amdgcn_readlane(s, kEW - 1);
+    return incl - v + (w ? __builtin_amdgcn_readlane(s, w - 1) : 0);
 }
 
-// Selection: one workgroup per (sequence, kv head).  The budget's smallest
-// kept key is found bit by bit; then the entries are passed once in order.
-__global__ void kv_select_kernel(const KvEvictArgs a) {
-    __shared__ int red[4];
-    const int b = blockIdx.x, h = blockIdx.y, n = kv_len(a.c, a.lens, b), M = a.budget;
-    if (n <= M) {
-        if (threadIdx.x == 0) a.moves[b * a.c.hkv + h] = 0;
-        return;
-    }
-    int last = (int)0x80000000;
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const long long e = kv_entry(a.c, b, h, i);
-        if (e >= 0) last = max(last, a.c.pos[e]);
-    }
-    for (int k = 32; k; k >>= 1) last = max(last, __shfl_xor(last, k));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = last;
-    __syncthreads();
-    last = max(max(red[0], red[1]), max(red[2], red[3]));
-    auto key = [&](int i) {
-        const long long e = kv_entry(a.c, b, h, i);
-        return e < 0 ? 0u : kv_key(a.c.weight[e], (long long)a.c.pos[e] > (long long)last - a.recent);
+// Entries 4 g .. 4 g + 3 of a sequence (they lie in one page): their first
+// place among the entries of all pages, or -1
+__device__ __forceinline__ long long four_at(const KvCache& c, int b, int h, int g) {
+    return kv_entry(c, b, h, 4 * g);
+}
+
+enum Keep { kRegs, kLds, kReread };
+
+template <Keep KEEP>
+__device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int n, EvictLds& L, uint4* keys) {
+    const int tid = threadIdx.x, M = a.budget, groups = (n + 3) / 4;
+    const int per = KEEP == kRegs ? 1 : (groups + kET - 1) / kET, g0 = tid * per;
+    auto get = [&](int g, float4& ww, int4& pp) __attribute__((always_inline)) {
+        ww = float4{NAN, NAN, NAN, NAN};
+        pp = int4{INT_MIN, INT_MIN, INT_MIN, INT_MIN};
+        if (g >= groups) return;
+        const long long e = four_at(a.c, b, h, g);
+        if (e < 0) return;
+        ww = *reinterpret_cast<const float4*>(a.c.weight + e);
+        pp = *reinterpret_cast<const int4*>(a.c.pos + e);
     };
-    // the largest t with at least M keys >= t
-    unsigned t = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        int v = 0;
-        for (int i = threadIdx.x; i < n; i += 256) v += key(i) >= (t | 1u << bit);
-        if (block_sum(v, red) >= M) t |= 1u << bit;
+    // the largest position
+    float4 w;
+    int4 p;
+    int last = INT_MIN;
+    for (int i = tid; i < 2048; i += kET) L.hist[i] = 0;
+    if (tid == 0) L.last = INT_MIN;
+#pragma unroll 2
+    for (int k = 0; k < per; ++k) {
+        get(g0 + k, w, p);
+        const int i = 4 * (g0 + k);
+        if (i < n) last = max(last, p.x);
+        if (i + 1 < n) last = max(last, p.y);
+        if (i + 2 < n) last = max(last, p.z);
+        if (i + 3 < n) last = max(last, p.w);
     }
-    int v = 0;
-    for (int i = threadIdx.x; i < n; i += 256) v += key(i) > t;
-    const int ties = M - block_sum(v, red);       // of the entries with key t, so many stay
-    int eq0 = 0, free0 = 0, move0 = 0;
-    for (int i0 = 0; i0 < n; i0 += 256) {
-        const int i = i0 + threadIdx.x;
-        const unsigned k = i < n ? key(i) : 0u;
-        auto scan = [&](int x, int& base) {       // exclusive prefix over the workgroup, continued
-            const int incl = wave_incl_scan(x);
-            __syncthreads();
-            if ((threadIdx.x & 63) == 63) red[threadIdx.x >> 6] = incl;
-            __syncthreads();
-            int at = base + incl - x;
-            for (int q = 0; q < 4; ++q) {
-                if (q < (int)(threadIdx.x >> 6)) at += red[q];
-                base += red[q];
+#pragma unroll
+    for (int x = 32; x; x >>= 1) last = max(last, __shfl_xor(last, x));
+    __syncthreads();
+    if ((tid & 63) == 0) atomicMax(&L.last, last);
+    __syncthreads();
+    const long long floor_ = (long long)L.last - a.recent;
+    auto key4 = [&](const float4& ww, const int4& pp) __attribute__((always_inline)) {
+        return uint4{kv_key(ww.x, pp.x > floor_), kv_key(ww.y, pp.y > floor_), kv_key(ww.z, pp.z > floor_), kv_key(ww.w, pp.w > floor_)};
+    };
+    uint4 key = key4(w, p);
+    if constexpr (KEEP == kLds) {
+#pragma unroll 2
+        for (int k = 0; k < per; ++k) {
+            get(g0 + k, w, p);
+            keys[k * kET + tid] = key4(w, p);
+        }
+    }
+    // f(entry, key) for the thread's entries in order
+    auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int k = 0; k < per; ++k) {
+            if constexpr (KEEP == kLds) key = keys[k * kET + tid];
+            if constexpr (KEEP == kReread) {
+                get(g0 + k, w, p);
+                key = key4(w, p);
             }
-            return at;
-        };
-        const int eq = i < n && k == t, r = scan(eq, eq0);
-        const bool kept = i < n && (k > t || (eq && r < ties));
-        const int fr = i < M && !kept, mv = i >= M && kept;
-        const int fk = scan(fr, free0), mk = scan(mv, move0);
-        if (fr || mv) {
-            const long long e = kv_entry(a.c, b, h, fr ? fk : M + mk);
+            const int i = 4 * (g0 + k);
+            if (i < n) f(i, key.x);
+            if (i + 1 < n) f(i + 1, key.y);
+            if (i + 2 < n) f(i + 2, key.z);
+            if (i + 3 < n) f(i + 3, key.w);
+        }
+    };
+    // the M-th largest key, 11, 11 and 10 bits at a time
+    unsigned known = 0, need = M;       // its leading bits; how many of the keys with these bits stay
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+        const unsigned mask = pass == 2 ? 1023u : 2047u;
+        each([&](int, unsigned k) __attribute__((always_inline)) {
+            if (pass && (k >> above) != known) return;
+            const unsigned dgt = (k >> shift) & mask;
+            // (where a wave's keys agree, one lane counts them)
+            const unsigned first = (unsigned)__builtin_amdgcn_readfirstlane((int)dgt);
+            const unsigned long long act = __ballot(1), same = __ballot(dgt == first);
+            if (same == act) {
+                if ((int)(threadIdx.x & 63) == __ffsll((long long)act) - 1) atomicAdd(&L.hist[first], (unsigned)__popcll(act));
+            } else {
+                atomicAdd(&L.hist[dgt], 1u);
+            }
+        });
+        __syncthreads();
+        // bins from the top: thread t has 2047 - 2 t and 2046 - 2 t
+        const unsigned c0 = L.hist[2047 - 2 * tid], c1 = L.hist[2046 - 2 * tid];
+        int total;
+        const unsigned before = (unsigned)block_scan((int)(c0 + c1), &total, L.wave[0]);
+        if (before < need && need <= before + c0) {
+            L.digit = 2047 - 2 * tid;
+            L.need = need - before;
+        } else if (before + c0 < need && need <= before + c0 + c1) {
+            L.digit = 2046 - 2 * tid;
+            L.need = need - before - c0;
+        }
+        L.hist[2047 - 2 * tid] = 0;
+        L.hist[2046 - 2 * tid] = 0;
+        __syncthreads();
+        known = pass == 2 ? known << 10 | L.digit : known << 11 | L.digit;
+        need = L.need;
+    }
+    // entries with that key: the first `need` of them stay
+    int eq = 0, total;
+    each([&](int, unsigned k) __attribute__((always_inline)) { eq += k == known; });
+    const int eq0 = block_scan(eq, &total, L.wave[0]);
+    int fr = 0, mv = 0;
+    eq = eq0;
+    each([&](int i, unsigned k) __attribute__((always_inline)) {
+        const bool kept = k > known || (k == known && eq++ < (int)need);
+        fr += i < M && !kept;
+        mv += i >= M && kept;
+    });
+    int moves;
+    const int fr0 = block_scan(fr, &moves, L.wave[1]);
+    __syncthreads();
+    const int mv0 = block_scan(mv, &total, L.wave[0]);
+    fr = fr0;
+    mv = mv0;
+    eq = eq0;
+    const bool in_lds = moves <= kListCap;
+    each([&](int i, unsigned k) __attribute__((always_inline)) {
+        const bool kept = k > known || (k == known && eq++ < (int)need);
+        const bool f = i < M && !kept, m = i >= M && kept;
+        if (!f && !m) return;
+        const int at = f ? fr++ : mv++;
+        if (in_lds) {
+            (f ? L.freed : L.moved)[at] = i;
+        } else {
+            const long long e = kv_entry(a.c, b, h, f ? at : M + at);
             if (e >= 0) a.scratch[e] = i;
         }
-    }
-    if (threadIdx.x == 0) a.moves[b * a.c.hkv + h] = free0;
+    });
+    return moves;
 }
 
-template <int ROW>
-__global__ void kv_move_kernel(const KvEvictArgs a) {
-    const int b = blockIdx.x, h = blockIdx.y, n = a.moves[b * a.c.hkv + h], l = threadIdx.x & 63;
-    for (int k = blockIdx.z * 4 + wave_id(); k < n; k += gridDim.z * 4) {
-        const long long ef = kv_entry(a.c, b, h, k), em = kv_entry(a.c, b, h, a.budget + k);
-        if (ef < 0 || em < 0) continue;
-        const long long to = kv_entry(a.c, b, h, a.scratch[ef]), from = kv_entry(a.c, b, h, a.scratch[em]);
-        if (to < 0 || from < 0) continue;
-        for (int x = l * 4; x < ROW; x += 256) {
-            *reinterpret_cast<uint32_t*>(a.c.K + to * ROW + x) = *reinterpret_cast<const uint32_t*>(a.c.K + from * ROW + x);
-            *reinterpret_cast<uint32_t*>(a.c.V + to * ROW + x) = *reinterpret_cast<const uint32_t*>(a.c.V + from * ROW + x);
+// LONG: rows of the page table that can name more than kRegEntries
+template <int ROW, bool LONG>
+__global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
+    __shared__ EvictLds L;
+    __shared__ uint4 keys[LONG ? kLdsEntries / 4 : 1];
+    __shared__ bool last_head;
+    const int b = blockIdx.x, h = blockIdx.y, z = blockIdx.z, Z = gridDim.z, M = a.budget;
+    const int raw = a.lens[b], n = kv_len(a.c, a.lens, b);
+    if (n <= M) {
+        // (a length that is none becomes one; reading it before or after is the same)
+        if (h == 0 && z == 0 && threadIdx.x == 0 && raw != n) a.lens[b] = n;
+        return;
+    }
+    int moves;
+    if (!LONG || n <= kRegEntries)
+        moves = kv_select<kRegs>(a, b, h, n, L, keys);
+    else if (n <= kLdsEntries)
+        moves = kv_select<kLds>(a, b, h, n, L, keys);
+    else
+        moves = kv_select<kReread>(a, b, h, n, L, keys);
+    // this workgroup has read what it needs of weights, positions and lengths
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        unsigned* const ch = a.count + (size_t)b * a.c.hkv + h;
+        unsigned* const cs = a.count + (size_t)gridDim.x * a.c.hkv + b;
+        const bool lh = __hip_atomic_fetch_add(ch, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)Z - 1;
+        const bool ls = __hip_atomic_fetch_add(cs, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)Z * a.c.hkv - 1;
+        if (lh) __hip_atomic_store(ch, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (ls) {
+            __hip_atomic_store(cs, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            a.lens[b] = M;
         }
-        if (l == 0) {
+        last_head = lh;
+    }
+    const bool in_lds = moves <= kListCap;
+    // place and source of move k, as entries of all pages; false where a page is none
+    auto move = [&](int k, long long& to, long long& from) __attribute__((always_inline)) {
+        int i, j;
+        if (in_lds) {
+            i = L.freed[k];
+            j = L.moved[k];
+        } else {
+            const long long ef = kv_entry(a.c, b, h, k), em = kv_entry(a.c, b, h, M + k);
+            if (ef < 0 || em < 0) return false;
+            i = a.scratch[ef];
+            j = a.scratch[em];
+        }
+        to = kv_entry(a.c, b, h, i);
+        from = kv_entry(a.c, b, h, j);
+        return to >= 0 && from >= 0;
+    };
+    // keys and values: LPR lanes a row, four moves in flight
+    constexpr int LPR = ROW / 16, RPP = kET / LPR, U = 4;
+    const int k1 = (int)((long long)moves * (z + 1) / Z), c = threadIdx.x % LPR * 16;
+    for (int k0 = (int)((long long)moves * z / Z) + threadIdx.x / LPR; k0 < k1; k0 += U * RPP) {
+        long long to[U], from[U];
+        bool ok[U];
+        u32x4 x[U], y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) ok[u] = k0 + u * RPP < k1 && move(k0 + u * RPP, to[u], from[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (ok[u]) {
+                x[u] = *reinterpret_cast<const u32x4*>(a.c.K + from[u] * ROW + c);
+                y[u] = *reinterpret_cast<const u32x4*>(a.c.V + from[u] * ROW + c);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (ok[u]) {
+                *reinterpret_cast<u32x4*>(a.c.K + to[u] * ROW + c) = x[u];
+                *reinterpret_cast<u32x4*>(a.c.V + to[u] * ROW + c) = y[u];
+            }
+    }
+    __syncthreads();
+    if (last_head)
+        for (int k = threadIdx.x; k < moves; k += kET) {
+            long long to, from;
+            if (!move(k, to, from)) continue;
             a.c.weight[to] = a.c.weight[from];
             a.c.pos[to] = a.c.pos[from];
         }
-    }
-    if (h == 0 && blockIdx.z == 0 && threadIdx.x == 0) a.lens[b] = min(kv_len(a.c, a.lens, b), a.budget);
 }
 
+}  // namespace
+
+hipError_t launch_kv_append(const KvAppendArgs& a, int head_dim, bool fp8, hipStream_t s) {
+    if (head_dim == 64) return fp8 ? append<64, true>(a, s) : append<64, false>(a, s);
+    return fp8 ? append<128, true>(a, s) : append<128, false>(a, s);
+}
+
+namespace {
+
+template <int ROW>
+void evict(const KvEvictArgs& a, const dim3& grid, bool many, hipStream_t s) {
+    if (many)
+        kv_evict_kernel<ROW, true><<<grid, kET, 0, s>>>(a);
+    else
+        kv_evict_kernel<ROW, false><<<grid, kET, 0, s>>>(a);
+}
+
+}  // namespace
+
 hipError_t launch_kv_evict(const KvEvictArgs& a, int head_dim, bool fp8, hipStream_t s) {
-    kv_select_kernel<<<dim3(a.B, a.c.hkv), 256, 0, s>>>(a);
-    const dim3 grid(a.B, a.c.hkv, 16);
+    // a workgroup per compute unit, and no more of a head than its moves could feed
+    const long long heads = (long long)a.B * a.c.hkv, cap = (long long)a.c.width << a.c.ps_shift;
+    const long long most = std::min<long long>(a.budget, std::max(0LL, cap - a.budget));
+    const int z = (int)std::max(1LL, std::min({a.n_cu / heads, (most + 63) / 64, 64LL}));
+    const dim3 grid(a.B, a.c.hkv, z);
+    const bool many = cap > kRegEntries;
     switch (head_dim * (fp8 ? 1 : 2)) {
-    case 64: kv_move_kernel<64><<<grid, 256, 0, s>>>(a); break;
-    case 128: kv_move_kernel<128><<<grid, 256, 0, s>>>(a); break;
-    default: kv_move_kernel<256><<<grid, 256, 0, s>>>(a); break;
+    case 64: evict<64>(a, grid, many, s); break;
+    case 128: evict<128>(a, grid, many, s); break;
+    default: evict<256>(a, grid, many, s); break;
     }
     return hipGetLastError();
 }

@@ -26,7 +26,7 @@ struct bdlora_kv {
     unsigned* count = nullptr;     // [max_seqs][n_kv_heads][head tiles]
     unsigned* group_count = nullptr;   // [2 kKvAttendGrid]
     float* logits = nullptr;       // [n_pages][n_q_heads][page_size]
-    int* moves = nullptr;          // [max_seqs][n_kv_heads]
+    unsigned* evict_count = nullptr;   // [max_seqs][n_kv_heads + 1]
     int* scratch = nullptr;        // [n_pages][n_kv_heads][page_size], where logits lie too
 };
 
@@ -82,7 +82,7 @@ int check_desc(const bdlora_kv_desc* d) {
 }
 
 struct Parts {
-    long long clear, err, count, group_count, part, lse2, moves, logits, total;   // (what starts at zero lies below clear)
+    long long clear, err, count, group_count, evict_count, part, lse2, logits, total;   // (what starts at zero lies below clear)
 };
 
 Parts layout(const bdlora_kv_desc& d, bool weights) {
@@ -97,10 +97,10 @@ Parts layout(const bdlora_kv_desc& d, bool weights) {
     p.err = take(4);
     p.count = take(4LL * d.max_seqs * d.n_kv_heads * ((group + bdl::kKvHeads - 1) / bdl::kKvHeads));
     p.group_count = take(2LL * bdl::kKvAttendGrid * 4);
+    p.evict_count = take(weights ? 4LL * d.max_seqs * (d.n_kv_heads + 1) : 0);
     p.clear = at;
     p.part = take(2LL * bdl::kKvAttendGrid * bdl::kv_part_floats(d.head_dim) * 4);
     p.lse2 = take(weights ? 4LL * d.max_seqs * d.n_q_heads : 0);
-    p.moves = take(weights ? 4LL * d.max_seqs * d.n_kv_heads : 0);
     p.logits = take(weights ? 4LL * d.n_pages * d.n_q_heads * d.page_size : 0);
     p.total = at;
     return p;
@@ -196,7 +196,7 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
         c->part = (float*)(ws + p.part);
         c->lse2 = (float*)(ws + p.lse2);
         c->logits = (float*)(ws + p.logits);
-        c->moves = (int*)(ws + p.moves);
+        c->evict_count = (unsigned*)(ws + p.evict_count);
         c->scratch = (int*)(ws + p.logits);
         *out = c;
         return BDLORA_OK;
@@ -335,7 +335,8 @@ int bdlora_kv_evict(bdlora_kv_t c, int32_t B, const int32_t* table, int64_t tabl
         a.budget = budget;
         a.recent = recent;
         a.scratch = c->scratch;
-        a.moves = c->moves;
+        a.count = c->evict_count;
+        a.n_cu = c->n_cu;
         if (hipError_t e = bdl::launch_kv_evict(a, c->d.head_dim, c->d.format == BDLORA_KV_FP8_E4M3, (hipStream_t)stream))
             return hip_fail("evict launch", e);
         return BDLORA_OK;

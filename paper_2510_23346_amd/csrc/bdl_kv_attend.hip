@@ -97,12 +97,6 @@ __device__ __forceinline__ u32x4 bf16_of(uint32_t a, uint32_t b) {
     return r;
 }
 
-__device__ __forceinline__ uint32_t pk_bf16(float x, float y) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
-}
-
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -138,7 +132,6 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     __shared__ int4 info[2 * NW];                   // [wave][piece 1, 0]: sequence (-1: none), head, first and last tile it has, tiles
     __shared__ unsigned info0[2 * NW];              // its sequence's first tile on the line
     __shared__ int flag[2];
-    static_assert(kKvHeads * D / 4 <= NT, "a group's share is read before it is written over");
     const int w = wave_id(), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
     const int G = a.c.hq / a.c.hkv, HT = (G + kKvHeads - 1) / kKvHeads, HH = a.c.hkv * HT;
     const int psh = a.c.ps_shift, pmask = (1 << psh) - 1;
@@ -524,7 +517,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
                 f[z] = f[z] == -INFINITY ? 0.f : exp2_(f[z] - M);
                 S += f[z] * s[z];                                   // (a NaN stays one)
             }
-            if (threadIdx.x < DT * 64) {
+            for (int u = threadIdx.x; u < DT * 64; u += NT) {
                 f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int z0 = 0; z0 < NW; z0 += 4) {
@@ -532,12 +525,12 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
                     f32x4 y[4];
 #pragma unroll
                     for (int z = 0; z < 4; ++z)
-                        y[z] = reinterpret_cast<const f32x4*>(lds)[(wave(z0 + z) * 2 + piece(z0 + z)) * BUF + threadIdx.x];
+                        y[z] = reinterpret_cast<const f32x4*>(lds)[(wave(z0 + z) * 2 + piece(z0 + z)) * BUF + u];
 #pragma unroll
                     for (int z = 0; z < 4; ++z)
                         if (f[z0 + z] != 0.f) v += f[z0 + z] * y[z];
                 }
-                const int d = (threadIdx.x >> 6) * 16 + ((threadIdx.x >> 4) & 3) * 4;
+                const int d = (u >> 6) * 16 + ((u >> 4) & 3) * 4;
                 if (whole) {
                     finish(b, hd.hq0 + head, d, v, M, S);
                 } else {
@@ -606,11 +599,14 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
             return a.part + (size_t)(2 * v + (v == v0)) * kv_part_floats(D);
         };
         // one item = 4 numbers of a head; groups of threads take every ng-th share
-        const int items = hd.n * (D / 4), ng = NT / items, g = threadIdx.x / items, item = threadIdx.x - g * items;
+        const int all = hd.n * (D / 4), items = min(all, NT), ng = NT / items, g = threadIdx.x / items;
+        for (int i0 = 0; i0 < all; i0 += NT) {
+        const int item = i0 + threadIdx.x - g * items;
         const int hq = item / (D / 4), d = item % (D / 4) * 4;
+        const bool in = g < ng && item < all;
         f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
         float ss = 0.f, top = -INFINITY;
-        if (g < ng)
+        if (in)
             for (unsigned x0 = g; x0 < n; x0 += 4 * ng) {
                 float2 ms[4], y0[4], y1[4];
 #pragma unroll
@@ -659,7 +655,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
                 if (fx != 0.f) v += fx * fv[x * items + threadIdx.x];
             }
         }
-        if (g == 0) {
+        if (in && g == 0) {
             if (level) {
                 finish(b, hd.hq0 + hq, d, v, top, ss);
             } else {                                               // the group's share takes its first one's place
@@ -668,6 +664,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
                 store_through(p + hq * D + d + 2, v[2], v[3]);
                 if (d == 0) store_through(p + kKvHeads * D + 2 * hq, top, ss);
             }
+        }
         }
     }
 }
@@ -710,19 +707,14 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) {
     }
 }
 
-#ifndef ATT_NW
-#define ATT_NW 8
-#define ATT_EU 2
-#define ATT_GRID 256
-#endif
 template <int D, bool FP8>
 hipError_t launch(const KvAttendArgs& a, bool accumulate, hipStream_t s) {
-    constexpr int NW = ATT_NW, EU = ATT_EU;
+    constexpr int NW = 4, EU = 2;                   // two workgroups per compute unit
     // no more workgroups than the table rows could have work for
     const long long G = a.c.hq / a.c.hkv, HH = a.c.hkv * ((G + kKvHeads - 1) / kKvHeads);
     const long long tiles = (((long long)a.c.width << a.c.ps_shift) + 31) / 32 * a.B * HH;
     int grid = 1;
-    while (grid < ATT_GRID && (long long)grid * NW < tiles) grid *= 2;
+    while (grid < kKvAttendGrid && (long long)grid * NW < tiles) grid *= 2;
     if (!accumulate) {
         kv_attend_kernel<D, FP8, false, NW, EU><<<grid, NW * 64, 0, s>>>(a);
         return hipGetLastError();

@@ -1,18 +1,23 @@
 // Device helpers of the key-value cache kernels (gfx950, wave64).
 #pragma once
 
+#include <algorithm>
+#include <climits>
+
 #include "bdl_device.h"
 #include "bdl_kv.h"
 
 namespace bdl {
 
-__device__ __forceinline__ float bf2f(uint32_t b) { return __uint_as_float(b << 16); }
-
-// e4m3 bits, round to nearest even, clamped to the largest number (NaN stays)
-__device__ __forceinline__ uint32_t f2e4m3(float f) {
-    const float c = f != f ? f : fminf(fmaxf(f, -448.f), 448.f);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, c, 0, false) & 0xffu;
+// two fp32 numbers as bf16, to nearest even (NaN stays)
+__device__ __forceinline__ uint32_t pk_bf16(float x, float y) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
 }
+
+// into the range of e4m3 (NaN stays)
+__device__ __forceinline__ float clamp_e4m3(float f) { return f != f ? f : fminf(fmaxf(f, -448.f), 448.f); }
 
 __device__ __forceinline__ void kv_error(const KvCache& c) {
     __hip_atomic_store(c.err, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
