@@ -52,7 +52,8 @@ struct KvAttendArgs {
     const uint16_t* q;
     uint16_t* out;
     long long q_stride, out_stride;
-    const int *lens, *starts;   // starts may be null
+    const int *lens, *starts;
+    int has_starts;             // 0: starts is there to be read, and means nothing
     float* lse;                 // may be null
     int B, n_cu;
     float* part;                // [2 kKvAttendGrid][kv_part_floats(D)]

@@ -296,7 +296,8 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         a.out = (uint16_t*)out;
         a.out_stride = out_stride;
         a.lens = lens;
-        a.starts = starts;
+        a.starts = starts ? starts : lens;
+        a.has_starts = starts != nullptr;
         a.lse = lse;
         a.B = B;
         a.n_cu = c->n_cu;

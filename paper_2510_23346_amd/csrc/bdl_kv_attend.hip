@@ -24,19 +24,23 @@ namespace bdl {
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int NW = 4, NT = NW * 64;     // waves and threads of a workgroup, of which a compute unit holds two
 
 // A sequence: entries first .. len - 1 in tiles that begin at a multiple of 16
 // (an empty one has a tile too, which writes its row)
 struct Seq {
     int len, first;
     unsigned tiles;
+    bool bad;         // the given length was none
 };
 
 __device__ __forceinline__ Seq seq_of(const KvAttendArgs& a, int b) {
     const int at = min(b, a.B - 1), cap = a.c.width << a.c.ps_shift;     // (at most 2^30)
+    const int n = a.lens[at], st = a.starts[at];
     Seq s;
-    s.len = min(max(a.lens[at], 0), cap);
-    s.first = a.starts ? max(a.starts[at], 0) : 0;
+    s.len = min(max(n, 0), cap);
+    s.bad = s.len != n;
+    s.first = a.has_starts ? max(st, 0) : 0;
     if (s.first >= s.len) s.len = s.first = 0;
     s.tiles = b < a.B ? max(1u, (unsigned)(s.len - (s.first & ~15) + 31) >> 5) : 0u;
     return s;
@@ -117,33 +121,34 @@ struct Tile {
 // first, so that no workgroup reads more than a few dozen
 constexpr unsigned kDirect = 24, kGroup = 16;
 
-template <int D, bool FP8, bool ACC, int NW, int EU>
-__global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendArgs a) {
+template <int D, bool FP8, bool ACC, bool WIDE>
+__global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArgs a) {
     constexpr int SZ = FP8 ? 1 : 2, ROW = D * SZ;
     constexpr int NL = 16 * ROW / 1024;             // 16-byte loads of a block
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int BUF = 32 * D / 8;                 // 16-byte pieces of a tile in LDS, or of a wave's sums
-    constexpr int NT = NW * 64;
-    static_assert(NW <= 8, "pieces of a workgroup are in the first 16 lanes");
-    // per wave: the tile being worked on (in the end the sums of its last
-    // sequence), and the sums of a sequence that came from the wave before
+    // per wave: the sums of a sequence that came from the wave before (piece
+    // 2 w), and the tile being worked on, in the end the sums of its last
+    // sequence (piece 2 w + 1)
     __shared__ u32x4 lds[NW * 2 * BUF];
-    __shared__ float stat[NW][2][2][kKvHeads];      // [wave][piece][maximum, sum][head]
-    __shared__ int4 info[2 * NW];                   // [wave][piece 1, 0]: sequence (-1: none), head, first and last tile it has, tiles
+    __shared__ float2 stat[2 * NW][kKvHeads];       // [piece][head]: maximum and sum
+    __shared__ int4 info[2 * NW];                   // [piece]: sequence (-1: none), head, whether it has the last tile, tiles
     __shared__ unsigned info0[2 * NW];              // its sequence's first tile on the line
     __shared__ int flag[2];
     const int w = wave_id(), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
-    const int G = a.c.hq / a.c.hkv, HT = (G + kKvHeads - 1) / kKvHeads, HH = a.c.hkv * HT;
+    const int G = a.c.hq / a.c.hkv, HT = WIDE ? (G + kKvHeads - 1) / kKvHeads : 1, HH = a.c.hkv * HT;
     const int psh = a.c.ps_shift, pmask = (1 << psh) - 1;
 
     // the line, this workgroup's stretch and the wave's part of it
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b < a.B; b += NT) (void)kv_len(a.c, a.lens, b);     // (flags lengths that are none)
+    bool bad = false;
     Seq four[4];                                    // sequences c0 + 64 i + lane
     unsigned incl[4], sum4[4], total = 0;
     auto look_four = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) four[i] = seq_of(a, c0 + 64 * i + l);
+        for (int i = 0; i < 4; ++i) {
+            four[i] = seq_of(a, c0 + 64 * i + l);
+            bad |= four[i].bad;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             incl[i] = (unsigned)wave_incl_scan((int)four[i].tiles);
@@ -152,6 +157,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     };
     if (a.B <= 64) {
         four[0] = seq_of(a, l);
+        bad = four[0].bad;
         incl[0] = (unsigned)wave_incl_scan((int)four[0].tiles);
         total = sum4[0] = (unsigned)wave_total((int)incl[0]);
 #pragma unroll
@@ -166,6 +172,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
             total += sum4[0] + sum4[1] + sum4[2] + sum4[3];
         }
     }
+    if (blockIdx.x == 0 && bad) kv_error(a.c);
     Line line;
     line.total = total * HH;
     // as many stretches as give every wave a tile, at most one per workgroup
@@ -256,7 +263,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     // are at most 2^30 of them)
     const unsigned page16 = (unsigned)a.c.hkv << psh, row16 = ROW / 16;
     auto locate = [&](Tile& x) __attribute__((always_inline)) {
-        const int kvh = HT == 1 ? x.h : x.h / HT;
+        const int kvh = WIDE ? x.h / HT : x.h;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             if (x.n[j] > 0 && (unsigned)x.page[j] >= (unsigned)a.c.n_pages) {
@@ -285,7 +292,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
         int hq0, n;
     };
     auto heads_of = [&](int h) __attribute__((always_inline)) {
-        if (HT == 1) return Heads{h * G, G};
+        if (!WIDE) return Heads{h * G, G};
         const int kvh = h / HT, ht = h - kvh * HT;
         return Heads{kvh * G + ht * kKvHeads, min(kKvHeads, G - ht * kKvHeads)};
     };
@@ -301,7 +308,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
             for (int i = 0; i < 4; ++i) q[ks][i] ^= a.q_sign;
         }
     };
-    u32x4* const buf = lds + w * 2 * BUF;
+    u32x4* const buf = lds + (2 * w + 1) * BUF;
     // rows as they were loaded (a block is contiguous) into LDS, bf16
     auto put = [&](const u32x4 (&x)[2][NL], bool value) __attribute__((always_inline)) {
         constexpr int LPR = ROW / 16;               // lanes of a row
@@ -324,7 +331,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     };
     // 4 numbers of a row's output, from number d of query head hq on
     auto finish = [&](int b, int hq, int d, f32x4 v, float top, float sum_) __attribute__((always_inline)) {
-        const float g = a.v_scale / sum_;
+        const float g = a.v_scale * __builtin_amdgcn_rcpf(sum_);
         const bool none = sum_ == 0.f;
         *reinterpret_cast<uint2*>(a.out + b * a.out_stride + hq * D + d) =
             uint2{none ? 0u : pk_bf16(v[0] * g, v[1] * g), none ? 0u : pk_bf16(v[2] * g, v[3] * g)};
@@ -344,16 +351,13 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
     for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     // the sums as a piece of a sequence that other waves share, into LDS
     auto leave = [&](int piece, const Tile& x) __attribute__((always_inline)) {
-        f32x4* const ob = reinterpret_cast<f32x4*>(buf + piece * BUF);
+        f32x4* const ob = reinterpret_cast<f32x4*>(lds + piece * BUF);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) ob[dt * 64 + l] = o[dt];
-        if (l < kKvHeads) {
-            stat[w][piece][0][l] = m;
-            stat[w][piece][1][l] = sum;
-        }
+        if (l < kKvHeads) stat[piece][l] = float2{m, sum};
         if (l == 0) {
-            info[2 * w + 1 - piece] = int4{x.b, x.h, (piece == 0 ? 1 : 0) | (x.last ? 2 : 0), (int)x.tiles};
-            info0[2 * w + 1 - piece] = head0;
+            info[piece] = int4{x.b, x.h, x.last, (int)x.tiles};
+            info0[piece] = head0;
         }
     };
     if (l < 2) info[2 * w + l] = int4{-1, 0, 0, 0};
@@ -458,7 +462,7 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
 #pragma unroll
                         for (int dt = 0; dt < DT; ++dt) finish(cur.b, hd.hq0 + lr, dt * 16 + 4 * lg, o[dt], m, sum);
                 } else {
-                    leave(first ? 0 : 1, cur);
+                    leave(2 * w + first, cur);
                 }
                 if (i + 1 < left) {
                     load_q(nxt);
@@ -475,15 +479,14 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
         }
     }
 
-    // The pieces of the workgroup, in the line's order (lane 2 wave + 0, 1:
-    // piece 1, which came from the wave before, and piece 0).  Each sequence's
-    // are added, and those that the workgroup has alone are finished
+    // The pieces of the workgroup, in the line's order.  Each sequence's are
+    // added, and those that the workgroup has alone are finished
     __syncthreads();
     const int head = threadIdx.x & 15;
     const int4 pi = info[min(l, 2 * NW - 1)];
     const unsigned ph0 = info0[min(l, 2 * NW - 1)];
     const unsigned valid = (unsigned)__ballot(pi.x >= 0 && l < 2 * NW);
-    const unsigned lasts = (unsigned)__ballot((pi.z & 2) != 0) & valid;
+    const unsigned lasts = (unsigned)__ballot(pi.z != 0) & valid;
     unsigned starts = valid & (0xaaaau | (valid & -valid));
     int nsh = 0;
     int share_b[2], share_h[2];
@@ -497,39 +500,32 @@ __global__ __launch_bounds__(NW * 64, EU) void kv_attend_kernel(const KvAttendAr
         const bool has_first = i0 & 1, whole = has_first && (lasts & members);
         const Heads hd = heads_of(h);
         float* const part = a.part + (size_t)(2 * blockIdx.x + (has_first ? 1 : 0)) * kv_part_floats(D);
-        auto piece = [&](int z) __attribute__((always_inline)) { return (z && z < n) | !has_first; };
-        auto wave = [&](int z) __attribute__((always_inline)) { return pw + (z < n ? z : 0); };
+        // the chain's z-th piece (past the last: the first again, for nothing)
+        auto piece = [&](int z) __attribute__((always_inline)) { return z && z < n ? 2 * (pw + z) : i0; };
         if (head < hd.n) {
-            float f[NW], s[NW], M = -INFINITY, S = 0.f;
+            float2 st[NW];
+            float M = -INFINITY, S = 0.f;
+#pragma unroll
+            for (int z = 0; z < NW; ++z) st[z] = stat[piece(z)][head];
 #pragma unroll
             for (int z = 0; z < NW; ++z) {
-                f[z] = stat[wave(z)][piece(z)][0][head];
-                s[z] = stat[wave(z)][piece(z)][1][head];
+                st[z] = z < n ? st[z] : float2{-INFINITY, 0.f};
+                M = fmaxf(M, st[z].x);
             }
 #pragma unroll
             for (int z = 0; z < NW; ++z) {
-                f[z] = z < n ? f[z] : -INFINITY;
-                s[z] = z < n ? s[z] : 0.f;
-                M = fmaxf(M, f[z]);
+                st[z].x = st[z].x == -INFINITY ? 0.f : exp2_(st[z].x - M);
+                S += st[z].x * st[z].y;                             // (a NaN stays one)
             }
 #pragma unroll
-            for (int z = 0; z < NW; ++z) {
-                f[z] = f[z] == -INFINITY ? 0.f : exp2_(f[z] - M);
-                S += f[z] * s[z];                                   // (a NaN stays one)
-            }
-            for (int u = threadIdx.x; u < DT * 64; u += NT) {
-                f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int u0 = 0; u0 < DT * 64; u0 += NT) {
+                const int u = u0 + threadIdx.x;
+                f32x4 y[NW], v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int z0 = 0; z0 < NW; z0 += 4) {
-                    if (z0 >= n) break;
-                    f32x4 y[4];
+                for (int z = 0; z < NW; ++z) y[z] = reinterpret_cast<const f32x4*>(lds)[piece(z) * BUF + u];
 #pragma unroll
-                    for (int z = 0; z < 4; ++z)
-                        y[z] = reinterpret_cast<const f32x4*>(lds)[(wave(z0 + z) * 2 + piece(z0 + z)) * BUF + u];
-#pragma unroll
-                    for (int z = 0; z < 4; ++z)
-                        if (f[z0 + z] != 0.f) v += f[z0 + z] * y[z];
-                }
+                for (int z = 0; z < NW; ++z)
+                    if (st[z].x != 0.f) v += st[z].x * y[z];
                 const int d = (u >> 6) * 16 + ((u >> 4) & 3) * 4;
                 if (whole) {
                     finish(b, hd.hq0 + head, d, v, M, S);
@@ -707,22 +703,26 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) {
     }
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool WIDE>
 hipError_t launch(const KvAttendArgs& a, bool accumulate, hipStream_t s) {
-    constexpr int NW = 4, EU = 2;                   // two workgroups per compute unit
     // no more workgroups than the table rows could have work for
     const long long G = a.c.hq / a.c.hkv, HH = a.c.hkv * ((G + kKvHeads - 1) / kKvHeads);
     const long long tiles = (((long long)a.c.width << a.c.ps_shift) + 31) / 32 * a.B * HH;
     int grid = 1;
     while (grid < kKvAttendGrid && (long long)grid * NW < tiles) grid *= 2;
     if (!accumulate) {
-        kv_attend_kernel<D, FP8, false, NW, EU><<<grid, NW * 64, 0, s>>>(a);
+        kv_attend_kernel<D, FP8, false, WIDE><<<grid, NT, 0, s>>>(a);
         return hipGetLastError();
     }
-    kv_attend_kernel<D, FP8, true, NW, EU><<<grid, NW * 64, 0, s>>>(a);
+    kv_attend_kernel<D, FP8, true, WIDE><<<grid, NT, 0, s>>>(a);
     const long long blocks = (((long long)a.c.width << a.c.ps_shift) + 255) / 256 * a.B * a.c.hkv;
     kv_weigh_kernel<<<(int)std::min(blocks, 1024LL), 256, 0, s>>>(a);
     return hipGetLastError();
+}
+
+template <int D, bool FP8>
+hipError_t launch(const KvAttendArgs& a, bool accumulate, hipStream_t s) {
+    return a.c.hq / a.c.hkv > kKvHeads ? launch<D, FP8, true>(a, accumulate, s) : launch<D, FP8, false>(a, accumulate, s);
 }
 
 }  // namespace

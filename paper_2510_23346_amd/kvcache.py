@@ -12,7 +12,7 @@ import ctypes as _c
 import math
 from typing import Tuple
 
-from . import KV_BF16, KV_FP8_E4M3, KVDesc, _check, _stream_handle, lib
+from . import KV_BF16, KV_FP8_E4M3, KVDesc, _check, lib
 
 __all__ = ["KVCache", "kv_bytes"]
 
@@ -74,6 +74,8 @@ class KVCache:
                                       self.weight.data_ptr() if weights else None, self.pos.data_ptr() if weights else None,
                                       self.device, _c.byref(h)))
         self._h = h
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda device: torch.cuda.current_stream(device).cuda_stream)
         self._scale = 1.0 / math.sqrt(self.head_dim)
         self._qw = self.n_q_heads * self.head_dim
         self._qkvw = self._qw + 2 * self.n_kv_heads * self.head_dim
@@ -99,6 +101,15 @@ class KVCache:
         self.close()
 
     # -- arguments --------------------------------------------------------
+    # (these checks run in front of every call, and a call's kernel may take 5
+    # us: they touch each property of a tensor once)
+    def _stream(self, stream):
+        if stream is None:
+            # the handle alone: torch.cuda.current_stream() builds an object
+            # around it, which takes 2.7 us
+            return self._raw_stream(self.device)
+        return stream if isinstance(stream, int) else int(stream.cuda_stream)
+
     def _rows(self, name, t, n, width):
         """Row stride of a bf16 tensor of n rows: [n, width], or [n, heads, head_dim]."""
         sh, st = t.shape, t.stride()
@@ -145,7 +156,7 @@ class KVCache:
                             self._ints("seqs", seqs, T), self._ints("index", index, T),
                             self._ints("positions", positions, T), T, tp, ts, tw, n,
                             None if lens is None else self._ints("lens", lens, n), q_out.data_ptr(), os_,
-                            _stream_handle(stream)))
+                            self._stream(stream)))
 
     def attend(self, q, table, lens, out, starts=None, scale=None, lse=None, accumulate: bool = False, stream=None):
         """Attention of row b of ``q [B, n_q_heads head_dim]`` over entries
@@ -166,7 +177,7 @@ class KVCache:
         _check(self._attend(self._h, q.data_ptr(), qs, B, tp, ts, tw, self._ints("lens", lens, B),
                             None if starts is None else self._ints("starts", starts, B),
                             self._scale if scale is None else scale, int(accumulate), out.data_ptr(), os_,
-                            None if lse is None else lse.data_ptr(), _stream_handle(stream)))
+                            None if lse is None else lse.data_ptr(), self._stream(stream)))
 
     def evict(self, table, lens, budget: int, recent: int = 0, stream=None):
         """Cut the sequences of ``table`` to ``budget`` entries per kv head:
@@ -175,9 +186,9 @@ class KVCache:
         tp, ts, tw = self._table(table)
         B = table.shape[0]
         _check(self._evict(self._h, B, tp, ts, tw, self._ints("lens", lens, B), int(budget), int(recent),
-                           _stream_handle(stream)))
+                           self._stream(stream)))
 
     def device_error(self, stream=None) -> int:
         f = _c.c_int32(0)
-        _check(lib().bdlora_kv_get_device_error(self._h, _stream_handle(stream), _c.byref(f)))
+        _check(lib().bdlora_kv_get_device_error(self._h, self._stream(stream), _c.byref(f)))
         return f.value
