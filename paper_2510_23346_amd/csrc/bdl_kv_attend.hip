@@ -65,16 +65,26 @@ __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlan
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ __forceinline__ void store_through(float* p, float x, float y) {
-    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p),
-                       (unsigned long long)__float_as_uint(x) | ((unsigned long long)__float_as_uint(y) << 32),
-                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Shares go past the caches that the compute units do not have in common
+// (device scope), 8 or 16 bytes at byte `at` of the workspace
+constexpr int kDeviceScope = 16;
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void store_through(__amdgpu_buffer_rsrc_t r, unsigned at, f32x4 v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, (int)at, 0, kDeviceScope);
 }
 
-__device__ __forceinline__ float2 load_through(const float* p) {
-    const unsigned long long v =
-        __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return float2{__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32))};
+__device__ __forceinline__ void store_through(__amdgpu_buffer_rsrc_t r, unsigned at, float2 v) {
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v.x), __float_as_uint(v.y)}, r, (int)at, 0, kDeviceScope);
+}
+
+__device__ __forceinline__ f32x4 load_through4(__amdgpu_buffer_rsrc_t r, unsigned at) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, kDeviceScope));
+}
+
+__device__ __forceinline__ float2 load_through2(__amdgpu_buffer_rsrc_t r, unsigned at) {
+    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, 0, kDeviceScope));
+    return float2{__uint_as_float(v[0]), __uint_as_float(v[1])};
 }
 
 // Where a 16-byte chunk c of row r of a tile lies in LDS: rows of D bf16
@@ -119,7 +129,8 @@ struct Tile {
 // A share's way through the workspace: up to kDirect shares of a sequence are
 // added by its last workgroup; more are added in groups of kGroup workgroups
 // first, so that no workgroup reads more than a few dozen
-constexpr unsigned kDirect = 24, kGroup = 16;
+constexpr unsigned kDirect = 32, kGroup = 16;
+constexpr int kBatch = 4;               // shares whose loads are in flight at once
 
 template <int D, bool FP8, bool ACC, bool WIDE>
 __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArgs a) {
@@ -482,186 +493,207 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
     // The pieces of the workgroup, in the line's order.  Each sequence's are
     // added, and those that the workgroup has alone are finished
     __syncthreads();
-    const int head = threadIdx.x & 15;
     const int4 pi = info[min(l, 2 * NW - 1)];
     const unsigned ph0 = info0[min(l, 2 * NW - 1)];
     const unsigned valid = (unsigned)__ballot(pi.x >= 0 && l < 2 * NW);
     const unsigned lasts = (unsigned)__ballot(pi.z != 0) & valid;
-    unsigned starts = valid & (0xaaaau | (valid & -valid));
-    int nsh = 0;
-    int share_b[2], share_h[2];
-    unsigned share_0[2], share_tiles[2];
-    while (starts) {
-        const int i0 = __ffs((int)starts) - 1;
-        starts &= starts - 1;
-        const unsigned members = valid & ~((1u << i0) - 1) & (starts ? (starts & -starts) - 1 : 0xffffu);
-        const int n = __popc(members), pw = i0 >> 1;                // waves pw .. pw + n - 1, all but the first with piece 1
-        const int b = __builtin_amdgcn_readlane(pi.x, i0), h = __builtin_amdgcn_readlane(pi.y, i0);
-        const bool has_first = i0 & 1, whole = has_first && (lasts & members);
-        const Heads hd = heads_of(h);
-        float* const part = a.part + (size_t)(2 * blockIdx.x + (has_first ? 1 : 0)) * kv_part_floats(D);
-        // the chain's z-th piece (past the last: the first again, for nothing)
-        auto piece = [&](int z) __attribute__((always_inline)) { return z && z < n ? 2 * (pw + z) : i0; };
-        if (head < hd.n) {
-            float2 st[NW];
-            float M = -INFINITY, S = 0.f;
+    constexpr unsigned kPart = kv_part_floats(D) * 4;
+    const __amdgpu_buffer_rsrc_t pr = buf_rsrc(a.part, 2 * kKvAttendGrid * kPart);
+    // a chain of pieces: one sequence's, from its start on; only the first and
+    // the last chain can be shared with other workgroups
+    const unsigned starts = valid & (0xaaaau | (valid & -valid));
+    if (!starts) return;                            // (every sequence was within one wave)
+    const int chains = __popc(starts);
+    struct Chain {
+        int i0, n;        // first piece and how many
+        bool whole;
+    };
+    auto chain_at = [&](unsigned from) __attribute__((always_inline)) {       // from: starts, those before cut off
+        const int i0 = __ffs((int)from) - 1;
+        const unsigned rest = from & (from - 1);
+        const unsigned members = valid & ~((1u << i0) - 1) & (rest ? (rest & -rest) - 1 : 0xffffu);
+        return Chain{i0, (int)__popc(members), (i0 & 1) && (lasts & members)};
+    };
+    {
+        // one or two chains take all or half of the waves, more a wave each
+        const int per = chains == 1 ? NW : chains == 2 ? NW / 2 : 1, step = NW / per;
+        unsigned from = starts;
+        for (int c = 0; c < w / per; ++c) from &= from - 1;
+        for (int c = w / per; c < chains; c += step) {
+            const Chain ch_ = chain_at(from);
+            for (int x = 0; x < step; ++x) from &= from - 1;
+            const int i0 = ch_.i0, n = ch_.n, pw = i0 >> 1;         // waves pw .. pw + n - 1
+            const int b = __builtin_amdgcn_readlane(pi.x, i0);
+            const Heads hd = heads_of(__builtin_amdgcn_readlane(pi.y, i0));
+            const unsigned part = (2 * blockIdx.x + (i0 & 1)) * kPart;
+            // the chain's z-th piece (past the last: the first again, for nothing)
+            auto piece = [&](int z) __attribute__((always_inline)) { return z && z < n ? 2 * (pw + z) : i0; };
+            if (lr < hd.n) {
+                float2 st[NW];
+                float M = -INFINITY, S = 0.f;
 #pragma unroll
-            for (int z = 0; z < NW; ++z) st[z] = stat[piece(z)][head];
+                for (int z = 0; z < NW; ++z) st[z] = stat[piece(z)][lr];
 #pragma unroll
-            for (int z = 0; z < NW; ++z) {
-                st[z] = z < n ? st[z] : float2{-INFINITY, 0.f};
-                M = fmaxf(M, st[z].x);
-            }
+                for (int z = 0; z < NW; ++z) {
+                    st[z] = z < n ? st[z] : float2{-INFINITY, 0.f};
+                    M = fmaxf(M, st[z].x);
+                }
 #pragma unroll
-            for (int z = 0; z < NW; ++z) {
-                st[z].x = st[z].x == -INFINITY ? 0.f : exp2_(st[z].x - M);
-                S += st[z].x * st[z].y;                             // (a NaN stays one)
-            }
+                for (int z = 0; z < NW; ++z) {
+                    st[z].x = st[z].x == -INFINITY ? 0.f : exp2_(st[z].x - M);
+                    S += st[z].x * st[z].y;                         // (a NaN stays one)
+                }
+#pragma unroll 2
+                for (int dt = w % per; dt < DT; dt += per) {
+                    f32x4 y[NW], v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int u0 = 0; u0 < DT * 64; u0 += NT) {
-                const int u = u0 + threadIdx.x;
-                f32x4 y[NW], v = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int z = 0; z < NW; ++z) y[z] = reinterpret_cast<const f32x4*>(lds)[piece(z) * BUF + dt * 64 + l];
 #pragma unroll
-                for (int z = 0; z < NW; ++z) y[z] = reinterpret_cast<const f32x4*>(lds)[piece(z) * BUF + u];
-#pragma unroll
-                for (int z = 0; z < NW; ++z)
-                    if (st[z].x != 0.f) v += st[z].x * y[z];
-                const int d = (u >> 6) * 16 + ((u >> 4) & 3) * 4;
-                if (whole) {
-                    finish(b, hd.hq0 + head, d, v, M, S);
-                } else {
-                    store_through(part + head * D + d, v[0], v[1]);
-                    store_through(part + head * D + d + 2, v[2], v[3]);
-                    if (d == 0) store_through(part + kKvHeads * D + 2 * head, M, S);
+                    for (int z = 0; z < NW; ++z)
+                        if (st[z].x != 0.f) v += st[z].x * y[z];
+                    const int d = dt * 16 + 4 * lg;
+                    if (ch_.whole) {
+                        finish(b, hd.hq0 + lr, d, v, M, S);
+                    } else {
+                        store_through(pr, part + (lr * D + d) * 4, v);
+                        if (d == 0) store_through(pr, part + (kKvHeads * D + 2 * lr) * 4, float2{M, S});
+                    }
                 }
             }
-        }
-        if (!whole) {                                               // (at most two: the stretch's first and last sequence)
-            const unsigned h0 = (unsigned)__builtin_amdgcn_readlane((int)ph0, i0), tl = (unsigned)__builtin_amdgcn_readlane(pi.w, i0);
-            if (nsh == 0) {
-                share_b[0] = b;
-                share_h[0] = h;
-                share_0[0] = h0;
-                share_tiles[0] = tl;
-            } else {
-                share_b[1] = b;
-                share_h[1] = h;
-                share_0[1] = h0;
-                share_tiles[1] = tl;
-            }
-            ++nsh;
         }
     }
 
     // Shares: counted; the workgroup that completes a sequence, or a group of
     // its workgroups, adds them in the line's order
+    const Chain c0 = chain_at(starts), c1 = chain_at(1u << (31 - __builtin_clz(starts)));
+    const bool two = chains > 1 && !c0.whole && !c1.whole;
+    const int nsh = two ? 2 : c0.whole && (chains == 1 || c1.whole) ? 0 : 1;
     if (nsh == 0) return;
-    unsigned w0[2], w1[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        if (k < nsh) {
-            w0[k] = line.owner(share_0[k]);
-            w1[k] = line.owner(share_0[k] + share_tiles[k] - 1);
-        }
+    struct Share {
+        int b, h;
+        unsigned v0, v1;      // the sequence's first and last workgroup
+        // members m0 + stride x (the first workgroup in place of what lies before
+        // it), x = 0 .. n - 1, and their counter; level 0: a group's, 1: all
+        unsigned m0, stride, n;
+        unsigned* count;
+        bool direct;
+    };
     const unsigned grp = blockIdx.x / kGroup;
+    auto at_level = [&](Share& s, int level) __attribute__((always_inline)) {
+        s.m0 = s.direct ? s.v0 : level ? s.v0 / kGroup * kGroup : max(s.v0, grp * kGroup);
+        s.stride = s.direct || !level ? 1u : kGroup;
+        s.n = s.direct ? s.v1 - s.v0 + 1 : level ? s.v1 / kGroup - s.v0 / kGroup + 1 : min(s.v1 + 1, (grp + 1) * kGroup) - s.m0;
+        s.count = level ? a.count + (size_t)s.b * HH + s.h : a.group_count + 2 * s.m0 + (s.m0 == s.v0);
+    };
+    auto share_of = [&](const Chain& c) __attribute__((always_inline)) {
+        Share s;
+        s.b = __builtin_amdgcn_readlane(pi.x, c.i0);
+        s.h = __builtin_amdgcn_readlane(pi.y, c.i0);
+        const unsigned h0 = (unsigned)__builtin_amdgcn_readlane((int)ph0, c.i0);
+        s.v0 = line.owner(h0);
+        s.v1 = line.owner(h0 + (unsigned)__builtin_amdgcn_readlane(pi.w, c.i0) - 1);
+        s.direct = s.v1 - s.v0 < kDirect;
+        at_level(s, s.direct);
+        return s;
+    };
+    Share sh0 = share_of(two || !c0.whole ? c0 : c1), sh1 = sh0;
+    if (two) sh1 = share_of(c1);
+    // what this wave left has reached memory; then one atomic operation for each
+    auto arrive = [&](unsigned* c, unsigned n) __attribute__((always_inline)) {
+        const bool is_last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+        if (is_last) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return is_last;
+    };
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if ((int)threadIdx.x < nsh) flag[threadIdx.x] = arrive(threadIdx.x ? sh1.count : sh0.count, threadIdx.x ? sh1.n : sh0.n);
+    __syncthreads();
+    const bool last0 = uni(flag[0]), last1 = nsh == 2 && uni(flag[1]);
 #pragma unroll 1
-    for (int round = 0; round < 2 * nsh; ++round) {
-        const int k = round >> 1, level = round & 1;
-        const unsigned v0 = k ? w0[1] : w0[0], v1 = k ? w1[1] : w1[0];
-        const int b = k ? share_b[1] : share_b[0], h = k ? share_h[1] : share_h[0];
-        const Heads hd = heads_of(h);
-        const bool direct = v1 - v0 < kDirect;
-        if (direct && !level) continue;
-        // members m0 + stride x (the sequence's first workgroup in place of what
-        // lies before it), x = 0 .. n - 1
-        const unsigned m0 = direct ? v0 : level ? v0 / kGroup * kGroup : max(v0, grp * kGroup);
-        const unsigned stride = direct || !level ? 1u : kGroup;
-        const unsigned n = direct ? v1 - v0 + 1 : level ? v1 / kGroup - v0 / kGroup + 1 : min(v1 + 1, (grp + 1) * kGroup) - m0;
-        unsigned* const c = level ? a.count + (size_t)b * HH + h : a.group_count + 2 * m0 + (m0 == v0);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // what this wave left has reached memory
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const unsigned old = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            flag[0] = old == n - 1;
-            if (flag[0]) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (!uni(flag[0])) {
-            if (!level) ++round;                                   // (the sequence is another's)
-            continue;
-        }
-        auto share = [&](unsigned x) __attribute__((always_inline)) {
-            const unsigned v = max(v0, m0 + stride * x);
-            return a.part + (size_t)(2 * v + (v == v0)) * kv_part_floats(D);
-        };
-        // one item = 4 numbers of a head; groups of threads take every ng-th share
-        const int all = hd.n * (D / 4), items = min(all, NT), ng = NT / items, g = threadIdx.x / items;
-        for (int i0 = 0; i0 < all; i0 += NT) {
-        const int item = i0 + threadIdx.x - g * items;
-        const int hq = item / (D / 4), d = item % (D / 4) * 4;
-        const bool in = g < ng && item < all;
-        f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-        float ss = 0.f, top = -INFINITY;
-        if (in)
-            for (unsigned x0 = g; x0 < n; x0 += 4 * ng) {
-                float2 ms[4], y0[4], y1[4];
+    for (int k = 0; k < 2; ++k) {
+        if (!(k ? last1 : last0)) continue;
+        Share s = k ? sh1 : sh0;
+        const Heads hd = heads_of(s.h);
+#pragma unroll 1
+        for (int level = s.direct;; ++level) {
+            auto share = [&](unsigned x) __attribute__((always_inline)) {
+                const unsigned v = max(s.v0, s.m0 + s.stride * x);
+                return (2 * v + (v == s.v0)) * kPart;
+            };
+            // one item = 4 numbers of a head; groups of threads take every ng-th share
+            const int all = hd.n * (D / 4), items = min(all, NT), ng = NT / items, g = threadIdx.x / items;
+            for (int i0 = 0; i0 < all; i0 += NT) {
+                const int item = i0 + threadIdx.x - g * items;
+                const int hq = item / (D / 4), d = item % (D / 4) * 4;
+                const bool in = g < ng && item < all;
+                f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+                float ss = 0.f, top = -INFINITY;
+                if (in)
+                    for (int x0 = g; x0 < (int)s.n; x0 += kBatch * ng) {
+                        float2 ms[kBatch];
+                        f32x4 y[kBatch];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const float* p = share(min(x0 + x * ng, n - 1));
-                    ms[x] = load_through(p + kKvHeads * D + 2 * hq);
-                    y0[x] = load_through(p + hq * D + d);
-                    y1[x] = load_through(p + hq * D + d + 2);
-                }
-                float tn = top;
+                        for (int x = 0; x < kBatch; ++x) {
+                            const unsigned p = x0 + x * ng < (int)s.n ? share((unsigned)(x0 + x * ng)) : kOob;
+                            ms[x] = load_through2(pr, p + (kKvHeads * D + 2 * hq) * 4);
+                            y[x] = load_through4(pr, p + (hq * D + d) * 4);
+                        }
+                        float tn = top;
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (x0 + x * ng < n) tn = fmaxf(tn, ms[x].x);
-                const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
-                top = tn;
-                ss *= fo;
-                v *= fo;
+                        for (int x = 0; x < kBatch; ++x) {
+                            if (x0 + x * ng >= (int)s.n) ms[x] = float2{-INFINITY, 0.f};
+                            tn = fmaxf(tn, ms[x].x);
+                        }
+                        const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
+                        top = tn;
+                        ss *= fo;
+                        v *= fo;
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    if (x0 + x * ng < n) {
-                        const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
-                        ss += fx * ms[x].y;
-                        if (fx != 0.f) v += fx * f32x4{y0[x].x, y0[x].y, y1[x].x, y1[x].y};
+                        for (int x = 0; x < kBatch; ++x) {
+                            const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
+                            ss += fx * ms[x].y;
+                            if (fx != 0.f) v += fx * y[x];
+                        }
                     }
+                f32x4* const fv = reinterpret_cast<f32x4*>(lds);
+                float2* const fs = reinterpret_cast<float2*>(lds + NT);
+                if (ng > 1) {
+                    fv[threadIdx.x] = v;
+                    fs[threadIdx.x] = float2{top, ss};
+                }
+                __syncthreads();                    // (also: a group's shares are read before one is written over)
+                if (ng > 1 && g == 0) {
+                    float tn = top;
+                    for (int x = 1; x < ng; ++x) tn = fmaxf(tn, fs[x * items + threadIdx.x].x);
+                    const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
+                    top = tn;
+                    ss *= fo;
+                    v *= fo;
+                    for (int x = 1; x < ng; ++x) {
+                        const float2 y = fs[x * items + threadIdx.x];
+                        const float fx = y.x == -INFINITY ? 0.f : exp2_(y.x - top);
+                        ss += fx * y.y;
+                        if (fx != 0.f) v += fx * fv[x * items + threadIdx.x];
+                    }
+                }
+                if (in && g == 0) {
+                    if (level) {
+                        finish(s.b, hd.hq0 + hq, d, v, top, ss);
+                    } else {                        // the group's share takes its first one's place
+                        store_through(pr, share(0) + (hq * D + d) * 4, v);
+                        if (d == 0) store_through(pr, share(0) + (kKvHeads * D + 2 * hq) * 4, float2{top, ss});
+                    }
+                }
             }
-        if (ng > 1) {
-            f32x4* const fv = reinterpret_cast<f32x4*>(lds);
-            float2* const fs = reinterpret_cast<float2*>(lds + NT);
-            fv[threadIdx.x] = v;
-            fs[threadIdx.x] = float2{top, ss};
+            if (level) break;
+            at_level(s, 1);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (threadIdx.x == 0) flag[0] = arrive(s.count, s.n);
+            __syncthreads();
+            if (!uni(flag[0])) break;
         }
         __syncthreads();
-        if (ng > 1 && g == 0) {
-            const f32x4* const fv = reinterpret_cast<const f32x4*>(lds);
-            const float2* const fs = reinterpret_cast<const float2*>(lds + NT);
-            float tn = top;
-            for (int x = 1; x < ng; ++x) tn = fmaxf(tn, fs[x * items + threadIdx.x].x);
-            const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
-            top = tn;
-            ss *= fo;
-            v *= fo;
-            for (int x = 1; x < ng; ++x) {
-                const float2 y = fs[x * items + threadIdx.x];
-                const float fx = y.x == -INFINITY ? 0.f : exp2_(y.x - top);
-                ss += fx * y.y;
-                if (fx != 0.f) v += fx * fv[x * items + threadIdx.x];
-            }
-        }
-        if (in && g == 0) {
-            if (level) {
-                finish(b, hd.hq0 + hq, d, v, top, ss);
-            } else {                                               // the group's share takes its first one's place
-                float* const p = share(0);
-                store_through(p + hq * D + d, v[0], v[1]);
-                store_through(p + hq * D + d + 2, v[2], v[3]);
-                if (d == 0) store_through(p + kKvHeads * D + 2 * hq, top, ss);
-            }
-        }
-        }
     }
 }
 
