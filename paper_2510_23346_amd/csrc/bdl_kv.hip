@@ -145,10 +145,11 @@ hipError_t append(const KvAppendArgs& a, hipStream_t s) {
 // Selection: the rank key of the last entry that stays, found in three passes
 // over the keys (11, 11 and 10 bits; histograms in LDS), then places and
 // sources by prefix sums.  A thread owns consecutive entries.  Their keys are
-// kept in registers (4096 entries of a sequence) or LDS (28672), and read
+// kept in registers (8192 entries of a sequence) or LDS (28672), and read
 // again in each pass above that.
 constexpr int kET = 1024, kEW = kET / 64;
-constexpr int kRegEntries = 4 * kET, kLdsEntries = 28 * kET;
+constexpr int kRegGroups = 2;           // groups of four entries a thread keeps in registers
+constexpr int kRegEntries = 4 * kRegGroups * kET, kLdsEntries = 28 * kET;
 constexpr int kListCap = 4096;          // moves whose lists fit LDS; more go through a.scratch
 
 // An entry's rank key: the protected ones above all, then the weights in
@@ -165,7 +166,7 @@ struct EvictLds {
     unsigned hist[2048];
     int freed[kListCap], moved[kListCap];
     int wave[2][kEW];
-    unsigned digit, need;
+    unsigned digit, need, same;
     int last;
 };
 
@@ -189,8 +190,9 @@ enum Keep { kRegs, kLds, kReread };
 
 template <Keep KEEP>
 __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int n, EvictLds& L, uint4* keys) {
+    constexpr int R = KEEP == kRegs ? kRegGroups : 1;
     const int tid = threadIdx.x, M = a.budget, groups = (n + 3) / 4;
-    const int per = KEEP == kRegs ? 1 : (groups + kET - 1) / kET, g0 = tid * per;
+    const int per = (groups + kET - 1) / kET, g0 = tid * per;
     auto get = [&](int g, float4& ww, int4& pp) __attribute__((always_inline)) {
         ww = float4{NAN, NAN, NAN, NAN};
         pp = int4{INT_MIN, INT_MIN, INT_MIN, INT_MIN};
@@ -201,19 +203,29 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
         pp = *reinterpret_cast<const int4*>(a.c.pos + e);
     };
     // the largest position
-    float4 w;
-    int4 p;
+    float4 w[R];
+    int4 p[R];
     int last = INT_MIN;
+    auto top = [&](int g, const int4& pp) __attribute__((always_inline)) {
+        const int i = 4 * g;
+        if (i < n) last = max(last, pp.x);
+        if (i + 1 < n) last = max(last, pp.y);
+        if (i + 2 < n) last = max(last, pp.z);
+        if (i + 3 < n) last = max(last, pp.w);
+    };
     for (int i = tid; i < 2048; i += kET) L.hist[i] = 0;
     if (tid == 0) L.last = INT_MIN;
+    if constexpr (KEEP == kRegs) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) get(k < per ? g0 + k : groups, w[k], p[k]);
+#pragma unroll
+        for (int k = 0; k < R; ++k) top(k < per ? g0 + k : groups, p[k]);
+    } else {
 #pragma unroll 2
-    for (int k = 0; k < per; ++k) {
-        get(g0 + k, w, p);
-        const int i = 4 * (g0 + k);
-        if (i < n) last = max(last, p.x);
-        if (i + 1 < n) last = max(last, p.y);
-        if (i + 2 < n) last = max(last, p.z);
-        if (i + 3 < n) last = max(last, p.w);
+        for (int k = 0; k < per; ++k) {
+            get(g0 + k, w[0], p[0]);
+            top(g0 + k, p[0]);
+        }
     }
 #pragma unroll
     for (int x = 32; x; x >>= 1) last = max(last, __shfl_xor(last, x));
@@ -224,28 +236,42 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     auto key4 = [&](const float4& ww, const int4& pp) __attribute__((always_inline)) {
         return uint4{kv_key(ww.x, pp.x > floor_), kv_key(ww.y, pp.y > floor_), kv_key(ww.z, pp.z > floor_), kv_key(ww.w, pp.w > floor_)};
     };
-    uint4 key = key4(w, p);
+    uint4 key[R];
+    if constexpr (KEEP == kRegs) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) key[k] = key4(w[k], p[k]);
+    }
     if constexpr (KEEP == kLds) {
 #pragma unroll 2
         for (int k = 0; k < per; ++k) {
-            get(g0 + k, w, p);
-            keys[k * kET + tid] = key4(w, p);
+            get(g0 + k, w[0], p[0]);
+            keys[k * kET + tid] = key4(w[0], p[0]);
         }
     }
     // f(entry, key) for the thread's entries in order
     auto each = [&](auto f) __attribute__((always_inline)) {
+        auto four = [&](int g, const uint4& k) __attribute__((always_inline)) {
+            const int i = 4 * g;
+            if (i < n) f(i, k.x);
+            if (i + 1 < n) f(i + 1, k.y);
+            if (i + 2 < n) f(i + 2, k.z);
+            if (i + 3 < n) f(i + 3, k.w);
+        };
+        if constexpr (KEEP == kRegs) {
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (k < per) four(g0 + k, key[k]);
+        } else {
 #pragma unroll 1
-        for (int k = 0; k < per; ++k) {
-            if constexpr (KEEP == kLds) key = keys[k * kET + tid];
-            if constexpr (KEEP == kReread) {
-                get(g0 + k, w, p);
-                key = key4(w, p);
+            for (int k = 0; k < per; ++k) {
+                if constexpr (KEEP == kLds) {
+                    key[0] = keys[k * kET + tid];
+                } else {
+                    get(g0 + k, w[0], p[0]);
+                    key[0] = key4(w[0], p[0]);
+                }
+                four(g0 + k, key[0]);
             }
-            const int i = 4 * (g0 + k);
-            if (i < n) f(i, key.x);
-            if (i + 1 < n) f(i + 1, key.y);
-            if (i + 2 < n) f(i + 2, key.z);
-            if (i + 3 < n) f(i + 3, key.w);
         }
     };
     // the M-th largest key, 11, 11 and 10 bits at a time
@@ -274,9 +300,11 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
         if (before < need && need <= before + c0) {
             L.digit = 2047 - 2 * tid;
             L.need = need - before;
+            L.same = c0;
         } else if (before + c0 < need && need <= before + c0 + c1) {
             L.digit = 2046 - 2 * tid;
             L.need = need - before - c0;
+            L.same = c1;
         }
         L.hist[2047 - 2 * tid] = 0;
         L.hist[2046 - 2 * tid] = 0;
@@ -284,24 +312,34 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
         known = pass == 2 ? known << 10 | L.digit : known << 11 | L.digit;
         need = L.need;
     }
-    // entries with that key: the first `need` of them stay
-    int eq = 0, total;
-    each([&](int, unsigned k) __attribute__((always_inline)) { eq += k == known; });
-    const int eq0 = block_scan(eq, &total, L.wave[0]);
-    int fr = 0, mv = 0;
-    eq = eq0;
+    // of the entries with that key the first `need` stay (where that is not
+    // all of them, a thread has to know how many come before its own)
+    const bool all_same = need == L.same;
+    int eq0 = 0, total;
+    if (!all_same) {
+        int eq = 0;
+        each([&](int, unsigned k) __attribute__((always_inline)) { eq += k == known; });
+        eq0 = block_scan(eq, &total, L.wave[0]);
+    }
+    int eq = all_same ? INT_MIN / 2 : eq0, fr = 0, mv = 0;
     each([&](int i, unsigned k) __attribute__((always_inline)) {
         const bool kept = k > known || (k == known && eq++ < (int)need);
         fr += i < M && !kept;
         mv += i >= M && kept;
     });
+    // (both counts in one scan where they fit 16 bits)
     int moves;
-    const int fr0 = block_scan(fr, &moves, L.wave[1]);
-    __syncthreads();
-    const int mv0 = block_scan(mv, &total, L.wave[0]);
-    fr = fr0;
-    mv = mv0;
-    eq = eq0;
+    if (n < 1 << 16) {
+        const int s = block_scan(fr | mv << 16, &moves, L.wave[1]);
+        fr = s & 0xffff;
+        mv = s >> 16 & 0xffff;
+        moves &= 0xffff;
+    } else {
+        fr = block_scan(fr, &moves, L.wave[1]);
+        __syncthreads();
+        mv = block_scan(mv, &total, L.wave[0]);
+    }
+    eq = all_same ? INT_MIN / 2 : eq0;
     const bool in_lds = moves <= kListCap;
     each([&](int i, unsigned k) __attribute__((always_inline)) {
         const bool kept = k > known || (k == known && eq++ < (int)need);
