@@ -608,92 +608,99 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
     __syncthreads();
     if ((int)threadIdx.x < nsh) flag[threadIdx.x] = arrive(threadIdx.x ? sh1.count : sh0.count, threadIdx.x ? sh1.n : sh0.n);
     __syncthreads();
-    const bool last0 = uni(flag[0]), last1 = nsh == 2 && uni(flag[1]);
+    unsigned todo = (unsigned)uni(flag[0]) | (nsh == 2 ? (unsigned)uni(flag[1]) << 1 : 0u);
+    unsigned level = (sh0.direct ? 1u : 0u) | (sh1.direct ? 2u : 0u);       // bit k: sh_k's members are all of its sequence's
 #pragma unroll 1
-    for (int k = 0; k < 2; ++k) {
-        if (!(k ? last1 : last0)) continue;
-        Share s = k ? sh1 : sh0;
-        const Heads hd = heads_of(s.h);
-#pragma unroll 1
-        for (int level = s.direct;; ++level) {
+    while (todo) {
+        // One item = 4 numbers of a head; ng threads have every ng-th member of
+        // an item: as many as fill half of the workgroup, or all of it for the
+        // many members of a long sequence, whether there is one share to add or
+        // two (the order of the sums is always the same)
+        const int items0 = heads_of(sh0.h).n * (D / 4), items1 = heads_of(sh1.h).n * (D / 4);
+        const int ng0 = max(1, (sh0.direct ? NT / 2 : NT) / items0), ng1 = max(1, (sh1.direct ? NT / 2 : NT) / items1);
+        const int slots0 = todo & 1 ? items0 * ng0 : 0, slots1 = todo & 2 ? items1 * ng1 : 0;
+        // (the threads of an item are in one pass)
+        const int from1 = slots0 + slots1 > NT ? (slots0 + NT - 1) / NT * NT : slots0;
+        for (int i0 = 0; i0 < from1 + slots1; i0 += NT) {
+            const int at = i0 + threadIdx.x;
+            const bool k = at >= from1, in = k ? at < from1 + slots1 : at < slots0;
+            const int slot = at - (k ? from1 : 0), items = k ? items1 : items0, ng = k ? ng1 : ng0;
+            const int g = ng == 1 ? 0 : slot / items, it = slot - g * items, hq = it / (D / 4), d = it % (D / 4) * 4;
+            const unsigned v0 = k ? sh1.v0 : sh0.v0, m0 = k ? sh1.m0 : sh0.m0, stride = k ? sh1.stride : sh0.stride;
+            const int n = (int)(k ? sh1.n : sh0.n);
             auto share = [&](unsigned x) __attribute__((always_inline)) {
-                const unsigned v = max(s.v0, s.m0 + s.stride * x);
-                return (2 * v + (v == s.v0)) * kPart;
+                const unsigned v = max(v0, m0 + stride * x);
+                return (2 * v + (v == v0)) * kPart;
             };
-            // one item = 4 numbers of a head; groups of threads take every ng-th share
-            const int all = hd.n * (D / 4), items = min(all, NT), ng = NT / items, g = threadIdx.x / items;
-            for (int i0 = 0; i0 < all; i0 += NT) {
-                const int item = i0 + threadIdx.x - g * items;
-                const int hq = item / (D / 4), d = item % (D / 4) * 4;
-                const bool in = g < ng && item < all;
-                f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-                float ss = 0.f, top = -INFINITY;
-                if (in)
-                    for (int x0 = g; x0 < (int)s.n; x0 += kBatch * ng) {
-                        float2 ms[kBatch];
-                        f32x4 y[kBatch];
+            f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+            float ss = 0.f, top = -INFINITY;
+            if (in)
+                for (int x0 = g; x0 < n; x0 += kBatch * ng) {
+                    float2 ms[kBatch];
+                    f32x4 y[kBatch];
 #pragma unroll
-                        for (int x = 0; x < kBatch; ++x) {
-                            const unsigned p = x0 + x * ng < (int)s.n ? share((unsigned)(x0 + x * ng)) : kOob;
-                            ms[x] = load_through2(pr, p + (kKvHeads * D + 2 * hq) * 4);
-                            y[x] = load_through4(pr, p + (hq * D + d) * 4);
-                        }
-                        float tn = top;
-#pragma unroll
-                        for (int x = 0; x < kBatch; ++x) {
-                            if (x0 + x * ng >= (int)s.n) ms[x] = float2{-INFINITY, 0.f};
-                            tn = fmaxf(tn, ms[x].x);
-                        }
-                        const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
-                        top = tn;
-                        ss *= fo;
-                        v *= fo;
-#pragma unroll
-                        for (int x = 0; x < kBatch; ++x) {
-                            const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
-                            ss += fx * ms[x].y;
-                            if (fx != 0.f) v += fx * y[x];
-                        }
+                    for (int x = 0; x < kBatch; ++x) {
+                        const unsigned p = x0 + x * ng < n ? share((unsigned)(x0 + x * ng)) : kOob;
+                        ms[x] = load_through2(pr, p + (kKvHeads * D + 2 * hq) * 4);
+                        y[x] = load_through4(pr, p + (hq * D + d) * 4);
                     }
-                f32x4* const fv = reinterpret_cast<f32x4*>(lds);
-                float2* const fs = reinterpret_cast<float2*>(lds + NT);
-                if (ng > 1) {
-                    fv[threadIdx.x] = v;
-                    fs[threadIdx.x] = float2{top, ss};
-                }
-                __syncthreads();                    // (also: a group's shares are read before one is written over)
-                if (ng > 1 && g == 0) {
                     float tn = top;
-                    for (int x = 1; x < ng; ++x) tn = fmaxf(tn, fs[x * items + threadIdx.x].x);
+#pragma unroll
+                    for (int x = 0; x < kBatch; ++x) {
+                        if (x0 + x * ng >= n) ms[x] = float2{-INFINITY, 0.f};
+                        tn = fmaxf(tn, ms[x].x);
+                    }
                     const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
                     top = tn;
                     ss *= fo;
                     v *= fo;
-                    for (int x = 1; x < ng; ++x) {
-                        const float2 y = fs[x * items + threadIdx.x];
-                        const float fx = y.x == -INFINITY ? 0.f : exp2_(y.x - top);
-                        ss += fx * y.y;
-                        if (fx != 0.f) v += fx * fv[x * items + threadIdx.x];
+#pragma unroll
+                    for (int x = 0; x < kBatch; ++x) {
+                        const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
+                        ss += fx * ms[x].y;
+                        if (fx != 0.f) v += fx * y[x];
                     }
                 }
-                if (in && g == 0) {
-                    if (level) {
-                        finish(s.b, hd.hq0 + hq, d, v, top, ss);
-                    } else {                        // the group's share takes its first one's place
-                        store_through(pr, share(0) + (hq * D + d) * 4, v);
-                        if (d == 0) store_through(pr, share(0) + (kKvHeads * D + 2 * hq) * 4, float2{top, ss});
-                    }
+            f32x4* const fv = reinterpret_cast<f32x4*>(lds);
+            float2* const fs = reinterpret_cast<float2*>(lds + NT);
+            fv[threadIdx.x] = v;
+            fs[threadIdx.x] = float2{top, ss};
+            __syncthreads();                        // (also: a group's shares are read before one is written over)
+            if (in && ng > 1 && g == 0) {
+                float tn = top;
+                for (int x = 1; x < ng; ++x) tn = fmaxf(tn, fs[x * items + threadIdx.x].x);
+                const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
+                top = tn;
+                ss *= fo;
+                v *= fo;
+                for (int x = 1; x < ng; ++x) {
+                    const float2 y = fs[x * items + threadIdx.x];
+                    const float fx = y.x == -INFINITY ? 0.f : exp2_(y.x - top);
+                    ss += fx * y.y;
+                    if (fx != 0.f) v += fx * fv[x * items + threadIdx.x];
                 }
             }
-            if (level) break;
-            at_level(s, 1);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (threadIdx.x == 0) flag[0] = arrive(s.count, s.n);
-            __syncthreads();
-            if (!uni(flag[0])) break;
+            if (in && g == 0) {
+                if (k ? level & 2 : level & 1) {
+                    finish(k ? sh1.b : sh0.b, heads_of(k ? sh1.h : sh0.h).hq0 + hq, d, v, top, ss);
+                } else {                            // the group's share takes its first one's place
+                    store_through(pr, share(0) + (hq * D + d) * 4, v);
+                    if (d == 0) store_through(pr, share(0) + (kKvHeads * D + 2 * hq) * 4, float2{top, ss});
+                }
+            }
         }
+        // groups that are complete now count for their sequences
+        todo &= ~level;
+        if (!todo) break;
+        level = 3;
+        at_level(sh0, 1);
+        at_level(sh1, 1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+        if (threadIdx.x < 2)
+            flag[threadIdx.x] = (todo >> threadIdx.x & 1) && arrive(threadIdx.x ? sh1.count : sh0.count, threadIdx.x ? sh1.n : sh0.n);
+        __syncthreads();
+        todo = (unsigned)uni(flag[0]) | (unsigned)uni(flag[1]) << 1;
     }
 }
 
