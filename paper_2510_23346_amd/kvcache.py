@@ -113,26 +113,30 @@ class KVCache:
     def _rows(self, name, t, n, width):
         """Row stride of a bf16 tensor of n rows: [n, width], or [n, heads, head_dim]."""
         sh, st = t.shape, t.stride()
-        ok = t.dtype == self._bf16 and t.get_device() == self.device and sh[0] == n
-        if len(sh) == 2:
-            ok = ok and sh[1] == width and st[1] == 1
-        else:
-            ok = ok and len(sh) == 3 and sh[2] == self.head_dim and sh[1] * sh[2] == width and st[2] == 1 and \
-                (st[1] == self.head_dim or sh[1] == 1)
-        if not ok:
-            raise ValueError(f"{name} must be a bf16 tensor [{n}, {width}] on cuda:{self.device} with contiguous rows")
-        return st[0] if n > 1 else width
+        if t.dtype is self._bf16 and t.get_device() == self.device:
+            if sh == (n, width):
+                if st[1] == 1:
+                    return st[0] if n > 1 else width
+            elif len(sh) == 3 and sh == (n, width // self.head_dim, self.head_dim) and st[2] == 1 and \
+                    (st[1] == self.head_dim or sh[1] == 1):
+                return st[0] if n > 1 else width
+        raise ValueError(f"{name} must be a bf16 tensor [{n}, {width}] on cuda:{self.device} with contiguous rows")
 
     def _ints(self, name, t, n):
-        if t.dtype != self._i32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != self.device:
-            raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values on cuda:{self.device}")
-        return t.data_ptr()
+        if t.dtype is self._i32 and t.shape == (n,) and t.get_device() == self.device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values on cuda:{self.device}")
 
     def _table(self, t):
-        st = t.stride()
-        if t.dtype != self._i32 or t.dim() != 2 or st[1] != 1 and t.shape[1] > 1 or t.get_device() != self.device:
-            raise ValueError(f"table must be an int32 tensor [sequences, width] on cuda:{self.device} with contiguous rows")
-        return t.data_ptr(), (st[0] if t.shape[0] > 1 else t.shape[1]), t.shape[1]
+        sh, st = t.shape, t.stride()
+        if t.dtype is self._i32 and len(sh) == 2 and (st[1] == 1 or sh[1] <= 1) and t.get_device() == self.device:
+            return t.data_ptr(), (st[0] if sh[0] > 1 else sh[1]), sh[1], sh[0]
+        raise ValueError(f"table must be an int32 tensor [sequences, width] on cuda:{self.device} with contiguous rows")
+
+    def _floats(self, name, t, shape):
+        if t.dtype is self._f32 and t.shape == shape and t.get_device() == self.device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name} must be a contiguous fp32 tensor {list(shape)} on cuda:{self.device}")
 
     # -- operators --------------------------------------------------------
     def append(self, qkv, cos, sin, seqs, index, positions, table, lens, q_out, interleaved: bool = False, stream=None):
@@ -145,18 +149,15 @@ class KVCache:
         T = qkv.shape[0]
         qs = self._rows("qkv", qkv, T, self._qkvw)
         os_ = self._rows("q_out", q_out, T, self._qw)
-        for t in (cos, sin):
-            if t.dtype != self._f32 or t.shape != cos.shape or t.dim() != 2 or t.shape[1] * 2 != self.head_dim or \
-                    not t.is_contiguous() or t.get_device() != self.device:
-                raise ValueError(f"cos and sin must be contiguous fp32 tensors [positions, {self.head_dim // 2}] on "
-                                 f"cuda:{self.device}")
-        tp, ts, tw = self._table(table)
-        n = table.shape[0]
-        _check(self._append(self._h, qkv.data_ptr(), qs, cos.data_ptr(), sin.data_ptr(), cos.shape[0], int(interleaved),
-                            self._ints("seqs", seqs, T), self._ints("index", index, T),
-                            self._ints("positions", positions, T), T, tp, ts, tw, n,
-                            None if lens is None else self._ints("lens", lens, n), q_out.data_ptr(), os_,
-                            self._stream(stream)))
+        P = cos.shape[0]
+        angles = (P, self.head_dim // 2)
+        tp, ts, tw, n = self._table(table)
+        rc = self._append(self._h, qkv.data_ptr(), qs, self._floats("cos", cos, angles), self._floats("sin", sin, angles), P,
+                          int(interleaved), self._ints("seqs", seqs, T), self._ints("index", index, T),
+                          self._ints("positions", positions, T), T, tp, ts, tw, n,
+                          None if lens is None else self._ints("lens", lens, n), q_out.data_ptr(), os_, self._stream(stream))
+        if rc:
+            _check(rc)
 
     def attend(self, q, table, lens, out, starts=None, scale=None, lse=None, accumulate: bool = False, stream=None):
         """Attention of row b of ``q [B, n_q_heads head_dim]`` over entries
@@ -168,25 +169,24 @@ class KVCache:
         B = q.shape[0]
         qs = self._rows("q", q, B, self._qw)
         os_ = self._rows("out", out, B, self._qw)
-        tp, ts, tw = self._table(table)
-        if table.shape[0] < B:
-            raise ValueError(f"table has {table.shape[0]} rows for {B} sequences")
-        if lse is not None and (lse.dtype != self._f32 or tuple(lse.shape) != (B, self.n_q_heads) or
-                                not lse.is_contiguous() or lse.get_device() != self.device):
-            raise ValueError(f"lse must be a contiguous fp32 tensor [{B}, {self.n_q_heads}] on cuda:{self.device}")
-        _check(self._attend(self._h, q.data_ptr(), qs, B, tp, ts, tw, self._ints("lens", lens, B),
-                            None if starts is None else self._ints("starts", starts, B),
-                            self._scale if scale is None else scale, int(accumulate), out.data_ptr(), os_,
-                            None if lse is None else lse.data_ptr(), self._stream(stream)))
+        tp, ts, tw, n = self._table(table)
+        if n < B:
+            raise ValueError(f"table has {n} rows for {B} sequences")
+        rc = self._attend(self._h, q.data_ptr(), qs, B, tp, ts, tw, self._ints("lens", lens, B),
+                          None if starts is None else self._ints("starts", starts, B),
+                          self._scale if scale is None else scale, int(accumulate), out.data_ptr(), os_,
+                          None if lse is None else self._floats("lse", lse, (B, self.n_q_heads)), self._stream(stream))
+        if rc:
+            _check(rc)
 
     def evict(self, table, lens, budget: int, recent: int = 0, stream=None):
         """Cut the sequences of ``table`` to ``budget`` entries per kv head:
         the last ``recent`` positions stay, then the largest weights; kept
         entries from behind the budget move into the freed places."""
-        tp, ts, tw = self._table(table)
-        B = table.shape[0]
-        _check(self._evict(self._h, B, tp, ts, tw, self._ints("lens", lens, B), int(budget), int(recent),
-                           self._stream(stream)))
+        tp, ts, tw, B = self._table(table)
+        rc = self._evict(self._h, B, tp, ts, tw, self._ints("lens", lens, B), int(budget), int(recent), self._stream(stream))
+        if rc:
+            _check(rc)
 
     def device_error(self, stream=None) -> int:
         f = _c.c_int32(0)
