@@ -378,17 +378,17 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
         moves = kv_select<kReread>(a, b, h, n, L, keys);
     // this workgroup has read what it needs of weights, positions and lengths
     __syncthreads();
+    const bool alone = Z == 1;              // of its head
     if (threadIdx.x == 0) {
         unsigned* const ch = a.count + (size_t)b * a.c.hkv + h;
         unsigned* const cs = a.count + (size_t)gridDim.x * a.c.hkv + b;
-        const bool lh = __hip_atomic_fetch_add(ch, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)Z - 1;
-        const bool ls = __hip_atomic_fetch_add(cs, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)Z * a.c.hkv - 1;
-        if (lh) __hip_atomic_store(ch, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (ls) {
-            __hip_atomic_store(cs, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            a.lens[b] = M;
-        }
-        last_head = lh;
+        auto arrive = [](unsigned* c, unsigned n) {
+            const bool last = n == 1 || __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+            if (last && n > 1) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            return last;
+        };
+        if (arrive(cs, (unsigned)Z * a.c.hkv)) a.lens[b] = M;
+        last_head = !alone && arrive(ch, (unsigned)Z);
     }
     const bool in_lds = moves <= kListCap;
     // place and source of move k, as entries of all pages; false where a page is none
@@ -407,13 +407,16 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
         from = kv_entry(a.c, b, h, j);
         return to >= 0 && from >= 0;
     };
-    // keys and values: LPR lanes a row, four moves in flight
+    // keys and values: LPR lanes a row, four moves in flight (and weights and
+    // positions, where no other workgroup is still to read them)
     constexpr int LPR = ROW / 16, RPP = kET / LPR, U = 4;
     const int k1 = (int)((long long)moves * (z + 1) / Z), c = threadIdx.x % LPR * 16;
     for (int k0 = (int)((long long)moves * z / Z) + threadIdx.x / LPR; k0 < k1; k0 += U * RPP) {
         long long to[U], from[U];
         bool ok[U];
         u32x4 x[U], y[U];
+        float w[U];
+        int p[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) ok[u] = k0 + u * RPP < k1 && move(k0 + u * RPP, to[u], from[u]);
 #pragma unroll
@@ -421,14 +424,23 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
             if (ok[u]) {
                 x[u] = *reinterpret_cast<const u32x4*>(a.c.K + from[u] * ROW + c);
                 y[u] = *reinterpret_cast<const u32x4*>(a.c.V + from[u] * ROW + c);
+                if (alone && c == 0) {
+                    w[u] = a.c.weight[from[u]];
+                    p[u] = a.c.pos[from[u]];
+                }
             }
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (ok[u]) {
                 *reinterpret_cast<u32x4*>(a.c.K + to[u] * ROW + c) = x[u];
                 *reinterpret_cast<u32x4*>(a.c.V + to[u] * ROW + c) = y[u];
+                if (alone && c == 0) {
+                    a.c.weight[to[u]] = w[u];
+                    a.c.pos[to[u]] = p[u];
+                }
             }
     }
+    if (alone) return;
     __syncthreads();
     if (last_head)
         for (int k = threadIdx.x; k < moves; k += kET) {
