@@ -203,6 +203,30 @@ def test_graph_replay_with_moved_tokens(torch):
     cache.close()
 
 
+def test_entries_beyond_four_gigabytes(torch):
+    import paper_2510_23346_amd as bd
+    n_pages, page, d = 90_000, 256, 128
+    k = torch.zeros(n_pages, 1, page, d, dtype=torch.bfloat16, device="cuda")        # 5.9 GB each
+    v = torch.zeros_like(k)
+    cache = bd.KVCache(2, 1, d, n_pages, page, 2, k=k, v=v)
+    rng = np.random.default_rng(4)
+    bits, x = wl.bf16_round(rng.standard_normal((2, 4 * d)))
+    qkv = torch.from_numpy(bits.view(np.int16)).cuda().view(torch.bfloat16)
+    c, s = _tables(d, 8)
+    table = torch.tensor([[0, n_pages - 1], [70_001, 3]], dtype=torch.int32, device="cuda")
+    i32 = lambda z: torch.tensor(z, dtype=torch.int32, device="cuda")  # noqa: E731
+    lens = i32([256, 200])
+    cache.append(qkv, torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda(), i32([0, 1]), i32([257, 255]), i32([3, 5]), table,
+                 lens, torch.empty(2, 2 * d, dtype=torch.bfloat16, device="cuda"))
+    x = x.reshape(2, 4, d)
+    for t, (pg, at, p) in enumerate(((n_pages - 1, 1, 3), (70_001, 255, 5))):
+        y = _f32_rotate(x[t, 2:3], c[p], s[p], False)
+        assert np.array_equal(host_bits(k[pg, 0, at]), wl.bf16_round(y)[0][0])
+        assert np.array_equal(host_bits(v[pg, 0, at]), bits.reshape(2, 4, d)[t, 3])
+    assert int(torch.count_nonzero(k.view(torch.int16)).item()) <= 2 * d and lens.tolist() == [258, 256]
+    cache.close()
+
+
 def test_refusals(torch):
     import paper_2510_23346_amd as bd
     dc = DrawnCache([4, 4], 1, 64, 16, seed=3, room=1)

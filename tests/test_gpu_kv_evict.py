@@ -150,6 +150,45 @@ def test_graph_replays(torch):
     cache.close()
 
 
+def test_entries_beyond_four_gigabytes(torch):
+    import paper_2510_23346_amd as bd
+    n_pages, page, d = 90_000, 256, 128
+    k = torch.zeros(n_pages, 1, page, d, dtype=torch.bfloat16, device="cuda")        # 5.9 GB each
+    v = torch.zeros_like(k)
+    cache = bd.KVCache(2, 1, d, n_pages, page, 1, k=k, v=v, weights=True)
+    at = [n_pages - 1, 5, 88_000]                                                    # 600 entries in three pages
+    table = torch.tensor([at], dtype=torch.int32, device="cuda")
+    rng = np.random.default_rng(5)
+    w = rng.permutation(768).astype(np.float32)
+    for j, pg in enumerate(at):
+        e = torch.arange(page, device="cuda") + j * page
+        k[pg, 0] = (e % 251)[:, None].to(torch.bfloat16)
+        v[pg, 0] = (e % 241)[:, None].to(torch.bfloat16)
+        cache.weight[pg, 0] = torch.from_numpy(w[j * page:(j + 1) * page]).cuda()
+        cache.pos[pg, 0] = e.int()
+    lens = torch.tensor([600], dtype=torch.int32, device="cuda")
+    cache.evict(table, lens, 300, 10)
+    places, sources = okv.evict_plan(w[:600], np.arange(600), 300, 10)
+    order = np.arange(600)
+    order[places] = sources
+    for i in range(300):
+        pg, o = at[i // page], i % page
+        assert float(k[pg, 0, o, 7]) == order[i] % 251 and float(v[pg, 0, o, 100]) == order[i] % 241
+        assert int(cache.pos[pg, 0, o]) == order[i] and float(cache.weight[pg, 0, o]) == w[order[i]]
+    assert lens.tolist() == [300] and cache.device_error() == 0
+    cache.close()
+
+
+@pytest.mark.parametrize("n,budget", [(8192, 4096), (8193, 4000), (28672, 9000), (28673, 20000), (8000, 7700)])
+def test_lengths_where_the_keys_move_house(torch, n, budget):
+    """Keys in registers, in LDS, read again; moves in LDS and in memory; one
+    workgroup a head and several."""
+    dc = DrawnCache([n, n - 1, 3], 2, 64, 16, seed=n + budget)
+    rng = np.random.default_rng(n)
+    _set(dc, 1, weight=rng.integers(0, 3, (2, n - 1)))
+    _check(torch, dc, budget, 100)
+
+
 def test_refusals(torch):
     import paper_2510_23346_amd as bd
     dc = DrawnCache([20, 30], 1, 64, 16, seed=6)
