@@ -622,6 +622,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
         // (the threads of an item are in one pass)
         const int from1 = slots0 + slots1 > NT ? (slots0 + NT - 1) / NT * NT : slots0;
         for (int i0 = 0; i0 < from1 + slots1; i0 += NT) {
+            if (i0) __syncthreads();                // (the pass before has read its sums)
             const int at = i0 + threadIdx.x;
             const bool k = at >= from1, in = k ? at < from1 + slots1 : at < slots0;
             const int slot = at - (k ? from1 : 0), items = k ? items1 : items0, ng = k ? ng1 : ng0;

@@ -167,6 +167,26 @@ def test_a_long_sequence_beside_short_ones_and_the_same_bits_again(torch):
     cache.close()
 
 
+@pytest.mark.parametrize("lens", [[9001, 8013, 8490, 9100], [1100, 990, 1300, 1201, 1055, 1499]])
+@pytest.mark.parametrize("hq,d", [(1, 64), (4, 128)])
+def test_sequences_that_meet_within_a_workgroup(torch, lens, hq, d):
+    """Each goes over many workgroups, and those at the ends have parts of
+    two: both may be completed, and added, by one workgroup."""
+    dc = DrawnCache(lens, 1, d, 16, seed=hq)
+    cache, table, dl = dc.device(n_q_heads=hq)
+    q, qv = _queries(torch, len(lens), hq, d, seed=8)
+    runs = []
+    for _ in range(8):
+        out = torch.full((len(lens), hq * d), float("nan"), dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((len(lens), hq), float("nan"), device="cuda")
+        cache.attend(q, table, dl, out, lse=lse)
+        runs.append((out, lse))
+    _check(dc, qv, *runs[0], None, None, d ** -0.5)
+    for out, lse in runs[1:]:
+        assert torch.equal(out.view(torch.int16), runs[0][0].view(torch.int16)) and torch.equal(lse, runs[0][1])
+    cache.close()
+
+
 def test_large_batch_of_short_sequences(torch):
     rng = np.random.default_rng(0)
     lens = rng.integers(0, 40, 700)
