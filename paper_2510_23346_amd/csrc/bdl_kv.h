@@ -19,6 +19,12 @@ constexpr int kKvMinPage = 16, kKvMaxPage = 65536;
 // and what one leaves for a sequence that it shares with others: unnormalised
 // sums [heads][D], then each head's maximum and sum
 constexpr int kKvAttendGrid = 512, kKvHeads = 16;
+
+// Counters lie a cache line apart (in numbers of 4 bytes): atomic operations on
+// one line wait for each other, 16 sequences' 512 of them for 2.5 us.  Attention
+// has one for each sequence that goes on behind the workgroup it begins in, and
+// one for each group of a sequence's workgroups, of which two can begin at one.
+constexpr int kKvCount = 32, kKvAttendCounts = 3 * kKvAttendGrid;
 constexpr int kv_part_floats(int D) { return kKvHeads * (D + 2); }
 
 // What every kernel knows of the cache and of the call's page table.  Pages
@@ -57,8 +63,7 @@ struct KvAttendArgs {
     float* lse;                 // may be null
     int B, n_cu;
     float* part;                // [2 kKvAttendGrid][kv_part_floats(D)]
-    unsigned* count;            // [B][hkv][head tiles]: zero between calls
-    unsigned* group_count;      // [2 kKvAttendGrid]: zero between calls
+    unsigned* count;            // kKvAttendCounts counters: zero between calls
     float* logits;              // accumulating: [n_pages][hq][page], products <q, k>
     float* lse2;                // accumulating: [B][hq], lse in those units
     float score_scale;    // > 0, times the product of raw values: scores in units of log 2
@@ -71,7 +76,7 @@ struct KvEvictArgs {
     int* lens;
     int B, budget, recent, n_cu;
     int* scratch;         // [n_pages][hkv][page]: the places to fill and what fills them
-    unsigned* count;      // [B][hkv], then [B]: zero between calls
+    unsigned* count;      // B hkv counters, then B: zero between calls
 };
 
 hipError_t launch_kv_append(const KvAppendArgs& a, int head_dim, bool fp8, hipStream_t s);

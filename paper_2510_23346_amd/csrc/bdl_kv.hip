@@ -386,15 +386,18 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
     __syncthreads();
     const bool alone = Z == 1;              // of its head
     if (threadIdx.x == 0) {
-        unsigned* const ch = a.count + (size_t)b * a.c.hkv + h;
-        unsigned* const cs = a.count + (size_t)gridDim.x * a.c.hkv + b;
-        auto arrive = [](unsigned* c, unsigned n) {
-            const bool last = n == 1 || __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
-            if (last && n > 1) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            return last;
-        };
-        if (arrive(cs, (unsigned)Z * a.c.hkv)) a.lens[b] = M;
-        last_head = !alone && arrive(ch, (unsigned)Z);
+        unsigned* const ch = a.count + ((size_t)b * a.c.hkv + h) * kKvCount;
+        unsigned* const cs = a.count + ((size_t)gridDim.x * a.c.hkv + b) * kKvCount;
+        const unsigned nh = Z, ns = Z * a.c.hkv;
+        // (both counted at once)
+        const unsigned at_h = nh > 1 ? __hip_atomic_fetch_add(ch, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+        const unsigned at_s = ns > 1 ? __hip_atomic_fetch_add(cs, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+        last_head = !alone && at_h == nh - 1;
+        if (last_head) __hip_atomic_store(ch, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (at_s == ns - 1) {
+            if (ns > 1) __hip_atomic_store(cs, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            a.lens[b] = M;
+        }
     }
     const bool in_lds = moves <= kListCap;
     // place and source of move k, as entries of all pages; false where a page is none

@@ -23,10 +23,9 @@ struct bdlora_kv {
     int n_cu = 0;
     float* lse2 = nullptr;         // [max_seqs][n_q_heads]
     float* part = nullptr;         // attend's shares of sequences
-    unsigned* count = nullptr;     // [max_seqs][n_kv_heads][head tiles]
-    unsigned* group_count = nullptr;   // [2 kKvAttendGrid]
+    unsigned* count = nullptr;     // kKvAttendCounts counters
     float* logits = nullptr;       // [n_pages][n_q_heads][page_size]
-    unsigned* evict_count = nullptr;   // [max_seqs][n_kv_heads + 1]
+    unsigned* evict_count = nullptr;   // [max_seqs][n_kv_heads + 1] counters
     int* scratch = nullptr;        // [n_pages][n_kv_heads][page_size], where logits lie too
 };
 
@@ -82,7 +81,7 @@ int check_desc(const bdlora_kv_desc* d) {
 }
 
 struct Parts {
-    long long clear, err, count, group_count, evict_count, part, lse2, logits, total;   // (what starts at zero lies below clear)
+    long long clear, err, count, evict_count, part, lse2, logits, total;   // (what starts at zero lies below clear)
 };
 
 Parts layout(const bdlora_kv_desc& d, bool weights) {
@@ -93,11 +92,9 @@ Parts layout(const bdlora_kv_desc& d, bool weights) {
         at += (bytes + 255) / 256 * 256;
         return r;
     };
-    const long long group = d.n_q_heads / d.n_kv_heads;
     p.err = take(4);
-    p.count = take(4LL * d.max_seqs * d.n_kv_heads * ((group + bdl::kKvHeads - 1) / bdl::kKvHeads));
-    p.group_count = take(2LL * bdl::kKvAttendGrid * 4);
-    p.evict_count = take(weights ? 4LL * d.max_seqs * (d.n_kv_heads + 1) : 0);
+    p.count = take(4LL * bdl::kKvCount * bdl::kKvAttendCounts);
+    p.evict_count = take(weights ? 4LL * bdl::kKvCount * d.max_seqs * (d.n_kv_heads + 1) : 0);
     p.clear = at;
     p.part = take(2LL * bdl::kKvAttendGrid * bdl::kv_part_floats(d.head_dim) * 4);
     p.lse2 = take(weights ? 4LL * d.max_seqs * d.n_q_heads : 0);
@@ -192,7 +189,6 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
         c->err = (int*)(ws + p.err);
         c->n_cu = std::max(1, prop.multiProcessorCount);
         c->count = (unsigned*)(ws + p.count);
-        c->group_count = (unsigned*)(ws + p.group_count);
         c->part = (float*)(ws + p.part);
         c->lse2 = (float*)(ws + p.lse2);
         c->logits = (float*)(ws + p.logits);
@@ -303,7 +299,6 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         a.n_cu = c->n_cu;
         a.part = c->part;
         a.count = c->count;
-        a.group_count = c->group_count;
         a.logits = c->logits;
         a.lse2 = c->lse2;
         // (the kernels mask with -infinity times the scale: it is kept above zero)

@@ -130,7 +130,6 @@ struct Tile {
 // added by its last workgroup; more are added in groups of kGroup workgroups
 // first, so that no workgroup reads more than a few dozen
 constexpr unsigned kDirect = 32, kGroup = 16;
-constexpr int kBatch = 4;               // shares whose loads are in flight at once
 
 template <int D, bool FP8, bool ACC, bool WIDE>
 __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArgs a) {
@@ -583,7 +582,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
         s.m0 = s.direct ? s.v0 : level ? s.v0 / kGroup * kGroup : max(s.v0, grp * kGroup);
         s.stride = s.direct || !level ? 1u : kGroup;
         s.n = s.direct ? s.v1 - s.v0 + 1 : level ? s.v1 / kGroup - s.v0 / kGroup + 1 : min(s.v1 + 1, (grp + 1) * kGroup) - s.m0;
-        s.count = level ? a.count + (size_t)s.b * HH + s.h : a.group_count + 2 * s.m0 + (s.m0 == s.v0);
+        s.count = a.count + (level ? s.v0 : kKvAttendGrid + 2 * s.m0 + (s.m0 == s.v0)) * kKvCount;
     };
     auto share_of = [&](const Chain& c) __attribute__((always_inline)) {
         Share s;
@@ -613,11 +612,17 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
 #pragma unroll 1
     while (todo) {
         // One item = 4 numbers of a head; ng threads have every ng-th member of
-        // an item: as many as fill half of the workgroup, or all of it for the
-        // many members of a long sequence, whether there is one share to add or
-        // two (the order of the sums is always the same)
+        // an item: as many as fill half of the workgroup, so that two shares are
+        // added at once, or all of it where one of these would have more than
+        // 16 members or in groups (64 sequences of 4096, 8 members: 22.2 against
+        // 22.9 us; one of 131072, 512: 36.6 against 35.7).  This depends on the
+        // share alone, and so does the order of its sums
         const int items0 = heads_of(sh0.h).n * (D / 4), items1 = heads_of(sh1.h).n * (D / 4);
-        const int ng0 = max(1, (sh0.direct ? NT / 2 : NT) / items0), ng1 = max(1, (sh1.direct ? NT / 2 : NT) / items1);
+        auto threads_of = [](const Share& s, int items) __attribute__((always_inline)) {
+            const int half = max(1, NT / 2 / items);
+            return s.direct && (int)s.n <= 16 * half ? half : max(1, NT / items);
+        };
+        const int ng0 = threads_of(sh0, items0), ng1 = threads_of(sh1, items1);
         const int slots0 = todo & 1 ? items0 * ng0 : 0, slots1 = todo & 2 ? items1 * ng1 : 0;
         // (the threads of an item are in one pass)
         const int from1 = slots0 + slots1 > NT ? (slots0 + NT - 1) / NT * NT : slots0;
@@ -635,7 +640,8 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
             };
             f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
             float ss = 0.f, top = -INFINITY;
-            if (in)
+            auto add = [&](auto batch) __attribute__((always_inline)) {
+                constexpr int kBatch = decltype(batch)::value;      // shares whose loads are in flight at once
                 for (int x0 = g; x0 < n; x0 += kBatch * ng) {
                     float2 ms[kBatch];
                     f32x4 y[kBatch];
@@ -662,6 +668,15 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
                         if (fx != 0.f) v += fx * y[x];
                     }
                 }
+            };
+            if (in) {
+                if (n <= 4 * ng)
+                    add(std::integral_constant<int, 4>{});
+                else if (n <= 8 * ng)
+                    add(std::integral_constant<int, 8>{});
+                else
+                    add(std::integral_constant<int, 16>{});
+            }
             f32x4* const fv = reinterpret_cast<f32x4*>(lds);
             float2* const fs = reinterpret_cast<float2*>(lds + NT);
             fv[threadIdx.x] = v;
