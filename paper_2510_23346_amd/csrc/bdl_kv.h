@@ -21,7 +21,7 @@ constexpr int kKvMinPage = 16, kKvMaxPage = 65536;
 constexpr int kKvAttendGrid = 512, kKvHeads = 16;
 
 // Counters lie a cache line apart (in numbers of 4 bytes): atomic operations on
-// one line wait for each other, 16 sequences' 512 of them for 2.5 us.  Attention
+// one line wait for each other, 512 of 16 sequences for 4 us.  Attention
 // has one for each sequence that goes on behind the workgroup it begins in, and
 // one for each group of a sequence's workgroups, of which two can begin at one.
 constexpr int kKvCount = 32, kKvAttendCounts = 3 * kKvAttendGrid;
