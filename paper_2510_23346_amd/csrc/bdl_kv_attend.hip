@@ -26,9 +26,9 @@
 //
 // Measured, one launch: 305 MB of keys and values in bf16 (256 sequences of up
 // to 4353 entries, 8 query heads of 128 on one kv head) 63.5 us, 4.8 TB/s; 134 MB of
-// one sequence of 131072 33.6 us; 73 MB of 64 sequences 20.8 us, in 8 bits
+// one sequence of 131072 33.6 us; 72 MB of 64 sequences 20.8 us, in 8 bits
 // 21.6 us; one sequence of 509 entries 8.6 us.  Without joining anything the
-// 73 MB take 16.7 us: what is over the copy's rate there is the wait for the
+// 72 MB take 16.7 us: what is over the copy's rate there is the wait for the
 // last wave's loads, the pieces in LDS (1.3 us), their way through memory
 // (1 us) and the sum of the shares (1.3 to 2 us).
 #include "bdl_kv_device.h"
