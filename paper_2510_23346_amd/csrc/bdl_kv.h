@@ -61,7 +61,7 @@ struct KvAttendArgs {
     const int *lens, *starts;
     int has_starts;             // 0: starts is there to be read, and means nothing
     float* lse;                 // may be null
-    int B, n_cu;
+    int B;
     float* part;                // [2 kKvAttendGrid][kv_part_floats(D)]
     unsigned* count;            // kKvAttendCounts counters: zero between calls
     float* logits;              // accumulating: [n_pages][hq][page], products <q, k>

@@ -296,7 +296,6 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         a.has_starts = starts != nullptr;
         a.lse = lse;
         a.B = B;
-        a.n_cu = c->n_cu;
         a.part = c->part;
         a.count = c->count;
         a.logits = c->logits;
