@@ -149,17 +149,19 @@ hipError_t append(const KvAppendArgs& a, hipStream_t s) {
 // Selection: the rank key of the last entry that stays, found in up to three
 // passes over the keys (11, 11 and 10 bits; histograms in LDS), then places and
 // sources by prefix sums.  A thread owns consecutive entries.  Their keys are
-// kept in registers (8192 entries of a sequence) or LDS (28672), and read
-// again in each pass above that.
+// kept in registers (up to 24576 entries of a sequence), or the first 8192 there
+// and 28672 more in LDS, and what is left is read again in each pass.
 //
 // Measured: 64 sequences from 2049 to 2048 entries 9.8 us, of which 2 are the
 // way to lengths, pages and weights, 1.1 to 1.5 each pass, 1.3 the places and 1
 // the one row that moves: a chain of waits, 64 workgroups.  8 sequences of two
 // kv heads from 8192 to 2048 18.3 us, 10 of them the same chain over four
 // times the entries and 5 the 25 MB that move.
+// One of 16384 to 4096 23 us, of 32768 42; of 131072 to 8192 234, most of it the
+// keys read again in each pass, a thread's at a time.
 constexpr int kET = 1024, kEW = kET / 64;
-constexpr int kRegGroups = 2;           // groups of four entries a thread keeps in registers
-constexpr int kRegEntries = 4 * kRegGroups * kET, kLdsEntries = 28 * kET;
+constexpr int kFewGroups = 2, kRegGroups = 6, kLdsGroups = 7;      // groups of four entries a thread keeps
+constexpr int kFewEntries = 4 * kFewGroups * kET, kRegEntries = 4 * kRegGroups * kET;
 constexpr int kListCap = 4096;          // moves whose lists fit LDS; more go through a.scratch
 
 // An entry's rank key: the protected ones above all, then the weights in
@@ -196,18 +198,19 @@ __device__ __forceinline__ long long four_at(const KvCache& c, int b, int h, int
     return kv_entry(c, b, h, 4 * g);
 }
 
-enum Keep { kRegs, kLds, kReread };
-
-template <Keep KEEP>
+// R groups of a thread in registers; with MORE the next ones in LDS, and what
+// is left is read again each time
+template <int R, bool MORE>
 __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int n, EvictLds& L, uint4* keys) {
-    constexpr int R = KEEP == kRegs ? kRegGroups : 1;
+    constexpr int U = 4;                // groups whose loads are in flight at once, behind the first R
     const int tid = threadIdx.x, M = a.budget, groups = (n + 3) / 4;
     const int per = (groups + kET - 1) / kET, g0 = tid * per;
-    auto get = [&](int g, float4& ww, int4& pp) __attribute__((always_inline)) {
+    int mine = min(n - 4 * g0, 4 * per);        // the thread's entries (none: less than one)
+    auto get = [&](int k, float4& ww, int4& pp) __attribute__((always_inline)) {
         ww = float4{NAN, NAN, NAN, NAN};
         pp = int4{INT_MIN, INT_MIN, INT_MIN, INT_MIN};
-        if (g >= groups) return;
-        const long long e = four_at(a.c, b, h, g);
+        if (k >= per || g0 + k >= groups) return;
+        const long long e = four_at(a.c, b, h, g0 + k);
         if (e < 0) return;
         ww = *reinterpret_cast<const float4*>(a.c.weight + e);
         pp = *reinterpret_cast<const int4*>(a.c.pos + e);
@@ -216,27 +219,33 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     float4 w[R];
     int4 p[R];
     int last = INT_MIN;
-    auto top = [&](int g, const int4& pp) __attribute__((always_inline)) {
-        const int i = 4 * g;
-        if (i < n) last = max(last, pp.x);
-        if (i + 1 < n) last = max(last, pp.y);
-        if (i + 2 < n) last = max(last, pp.z);
-        if (i + 3 < n) last = max(last, pp.w);
+    auto top = [&](int k, const int4& pp) __attribute__((always_inline)) {
+        const int i = 4 * k;
+        if (i < mine) last = max(last, pp.x);
+        if (i + 1 < mine) last = max(last, pp.y);
+        if (i + 2 < mine) last = max(last, pp.z);
+        if (i + 3 < mine) last = max(last, pp.w);
+    };
+    // f(k, weights, positions) for the groups from `from` on
+    auto read = [&](int from, auto f) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int k0 = from; k0 < per; k0 += U) {
+            float4 ww[U];
+            int4 pp[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) get(k0 + u, ww[u], pp[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (k0 + u < per) f(k0 + u, ww[u], pp[u]);
+        }
     };
     for (int i = tid; i < 2048; i += kET) L.hist[i] = 0;
     if (tid == 0) L.last = INT_MIN;
-    if constexpr (KEEP == kRegs) {
 #pragma unroll
-        for (int k = 0; k < R; ++k) get(k < per ? g0 + k : groups, w[k], p[k]);
+    for (int k = 0; k < R; ++k) get(k, w[k], p[k]);
 #pragma unroll
-        for (int k = 0; k < R; ++k) top(k < per ? g0 + k : groups, p[k]);
-    } else {
-#pragma unroll 2
-        for (int k = 0; k < per; ++k) {
-            get(g0 + k, w[0], p[0]);
-            top(g0 + k, p[0]);
-        }
-    }
+    for (int k = 0; k < R; ++k) top(k, p[k]);
+    if constexpr (MORE) read(R, [&](int k, const float4&, const int4& pp) __attribute__((always_inline)) { top(k, pp); });
 #pragma unroll
     for (int x = 32; x; x >>= 1) last = max(last, __shfl_xor(last, x));
     __syncthreads();
@@ -247,41 +256,40 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
         return uint4{kv_key(ww.x, pp.x > floor_), kv_key(ww.y, pp.y > floor_), kv_key(ww.z, pp.z > floor_), kv_key(ww.w, pp.w > floor_)};
     };
     uint4 key[R];
-    if constexpr (KEEP == kRegs) {
 #pragma unroll
-        for (int k = 0; k < R; ++k) key[k] = key4(w[k], p[k]);
-    }
-    if constexpr (KEEP == kLds) {
-#pragma unroll 2
-        for (int k = 0; k < per; ++k) {
-            get(g0 + k, w[0], p[0]);
-            keys[k * kET + tid] = key4(w[0], p[0]);
+    for (int k = 0; k < R; ++k) key[k] = key4(w[k], p[k]);
+    constexpr int kKept = R + kLdsGroups;
+    if constexpr (MORE)
+#pragma unroll
+        for (int k0 = R; k0 < kKept; k0 += U) {
+            float4 ww[U];
+            int4 pp[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (k0 + u < kKept) get(k0 + u, ww[u], pp[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (k0 + u < kKept) keys[(k0 + u - R) * kET + tid] = key4(ww[u], pp[u]);
         }
-    }
     // f(entry, key) for the thread's entries in order
     auto each = [&](auto f) __attribute__((always_inline)) {
-        auto four = [&](int g, const uint4& k) __attribute__((always_inline)) {
-            const int i = 4 * g;
-            if (i < n) f(i, k.x);
-            if (i + 1 < n) f(i + 1, k.y);
-            if (i + 2 < n) f(i + 2, k.z);
-            if (i + 3 < n) f(i + 3, k.w);
+        const int i0 = 4 * g0;
+        // (the comparisons stay where they are: their results, kept over the
+        // passes, would be more masks than there are scalar registers)
+        if constexpr (R > kFewGroups || MORE) asm volatile("" : "+v"(mine));
+        auto four = [&](int k, const uint4& key) __attribute__((always_inline)) {
+            if (4 * k < mine) f(i0 + 4 * k, key.x);
+            if (4 * k + 1 < mine) f(i0 + 4 * k + 1, key.y);
+            if (4 * k + 2 < mine) f(i0 + 4 * k + 2, key.z);
+            if (4 * k + 3 < mine) f(i0 + 4 * k + 3, key.w);
         };
-        if constexpr (KEEP == kRegs) {
 #pragma unroll
-            for (int k = 0; k < R; ++k)
-                if (k < per) four(g0 + k, key[k]);
-        } else {
+        for (int k = 0; k < R; ++k)
+            if (k < per) four(k, key[k]);
+        if constexpr (MORE) {
 #pragma unroll 1
-            for (int k = 0; k < per; ++k) {
-                if constexpr (KEEP == kLds) {
-                    key[0] = keys[k * kET + tid];
-                } else {
-                    get(g0 + k, w[0], p[0]);
-                    key[0] = key4(w[0], p[0]);
-                }
-                four(g0 + k, key[0]);
-            }
+            for (int k = R; k < min(per, kKept); ++k) four(k, keys[(k - R) * kET + tid]);
+            read(kKept, [&](int k, const float4& ww, const int4& pp) __attribute__((always_inline)) { four(k, key4(ww, pp)); });
         }
     };
     // the M-th largest key, 11, 11 and 10 bits at a time
@@ -372,11 +380,11 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     return moves;
 }
 
-// LONG: rows of the page table that can name more than kRegEntries
+// LONG: rows of the page table that can name more than kFewEntries
 template <int ROW, bool LONG>
 __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
     __shared__ EvictLds L;
-    __shared__ uint4 keys[LONG ? kLdsEntries / 4 : 1];
+    __shared__ uint4 keys[LONG ? kLdsGroups * kET : 1];
     __shared__ bool last_head;
     const int b = blockIdx.x, h = blockIdx.y, z = blockIdx.z, Z = gridDim.z, M = a.budget;
     const int raw = a.lens[b], n = kv_len(a.c, a.lens, b);
@@ -386,12 +394,12 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
         return;
     }
     int moves;
-    if (!LONG || n <= kRegEntries)
-        moves = kv_select<kRegs>(a, b, h, n, L, keys);
-    else if (n <= kLdsEntries)
-        moves = kv_select<kLds>(a, b, h, n, L, keys);
+    if (!LONG || n <= kFewEntries)
+        moves = kv_select<kFewGroups, false>(a, b, h, n, L, keys);
+    else if (n <= kRegEntries)
+        moves = kv_select<kRegGroups, false>(a, b, h, n, L, keys);
     else
-        moves = kv_select<kReread>(a, b, h, n, L, keys);
+        moves = kv_select<kFewGroups, true>(a, b, h, n, L, keys);
     // this workgroup has read what it needs of weights, positions and lengths
     __syncthreads();
     const bool alone = Z == 1;              // of its head
@@ -497,7 +505,7 @@ hipError_t launch_kv_evict(const KvEvictArgs& a, int head_dim, bool fp8, hipStre
     const long long most = std::min<long long>(a.budget, std::max(0LL, cap - a.budget));
     const int z = most <= 256 ? 1 : (int)std::max(1LL, std::min({a.n_cu / heads, (most + 63) / 64, 64LL}));
     const dim3 grid(a.B, a.c.hkv, z);
-    const bool many = cap > kRegEntries;
+    const bool many = cap > kFewEntries;
     switch (head_dim * (fp8 ? 1 : 2)) {
     case 64: evict<64>(a, grid, many, s); break;
     case 128: evict<128>(a, grid, many, s); break;

@@ -207,3 +207,11 @@ def test_refusals(torch):
     cache.evict(table[:0], lens[:0], 5)
     cache.close()
     bare.close()
+
+
+@pytest.mark.parametrize("n,budget", [(24576, 9000), (24577, 9000), (36864, 12000), (36865, 9001), (70003, 66000), (70003, 200)])
+def test_lengths_where_the_keys_of_long_sequences_move_house(torch, n, budget):
+    dc = DrawnCache([n, n - 1, 3], 1, 64, 64, seed=n + budget)
+    rng = np.random.default_rng(n)
+    _set(dc, 1, weight=rng.integers(0, 3, (1, n - 1)))
+    _check(torch, dc, budget, 100)
