@@ -79,6 +79,24 @@ __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlan
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// What is left of a number without its upper 16 bits, those of two numbers side
+// by side, and the smaller or larger one of each half
+__device__ __forceinline__ float below_bf16(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+
+__device__ __forceinline__ uint32_t upper_halves(float x, float y) {
+    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+}
+
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t x, uint32_t y) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+}
+
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t x, uint32_t y) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+}
+
 // Shares go past the caches that the compute units do not have in common
 // (device scope), 8 or 16 bytes at byte `at` of the workspace
 constexpr int kDeviceScope = 16;
@@ -438,8 +456,9 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
             }
             const float mm = m == -INFINITY ? 0.f : m;
             // exponentials as two bf16 numbers whose sum has 16 significant bits
-            // (the first cut towards zero and the second never 0, so that an
-            // infinite value gives an infinite sum and no NaN)
+            // (the first cut towards zero.  Where it is not 0, neither is the second,
+            // so that an infinite value gives an infinite sum and no NaN; where it
+            // is 0, so is the second, so that the largest value adds nothing)
             u32x4 hi, lo;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -447,9 +466,9 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
                 for (int e = 0; e < 4; e += 2) {
                     const float x = exp2_(fmaf(s[j][e], a.score_scale, -mm)), y = exp2_(fmaf(s[j][e + 1], a.score_scale, -mm));
                     sum += x + y;
-                    const uint32_t ux = __float_as_uint(x), uy = __float_as_uint(y);
-                    hi[j * 2 + e / 2] = __builtin_amdgcn_perm(uy, ux, 0x07060302u);
-                    lo[j * 2 + e / 2] = pk_bf16(x - __uint_as_float(ux & 0xffff0000u), y - __uint_as_float(uy & 0xffff0000u)) | 0x00010001u;
+                    const uint32_t h = upper_halves(x, y);
+                    hi[j * 2 + e / 2] = h;
+                    lo[j * 2 + e / 2] = max_u16x2(pk_bf16(below_bf16(x), below_bf16(y)), min_u16x2(h, 0x00010001u));
                 }
             // (a value before the first entry may be NaN, and 0 times NaN is one)
             if ((cur.lo[0] | cur.lo[1]) > 0) {

@@ -377,3 +377,25 @@ def test_refusals(torch):
     cache.close()
     with pytest.raises(bd.BDLoRAError):
         cache.attend(q, table, dl, out)
+
+
+def test_large_values_of_entries_without_probability_add_nothing(torch):
+    """An entry whose score is -infinity, or far below the others', has
+    probability 0, and 0 times its value is 0, up to the largest number."""
+    dc = DrawnCache([40, 40, 3], 1, 64, 16, seed=2)
+    for b, n in enumerate(dc.lens):
+        k, v = np.zeros((1, n, 64), np.uint16), np.full((1, n, 64), 0x3A80, np.uint16)      # values of 2^-10
+        for e, key in ((1, 0xFF80), (2, 0xC700)):            # -infinity, -32768
+            k[0, e, 0], v[0, e, :] = key, 0x7F7F             # 3.4e38
+            v[0, e, ::2] |= 0x8000
+        dc.put(dc.K, b, k)
+        dc.put(dc.V, b, v)
+    cache, table, dl = dc.device(n_q_heads=4, weights=False)
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 1.0
+    out, lse = torch.empty(3, 256, dtype=torch.bfloat16, device="cuda"), torch.empty(3, 4, device="cuda")
+    cache.attend(q.flatten(1), table, dl, out, lse=lse, scale=1.0)
+    y = device_to_float(out)
+    assert (y == 2.0 ** -10).all(), np.unique(y)
+    assert np.allclose(lse.cpu().numpy(), np.log(np.array([38, 38, 1]))[:, None], atol=1e-6)
+    cache.close()
