@@ -399,3 +399,54 @@ def test_large_values_of_entries_without_probability_add_nothing(torch):
     assert (y == 2.0 ** -10).all(), np.unique(y)
     assert np.allclose(lse.cpu().numpy(), np.log(np.array([38, 38, 1]))[:, None], atol=1e-6)
     cache.close()
+
+
+@pytest.mark.parametrize("d,fp8", [(64, False), (128, False), (64, True)])
+def test_probabilities_keep_the_bits_of_32_in_the_sum_over_values(torch, d, fp8):
+    """Sums over values that all but cancel: one entry of probability p (before
+    the division) and value 1 (times 256 in 8 bits) beside entries of
+    probability 1 whose values are minus the first and the next bits of p (8
+    in bf16, 4 in e4m3), so that what is left is p's bits below about 2^-16.
+
+    Tolerance: the score is one product, exact in fp32; its scaling and the
+    subtraction round numbers of at most 2 in units of log 2 (2^-24 each of
+    it: 2^-23 in all), the exponential to 2^-23, and the sum has at most 9
+    terms that are not 0, 2^-23 each: less than 2^-19 of sum p |v|, and the
+    store's 2^-8 of the result."""
+    B, hq, n = 64, 16, 5
+    rng = np.random.default_rng(d + fp8)
+    dc = DrawnCache([n] * B, 1, d, 16, seed=1, fp8=fp8)
+    qbits, q = wl.bf16_round(rng.uniform(2.0, 9.0, (B, hq)))
+    kbits = okv.e4m3_encode(-1.0) if fp8 else 0xBF80
+    parts = (lambda x: okv.e4m3_values()[okv.e4m3_encode(x)]) if fp8 else (lambda x: wl.bf16_round(x)[1].astype(np.float64))
+    bits = okv.e4m3_encode if fp8 else (lambda x: wl.bf16_round(x)[0])
+    full = np.zeros((B, hq, d))
+    full[:, :, 0] = q
+    for b in range(B):
+        K = np.zeros((1, n, d), dc.K.dtype)
+        K[0, 1, 0] = kbits
+        p = np.exp(-0.125 * q[b].astype(np.float64))
+        v = np.zeros((1, n, d))
+        v[0, 1, :hq] = 256.0 if fp8 else 1.0
+        rest = p * v[0, 1, 0]
+        for e in (0, 2, 3, 4) if fp8 else (0, 2):           # columns 0 .. hq - 1, one for each query head
+            v[0, e, :hq] = -parts(rest)
+            rest = rest + v[0, e, :hq]
+        dc.k[b] = okv.e4m3_values()[K].astype(np.float64) if fp8 else wl.bf16_bits_to_float(K).astype(np.float64)
+        dc.v[b] = v
+        dc.put(dc.K, b, K)
+        dc.put(dc.V, b, bits(v).astype(dc.V.dtype))
+    cache, table, dl = dc.device(n_q_heads=hq, weights=False)
+    qd = torch.from_numpy(wl.bf16_round(full.reshape(B, hq * d))[0].view(np.int16)).cuda().view(torch.bfloat16)
+    out = torch.empty(B, hq * d, dtype=torch.bfloat16, device="cuda")
+    cache.attend(qd, table, dl, out, scale=0.125)
+    y = device_to_float(out).astype(np.float64).reshape(B, hq, d)
+    for b in range(B):
+        for h in range(hq):
+            p = np.exp(0.125 * (dc.k[b][0] @ full[b, h]))
+            p /= p.sum()
+            ref, mag = p @ dc.v[b][0], p @ np.abs(dc.v[b][0])
+            tol = 2.0 ** -8 * np.abs(ref) + 2.0 ** -19 * mag
+            err = np.abs(y[b, h] - ref)
+            assert (err <= tol).all(), (b, h, "times the tolerance: %.2f" % (err[tol > 0] / tol[tol > 0]).max())
+    cache.close()
