@@ -450,3 +450,26 @@ def test_probabilities_keep_the_bits_of_32_in_the_sum_over_values(torch, d, fp8)
             err = np.abs(y[b, h] - ref)
             assert (err <= tol).all(), (b, h, "times the tolerance: %.2f" % (err[tol > 0] / tol[tol > 0]).max())
     cache.close()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", [(16, 1, 128), (12, 1, 128), (40, 2, 128), (40, 2, 64), (17, 1, 64)])
+def test_many_query_heads_over_long_sequences(torch, hq, hkv, d, fp8):
+    """More than 8 query heads a kv head: a workgroup adds its shares in two
+    passes, and in groups where a sequence has more than 32 workgroups; more
+    than 16: further stretches of the line."""
+    lens = [9001, 40001, 8013, 300]
+    dc = DrawnCache(lens, hkv, d, 16, seed=hq + d, fp8=fp8, k_scale=0.02 if fp8 else 1.0, v_scale=0.011 if fp8 else 1.0)
+    cache, table, dl = dc.device(n_q_heads=hq)
+    q, qv = _queries(torch, len(lens), hq, d, seed=hq)
+    runs = []
+    for i in range(4):
+        out = torch.full((len(lens), hq * d), float("nan"), dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((len(lens), hq), float("nan"), device="cuda")
+        cache.attend(q, table, dl, out, lse=lse, accumulate=i == 0)
+        runs.append((out, lse))
+    _check(dc, qv, *runs[0], cache.weight, None, d ** -0.5)
+    for out, lse in runs[1:]:
+        assert torch.equal(out.view(torch.int16), runs[0][0].view(torch.int16)) and torch.equal(lse, runs[0][1])
+    assert cache.device_error() == 0
+    cache.close()
