@@ -562,7 +562,9 @@ int bdlora_kv_attend(bdlora_kv_t cache, const void* q, int64_t q_stride, int32_t
  * that are entries >= budget move, in ascending order, into the places below
  * budget that became free, in ascending order (k, v, weight and pos move;
  * the others are left alone).  lens[b] = min(lens[b], budget).  Sequences
- * within the budget stay as they are.
+ * within the budget stay as they are.  Where the row names a page that is
+ * none, its entries and places are not there: the others are ranked, and as
+ * many of them stay as there are places below the budget.
  * Errors: INVALID_ARG (a cache without weights, too), SHAPE, HIP. */
 int bdlora_kv_evict(bdlora_kv_t cache, int32_t B, const int32_t* table, int64_t table_stride, int32_t table_width,
                     int32_t* lens, int32_t budget, int32_t recent, void* stream);

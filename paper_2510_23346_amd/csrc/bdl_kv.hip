@@ -165,11 +165,12 @@ constexpr int kFewEntries = 4 * kFewGroups * kET, kRegEntries = 4 * kRegGroups *
 constexpr int kListCap = 4096;          // moves whose lists fit LDS; more go through a.scratch
 
 // An entry's rank key: the protected ones above all, then the weights in
-// their order, a NaN below all
+// their order, a NaN below all.  (0: the entry's page is none; it ranks below
+// every entry that is there)
 __device__ __forceinline__ unsigned kv_key(float w, bool prot) {
     const unsigned u = __float_as_uint(w);
     if (prot) return 0xffffffffu;
-    if (w != w) return 0u;
+    if (w != w) return 1u;
     if (w == 0.f) return 0x80000000u;      // either zero
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -179,7 +180,7 @@ struct EvictLds {
     int freed[kListCap], moved[kListCap];
     int wave[2][kEW];
     unsigned digit, need, same;
-    int last;
+    int last, lost;         // largest position; entries below the budget whose page is none
 };
 
 // exclusive prefix sum over the workgroup; total in *total
@@ -206,70 +207,86 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     const int tid = threadIdx.x, M = a.budget, groups = (n + 3) / 4;
     const int per = (groups + kET - 1) / kET, g0 = tid * per;
     int mine = min(n - 4 * g0, 4 * per);        // the thread's entries (none: less than one)
+    // (false: there is no such group, or its page is none)
     auto get = [&](int k, float4& ww, int4& pp) __attribute__((always_inline)) {
         ww = float4{NAN, NAN, NAN, NAN};
         pp = int4{INT_MIN, INT_MIN, INT_MIN, INT_MIN};
-        if (k >= per || g0 + k >= groups) return;
+        if (k >= per || g0 + k >= groups) return false;
         const long long e = four_at(a.c, b, h, g0 + k);
-        if (e < 0) return;
+        if (e < 0) return false;
         ww = *reinterpret_cast<const float4*>(a.c.weight + e);
         pp = *reinterpret_cast<const int4*>(a.c.pos + e);
+        return true;
     };
     // the largest position
     float4 w[R];
     int4 p[R];
-    int last = INT_MIN;
-    auto top = [&](int k, const int4& pp) __attribute__((always_inline)) {
+    bool there[R];
+    int last = INT_MIN, lost = 0;
+    auto top = [&](int k, const int4& pp, bool ok) __attribute__((always_inline)) {
         const int i = 4 * k;
+        if (!ok) lost += max(0, min(4, min(mine, M - 4 * g0) - i));
         if (i < mine) last = max(last, pp.x);
         if (i + 1 < mine) last = max(last, pp.y);
         if (i + 2 < mine) last = max(last, pp.z);
         if (i + 3 < mine) last = max(last, pp.w);
     };
-    // f(k, weights, positions) for the groups from `from` on
+    // f(k, weights, positions, whether they are there) for the groups from `from` on
     auto read = [&](int from, auto f) __attribute__((always_inline)) {
 #pragma unroll 1
         for (int k0 = from; k0 < per; k0 += U) {
             float4 ww[U];
             int4 pp[U];
+            bool ok[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) get(k0 + u, ww[u], pp[u]);
+            for (int u = 0; u < U; ++u) ok[u] = get(k0 + u, ww[u], pp[u]);
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (k0 + u < per) f(k0 + u, ww[u], pp[u]);
+                if (k0 + u < per) f(k0 + u, ww[u], pp[u], ok[u]);
         }
     };
     for (int i = tid; i < 2048; i += kET) L.hist[i] = 0;
-    if (tid == 0) L.last = INT_MIN;
+    if (tid == 0) {
+        L.last = INT_MIN;
+        L.lost = 0;
+    }
 #pragma unroll
-    for (int k = 0; k < R; ++k) get(k, w[k], p[k]);
+    for (int k = 0; k < R; ++k) there[k] = get(k, w[k], p[k]);
 #pragma unroll
-    for (int k = 0; k < R; ++k) top(k, p[k]);
-    if constexpr (MORE) read(R, [&](int k, const float4&, const int4& pp) __attribute__((always_inline)) { top(k, pp); });
+    for (int k = 0; k < R; ++k) top(k, p[k], there[k]);
+    if constexpr (MORE)
+        read(R, [&](int k, const float4&, const int4& pp, bool ok) __attribute__((always_inline)) { top(k, pp, ok); });
 #pragma unroll
     for (int x = 32; x; x >>= 1) last = max(last, __shfl_xor(last, x));
     __syncthreads();
     if ((tid & 63) == 0) atomicMax(&L.last, last);
+    if (lost) atomicAdd(&L.lost, lost);
     __syncthreads();
+    // as many stay as there are places for below the budget: no fewer entries
+    // are there, since those from the budget on are n - M or fewer
+    const int room = M - L.lost;
+    if (room == 0) return 0;
     const long long floor_ = (long long)L.last - a.recent;
-    auto key4 = [&](const float4& ww, const int4& pp) __attribute__((always_inline)) {
+    auto key4 = [&](const float4& ww, const int4& pp, bool ok) __attribute__((always_inline)) {
+        if (!ok) return uint4{0, 0, 0, 0};
         return uint4{kv_key(ww.x, pp.x > floor_), kv_key(ww.y, pp.y > floor_), kv_key(ww.z, pp.z > floor_), kv_key(ww.w, pp.w > floor_)};
     };
     uint4 key[R];
 #pragma unroll
-    for (int k = 0; k < R; ++k) key[k] = key4(w[k], p[k]);
+    for (int k = 0; k < R; ++k) key[k] = key4(w[k], p[k], there[k]);
     constexpr int kKept = R + kLdsGroups;
     if constexpr (MORE)
 #pragma unroll
         for (int k0 = R; k0 < kKept; k0 += U) {
             float4 ww[U];
             int4 pp[U];
+            bool ok[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (k0 + u < kKept) get(k0 + u, ww[u], pp[u]);
+                if (k0 + u < kKept) ok[u] = get(k0 + u, ww[u], pp[u]);
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (k0 + u < kKept) keys[(k0 + u - R) * kET + tid] = key4(ww[u], pp[u]);
+                if (k0 + u < kKept) keys[(k0 + u - R) * kET + tid] = key4(ww[u], pp[u], ok[u]);
         }
     // f(entry, key) for the thread's entries in order
     auto each = [&](auto f) __attribute__((always_inline)) {
@@ -289,11 +306,12 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
         if constexpr (MORE) {
 #pragma unroll 1
             for (int k = R; k < min(per, kKept); ++k) four(k, keys[(k - R) * kET + tid]);
-            read(kKept, [&](int k, const float4& ww, const int4& pp) __attribute__((always_inline)) { four(k, key4(ww, pp)); });
+            read(kKept, [&](int k, const float4& ww, const int4& pp, bool ok) __attribute__((always_inline)) { four(k, key4(ww, pp, ok)); });
         }
     };
-    // the M-th largest key, 11, 11 and 10 bits at a time
-    unsigned known = 0, need = M;       // its leading bits; how many of the keys with these bits stay
+    // the room-th largest key (never that of an entry that is not there), 11, 11
+    // and 10 bits at a time
+    unsigned known = 0, need = room;    // its leading bits; how many of the keys with these bits stay
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
@@ -348,7 +366,7 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     int eq = all_same ? INT_MIN / 2 : eq0, fr = 0, mv = 0;
     each([&](int i, unsigned k) __attribute__((always_inline)) {
         const bool kept = k > known || (k == known && eq++ < (int)need);
-        fr += i < M && !kept;
+        fr += i < M && !kept && k;
         mv += i >= M && kept;
     });
     // (both counts in one scan where they fit 16 bits)
@@ -367,7 +385,7 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     const bool in_lds = moves <= kListCap;
     each([&](int i, unsigned k) __attribute__((always_inline)) {
         const bool kept = k > known || (k == known && eq++ < (int)need);
-        const bool f = i < M && !kept, m = i >= M && kept;
+        const bool f = i < M && !kept && k, m = i >= M && kept;
         if (!f && !m) return;
         const int at = f ? fr++ : mv++;
         if (in_lds) {

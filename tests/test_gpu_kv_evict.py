@@ -215,3 +215,53 @@ def test_lengths_where_the_keys_of_long_sequences_move_house(torch, n, budget):
     rng = np.random.default_rng(n)
     _set(dc, 1, weight=rng.integers(0, 3, (1, n - 1)))
     _check(torch, dc, budget, 100)
+
+
+def _check_with_lost_pages(torch, dc, lost, budget, recent):
+    """lost[b]: pages of sequence b (places of its table row) that the table
+    names by numbers that are none.  Entries there are not there: what is left
+    is ranked, as many stay as there are places for below the budget, and none
+    of these is lost."""
+    cache, table, lens = dc.device()
+    for b, places in enumerate(lost):
+        for i, j in enumerate(places):
+            table[b, j] = -1 - i if i % 2 else dc.n_pages + i
+    cache.evict(table, lens, budget, recent)
+    torch.cuda.synchronize()
+    K, V, W, P = dc.K.copy(), dc.V.copy(), dc.W.copy(), dc.P.copy()
+    got = [host_bits(cache.k), host_bits(cache.v), cache.weight.cpu().numpy(), cache.pos.cpu().numpy()]
+    free = np.zeros(W.shape, bool)
+    moves = 0
+    for b, n in enumerate(dc.lens):
+        i = np.arange(n)
+        there = i[~np.isin(i // dc.ps, lost[b])]
+        room = int((there < budget).sum())
+        for h in range(dc.hkv):
+            if n <= budget:
+                continue
+            places, sources = okv.evict_plan(dc.weight[b][h][there], dc.pos[b][h][there], room, recent) if room else ([], [])
+            to, of = (tuple((dc.table[b, there[x] // dc.ps], h, there[x] % dc.ps)) for x in
+                      (np.array(places, int), np.array(sources, int)))
+            moves = max(moves, len(places))
+            for x in (K, V, W, P):
+                x[to] = x[of]
+        behind = there[there >= budget]
+        free[dc.table[b, behind // dc.ps], :, behind % dc.ps] = True
+    assert np.array_equal(lens.cpu().numpy(), np.minimum(dc.lens, budget))
+    for name, x, y in zip("KVWP", got, (K, V, W, P)):
+        assert np.array_equal(x[~free], y[~free], equal_nan=x.dtype.kind == "f"), name
+    assert cache.device_error() == 1
+    cache.close()
+    return moves
+
+
+@pytest.mark.parametrize("d,fp8", [(64, False), (128, True)])
+def test_pages_lost_below_the_budget_cost_no_entry_that_stays(torch, d, fp8):
+    dc = DrawnCache([400, 400, 400, 400, 399, 150], 2, d, 16, seed=d, fp8=fp8)
+    rng = np.random.default_rng(3)
+    _set(dc, 1, weight=rng.choice([0.0, np.nan, -np.inf, 1.0], (2, 400)))
+    _set(dc, 2, weight=np.full((2, 400), np.nan))
+    _set(dc, 4, pos=rng.permutation(800)[:399][None].repeat(2, 0))
+    # below the budget, behind it, across it (entries 192 to 207), all below it, the last page
+    lost = [[0, 3, 20], [5, 12, 13, 24], [1], list(range(13)), [2, 12, 24], []]
+    assert _check_with_lost_pages(torch, dc, lost, 200, 30) > 0
