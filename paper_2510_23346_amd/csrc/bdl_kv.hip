@@ -1,4 +1,6 @@
 // Key-value cache of decoder serving: append and eviction (gfx950, wave64).
+#include <type_traits>
+
 #include "bdl_kv_device.h"
 
 namespace bdl {
@@ -181,6 +183,7 @@ struct EvictLds {
     int wave[2][kEW];
     unsigned digit, need, same;
     int last, lost;         // largest position; entries below the budget whose page is none
+    int holes;              // whether there are such pages at all
 };
 
 // exclusive prefix sum over the workgroup; total in *total
@@ -199,9 +202,37 @@ __device__ __forceinline__ long long four_at(const KvCache& c, int b, int h, int
     return kv_entry(c, b, h, 4 * g);
 }
 
+// Pages of a sequence of n entries, and a thread's share of them
+__device__ __forceinline__ int pages_of(const KvCache& c, int n) { return (n + (1 << c.ps_shift) - 1) >> c.ps_shift; }
+__device__ __forceinline__ int page_share(const KvCache& c, int n) { return (pages_of(c, n) + kET - 1) / kET; }
+__device__ __forceinline__ bool page_there(const KvCache& c, int b, int page) {
+    return (unsigned)c.table[(long long)b * c.tstride + page] < (unsigned)c.n_pages;
+}
+
+// The lists of moves (the places, then the sources: 2 moves in all) that LDS
+// does not hold lie in a.scratch, element x in the place of the sequence's x-th
+// entry.  Where page numbers are none, these are passed over (at least 2 moves
+// entries are there): L.freed then has how many pages are there before each
+// thread's share
+__device__ __forceinline__ long long list_past_holes(const KvCache& c, int b, int h, int n, int x, const EvictLds& L) {
+    int t = 0, left = x >> c.ps_shift;
+#pragma unroll 1
+    for (int step = kET / 2; step; step /= 2)
+        if (L.freed[t + step] <= left) t += step;
+    left -= L.freed[t];
+    const int share = page_share(c, n), end = min(pages_of(c, n), (t + 1) * share);
+    int page = t * share;
+#pragma unroll 1
+    for (; page < end; ++page)
+        if (page_there(c, b, page) && left-- == 0) break;
+    return page < end ? kv_entry(c, b, h, (page << c.ps_shift) + (x & ((1 << c.ps_shift) - 1))) : -1;
+}
+
 // R groups of a thread in registers; with MORE the next ones in LDS, and what
-// is left is read again each time
-template <int R, bool MORE>
+// is left is read again each time.  Returns how many entries move; -1 where the
+// row names pages that are none, which only the form with HOLES can deal with
+// (one form for both costs every call 0.3 to 0.7 us)
+template <int R, bool MORE, bool HOLES>
 __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int n, EvictLds& L, uint4* keys) {
     constexpr int U = 4;                // groups whose loads are in flight at once, behind the first R
     const int tid = threadIdx.x, M = a.budget, groups = (n + 3) / 4;
@@ -223,9 +254,13 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     int4 p[R];
     bool there[R];
     int last = INT_MIN, lost = 0;
+    bool hole = false;
     auto top = [&](int k, const int4& pp, bool ok) __attribute__((always_inline)) {
         const int i = 4 * k;
-        if (!ok) lost += max(0, min(4, min(mine, M - 4 * g0) - i));
+        if (!ok && i < mine) {
+            hole = true;
+            lost += max(0, min(4, min(mine, M - 4 * g0) - i));
+        }
         if (i < mine) last = max(last, pp.x);
         if (i + 1 < mine) last = max(last, pp.y);
         if (i + 2 < mine) last = max(last, pp.z);
@@ -248,7 +283,7 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     for (int i = tid; i < 2048; i += kET) L.hist[i] = 0;
     if (tid == 0) {
         L.last = INT_MIN;
-        L.lost = 0;
+        L.lost = L.holes = 0;
     }
 #pragma unroll
     for (int k = 0; k < R; ++k) there[k] = get(k, w[k], p[k]);
@@ -260,15 +295,17 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     for (int x = 32; x; x >>= 1) last = max(last, __shfl_xor(last, x));
     __syncthreads();
     if ((tid & 63) == 0) atomicMax(&L.last, last);
-    if (lost) atomicAdd(&L.lost, lost);
+    if (HOLES && lost) atomicAdd(&L.lost, lost);
+    if (hole) L.holes = 1;
     __syncthreads();
+    if (!HOLES && L.holes) return -1;
     // as many stay as there are places for below the budget: no fewer entries
     // are there, since those from the budget on are n - M or fewer
-    const int room = M - L.lost;
-    if (room == 0) return 0;
+    const int room = HOLES ? M - L.lost : M;
+    if (HOLES && room == 0) return 0;
     const long long floor_ = (long long)L.last - a.recent;
     auto key4 = [&](const float4& ww, const int4& pp, bool ok) __attribute__((always_inline)) {
-        if (!ok) return uint4{0, 0, 0, 0};
+        if (HOLES && !ok) return uint4{0, 0, 0, 0};
         return uint4{kv_key(ww.x, pp.x > floor_), kv_key(ww.y, pp.y > floor_), kv_key(ww.z, pp.z > floor_), kv_key(ww.w, pp.w > floor_)};
     };
     uint4 key[R];
@@ -366,7 +403,7 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
     int eq = all_same ? INT_MIN / 2 : eq0, fr = 0, mv = 0;
     each([&](int i, unsigned k) __attribute__((always_inline)) {
         const bool kept = k > known || (k == known && eq++ < (int)need);
-        fr += i < M && !kept && k;
+        fr += i < M && !kept && (!HOLES || k);
         mv += i >= M && kept;
     });
     // (both counts in one scan where they fit 16 bits)
@@ -382,19 +419,37 @@ __device__ __forceinline__ int kv_select(const KvEvictArgs& a, int b, int h, int
         mv = block_scan(mv, &total, L.wave[0]);
     }
     eq = all_same ? INT_MIN / 2 : eq0;
-    const bool in_lds = moves <= kListCap;
-    each([&](int i, unsigned k) __attribute__((always_inline)) {
+    // (half of the entries at most)
+    const bool in_lds = (!MORE && 2 * R * kET <= kListCap) || moves <= kListCap;
+    auto put = [&](int i, unsigned k, auto place) __attribute__((always_inline)) {
         const bool kept = k > known || (k == known && eq++ < (int)need);
-        const bool f = i < M && !kept && k, m = i >= M && kept;
+        const bool f = i < M && !kept && (!HOLES || k), m = i >= M && kept;
         if (!f && !m) return;
         const int at = f ? fr++ : mv++;
         if (in_lds) {
             (f ? L.freed : L.moved)[at] = i;
         } else {
-            const long long e = kv_entry(a.c, b, h, f ? at : M + at);
+            const long long e = place(f ? at : moves + at);
             if (e >= 0) a.scratch[e] = i;
         }
-    });
+    };
+    if (!HOLES || in_lds) {
+        each([&](int i, unsigned k) __attribute__((always_inline)) { put(i, k, [&](int x) { return kv_entry(a.c, b, h, x); }); });
+        return moves;
+    }
+    // (an entry at a time from memory: nothing but a wrong page table comes here)
+    const int share = page_share(a.c, n), p0 = tid * share, p1 = min(pages_of(a.c, n), p0 + share);
+    int pages = 0;
+#pragma unroll 1
+    for (int j = p0; j < p1; ++j) pages += page_there(a.c, b, j);
+    __syncthreads();
+    L.freed[tid] = block_scan(pages, &total, L.wave[0]);
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 4 * g0; i < 4 * g0 + mine; ++i) {
+        const long long e = kv_entry(a.c, b, h, i);
+        put(i, e < 0 ? 0u : kv_key(a.c.weight[e], a.c.pos[e] > floor_), [&](int x) { return list_past_holes(a.c, b, h, n, x, L); });
+    }
     return moves;
 }
 
@@ -413,11 +468,15 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
     }
     int moves;
     if (!LONG || n <= kFewEntries)
-        moves = kv_select<kFewGroups, false>(a, b, h, n, L, keys);
+        moves = kv_select<kFewGroups, false, false>(a, b, h, n, L, keys);
     else if (n <= kRegEntries)
-        moves = kv_select<kRegGroups, false>(a, b, h, n, L, keys);
+        moves = kv_select<kRegGroups, false, false>(a, b, h, n, L, keys);
     else
-        moves = kv_select<kFewGroups, true>(a, b, h, n, L, keys);
+        moves = kv_select<kFewGroups, true, false>(a, b, h, n, L, keys);
+    if (moves < 0) {
+        __syncthreads();
+        moves = kv_select<kFewGroups, LONG, true>(a, b, h, n, L, keys);
+    }
     // this workgroup has read what it needs of weights, positions and lengths
     __syncthreads();
     const bool alone = Z == 1;              // of its head
@@ -435,15 +494,19 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
             a.lens[b] = M;
         }
     }
-    const bool in_lds = moves <= kListCap;
-    // place and source of move k, as entries of all pages; false where a page is none
-    auto move = [&](int k, long long& to, long long& from) __attribute__((always_inline)) {
+    const bool in_lds = !LONG || moves <= kListCap;
+    // place and source of move k, as entries of all pages; false where a page is
+    // none.  (past_holes: a list in memory of a row that names such pages)
+    auto move = [&](auto past_holes, int k, long long& to, long long& from) __attribute__((always_inline)) {
         int i, j;
-        if (in_lds) {
+        if (!past_holes.value && in_lds) {
             i = L.freed[k];
             j = L.moved[k];
         } else {
-            const long long ef = kv_entry(a.c, b, h, k), em = kv_entry(a.c, b, h, M + k);
+            auto at = [&](int x) __attribute__((always_inline)) {
+                return past_holes.value ? list_past_holes(a.c, b, h, n, x, L) : kv_entry(a.c, b, h, x);
+            };
+            const long long ef = at(k), em = at(moves + k);
             if (ef < 0 || em < 0) return false;
             i = a.scratch[ef];
             j = a.scratch[em];
@@ -454,46 +517,60 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
     };
     // keys and values: LPR lanes a row, four moves in flight (and weights and
     // positions, where no other workgroup is still to read them)
-    constexpr int LPR = ROW / 16, RPP = kET / LPR, U = 4;
+    constexpr int LPR = ROW / 16, RPP = kET / LPR;
     const int k1 = (int)((long long)moves * (z + 1) / Z), c = threadIdx.x % LPR * 16;
-    for (int k0 = (int)((long long)moves * z / Z) + threadIdx.x / LPR; k0 < k1; k0 += U * RPP) {
-        long long to[U], from[U];
-        bool ok[U];
-        u32x4 x[U], y[U];
-        float w[U];
-        int p[U];
+    auto rows = [&](auto past_holes) __attribute__((always_inline)) {
+        constexpr int U = decltype(past_holes)::value ? 1 : 4;
+        for (int k0 = (int)((long long)moves * z / Z) + threadIdx.x / LPR; k0 < k1; k0 += U * RPP) {
+            long long to[U], from[U];
+            bool ok[U];
+            u32x4 x[U], y[U];
+            float w[U];
+            int p[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) ok[u] = k0 + u * RPP < k1 && move(k0 + u * RPP, to[u], from[u]);
+            for (int u = 0; u < U; ++u) ok[u] = k0 + u * RPP < k1 && move(past_holes, k0 + u * RPP, to[u], from[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (ok[u]) {
-                x[u] = *reinterpret_cast<const u32x4*>(a.c.K + from[u] * ROW + c);
-                y[u] = *reinterpret_cast<const u32x4*>(a.c.V + from[u] * ROW + c);
-                if (alone && c == 0) {
-                    w[u] = a.c.weight[from[u]];
-                    p[u] = a.c.pos[from[u]];
+            for (int u = 0; u < U; ++u)
+                if (ok[u]) {
+                    x[u] = *reinterpret_cast<const u32x4*>(a.c.K + from[u] * ROW + c);
+                    y[u] = *reinterpret_cast<const u32x4*>(a.c.V + from[u] * ROW + c);
+                    if (alone && c == 0) {
+                        w[u] = a.c.weight[from[u]];
+                        p[u] = a.c.pos[from[u]];
+                    }
                 }
-            }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (ok[u]) {
-                *reinterpret_cast<u32x4*>(a.c.K + to[u] * ROW + c) = x[u];
-                *reinterpret_cast<u32x4*>(a.c.V + to[u] * ROW + c) = y[u];
-                if (alone && c == 0) {
-                    a.c.weight[to[u]] = w[u];
-                    a.c.pos[to[u]] = p[u];
+            for (int u = 0; u < U; ++u)
+                if (ok[u]) {
+                    *reinterpret_cast<u32x4*>(a.c.K + to[u] * ROW + c) = x[u];
+                    *reinterpret_cast<u32x4*>(a.c.V + to[u] * ROW + c) = y[u];
+                    if (alone && c == 0) {
+                        a.c.weight[to[u]] = w[u];
+                        a.c.pos[to[u]] = p[u];
+                    }
                 }
-            }
-    }
+        }
+    };
+    const bool holes = !in_lds && L.holes;
+    if (holes)
+        rows(std::true_type{});
+    else
+        rows(std::false_type{});
     if (alone) return;
     __syncthreads();
-    if (last_head)
+    auto weights = [&](auto past_holes) __attribute__((always_inline)) {
         for (int k = threadIdx.x; k < moves; k += kET) {
             long long to, from;
-            if (!move(k, to, from)) continue;
+            if (!move(past_holes, k, to, from)) continue;
             a.c.weight[to] = a.c.weight[from];
             a.c.pos[to] = a.c.pos[from];
         }
+    };
+    if (!last_head) return;
+    if (holes)
+        weights(std::true_type{});
+    else
+        weights(std::false_type{});
 }
 
 }  // namespace

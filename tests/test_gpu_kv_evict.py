@@ -265,3 +265,16 @@ def test_pages_lost_below_the_budget_cost_no_entry_that_stays(torch, d, fp8):
     # below the budget, behind it, across it (entries 192 to 207), all below it, the last page
     lost = [[0, 3, 20], [5, 12, 13, 24], [1], list(range(13)), [2, 12, 24], []]
     assert _check_with_lost_pages(torch, dc, lost, 200, 30) > 0
+
+
+@pytest.mark.parametrize("n,budget", [(12000, 6000), (20000, 10000), (30000, 11000), (50000, 20000)])
+def test_pages_lost_where_the_moves_are_listed_in_memory(torch, n, budget):
+    """More moves than LDS lists, keys in registers, in LDS and read again."""
+    dc = DrawnCache([n, n - 1, 20, n], 1, 64, 16, seed=n)
+    rng = np.random.default_rng(n)
+    _set(dc, 1, weight=rng.integers(0, 3, (1, n - 1)))
+    # all the weight lies behind the budget: every place below it is filled
+    _set(dc, 3, weight=np.where(np.arange(n) < budget, 0.0, 1.0) + rng.random(n) / 2)
+    pages = -(-n // 16)
+    lost = [[0, 1, 77, budget // 16, pages - 1], sorted(rng.choice(pages, pages // 8, replace=False)), [], [0, pages - 2]]
+    assert _check_with_lost_pages(torch, dc, lost, budget, 100) > 4096
