@@ -17,11 +17,25 @@ from . import KV_BF16, KV_FP8_E4M3, KVDesc, _check, lib
 __all__ = ["KVCache", "kv_bytes"]
 
 
+def _int32(name: str, v) -> int:
+    """``v`` as the C ABI's int32 takes it (ctypes would cut it to 32 bits)."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name} = {v} does not fit 32 bits")
+    return v
+
+
+def _desc(n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, fmt, k_scale=1.0, v_scale=1.0) -> KVDesc:
+    return KVDesc(_int32("n_q_heads", n_q_heads), _int32("n_kv_heads", n_kv_heads), _int32("head_dim", head_dim),
+                  _int32("page_size", page_size), _int32("n_pages", n_pages), _int32("max_seqs", max_seqs), _int32("fmt", fmt),
+                  float(k_scale), float(v_scale))
+
+
 def kv_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, max_seqs: int, *,
              fmt: int = KV_BF16, weights: bool = False) -> Tuple[int, int]:
     """Bytes of one page (k and v; with ``weights`` weight and pos too) and of
     a cache's workspace (pure host)."""
-    d = KVDesc(int(n_q_heads), int(n_kv_heads), int(head_dim), int(page_size), int(n_pages), int(max_seqs), int(fmt), 1.0, 1.0)
+    d = _desc(n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, fmt)
     a, b = _c.c_int64(), _c.c_int64()
     _check(lib().bdlora_kv_bytes(_c.byref(d), int(weights), _c.byref(a), _c.byref(b)))
     return a.value, b.value
@@ -47,11 +61,10 @@ class KVCache:
                  k=None, v=None, weight=None, pos=None):
         import torch
         self._h = None
-        self.n_q_heads, self.n_kv_heads, self.head_dim = int(n_q_heads), int(n_kv_heads), int(head_dim)
-        self.n_pages, self.page_size, self.max_seqs, self.fmt = int(n_pages), int(page_size), int(max_seqs), int(fmt)
-        self.device = int(device)
-        d = KVDesc(self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, self.max_seqs, self.fmt,
-                   float(k_scale), float(v_scale))
+        d = _desc(n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, fmt, k_scale, v_scale)
+        self.n_q_heads, self.n_kv_heads, self.head_dim = d.n_q_heads, d.n_kv_heads, d.head_dim
+        self.n_pages, self.page_size, self.max_seqs, self.fmt = d.n_pages, d.page_size, d.max_seqs, d.format
+        self.device = _int32("device", device)
         _check(lib().bdlora_kv_bytes(_c.byref(d), 0, None, None))       # refuses a bad description before any allocation
         self._bf16, self._i32, self._f32 = torch.bfloat16, torch.int32, torch.float32
         shape = (self.n_pages, self.n_kv_heads, self.page_size)
@@ -184,7 +197,8 @@ class KVCache:
         the last ``recent`` positions stay, then the largest weights; kept
         entries from behind the budget move into the freed places."""
         tp, ts, tw, B = self._table(table)
-        rc = self._evict(self._h, B, tp, ts, tw, self._ints("lens", lens, B), int(budget), int(recent), self._stream(stream))
+        rc = self._evict(self._h, B, tp, ts, tw, self._ints("lens", lens, B), _int32("budget", budget),
+                         _int32("recent", recent), self._stream(stream))
         if rc:
             _check(rc)
 

@@ -278,3 +278,14 @@ def test_pages_lost_where_the_moves_are_listed_in_memory(torch, n, budget):
     pages = -(-n // 16)
     lost = [[0, 1, 77, budget // 16, pages - 1], sorted(rng.choice(pages, pages // 8, replace=False)), [], [0, pages - 2]]
     assert _check_with_lost_pages(torch, dc, lost, budget, 100) > 4096
+
+
+def test_budgets_that_32_bits_do_not_hold_are_refused(torch):
+    dc = DrawnCache([20, 30], 1, 64, 16, seed=7)
+    cache, table, lens = dc.device()
+    for f in (lambda: cache.evict(table, lens, 2 ** 32 + 5), lambda: cache.evict(table, lens, 5, 2 ** 32 + 1),
+              lambda: cache.evict(table, lens, 2 ** 31), lambda: cache.evict(table, lens, -2 ** 32 + 5)):
+        with pytest.raises(ValueError):
+            f()
+    assert lens.tolist() == [20, 30]
+    cache.close()

@@ -48,3 +48,11 @@ def test_sizes():
     assert pagew == page + 8 * 64 and wsw - ws >= 4 * 4 * 64 * 1000
     with pytest.raises(bd.BDLoRAError):
         bd.kv_bytes(4, 1, 80, 64, 1000, 64)
+
+
+@pytest.mark.parametrize("at", range(6))
+def test_sizes_that_32_bits_do_not_hold_are_refused(at):
+    good = [4, 1, 128, 64, 1000, 64]
+    for big in (2 ** 32 + good[at], 2 ** 31, -2 ** 32 + good[at]):
+        with pytest.raises(ValueError):
+            bd.kv_bytes(*good[:at], big, *good[at + 1:])
