@@ -527,8 +527,8 @@ int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_b
  * query part of qkv itself).  Token t becomes entry index[t] of table row
  * seqs[t] (0..n_seqs - 1; -1: it is not stored, its query is rotated all the
  * same), with weight 0 and pos positions[t]; lens (int32 [n_seqs], may be
- * null, and not the memory of index): lens[seqs[t]] = max(lens[seqs[t]],
- * index[t] + 1).  No two tokens of a call may become the same entry.  A token whose position is outside the
+ * null, and not the memory of seqs, index or positions, which are still read
+ * while it changes): lens[seqs[t]] = max(lens[seqs[t]], index[t] + 1).  No two tokens of a call may become the same entry.  A token whose position is outside the
  * tables is not stored and its query row is zero.  Strides: multiples of 8;
  * qkv, q_out, cos, sin 16-byte aligned.
  * Errors: INVALID_ARG, SHAPE, HIP. */

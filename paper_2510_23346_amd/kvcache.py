@@ -156,19 +156,25 @@ class KVCache:
         """Rotate the queries and keys of ``qkv [T, (n_q_heads + 2
         n_kv_heads) head_dim]`` (the qkv projection's output), store keys and
         values as entries ``index`` of table rows ``seqs`` (-1: not stored),
-        raise ``lens`` (may be None) to cover them, and write the rotated
-        queries to ``q_out`` (it may be qkv's own query columns).  ``cos`` and
-        ``sin``: fp32 ``[positions, head_dim / 2]``."""
+        raise ``lens`` (may be None; not the memory of the other integers,
+        which are still read while it changes) to cover them, and write the
+        rotated queries to ``q_out`` (it may be qkv's own query columns).
+        ``cos`` and ``sin``: fp32 ``[positions, head_dim / 2]``."""
         T = qkv.shape[0]
         qs = self._rows("qkv", qkv, T, self._qkvw)
         os_ = self._rows("q_out", q_out, T, self._qw)
         P = cos.shape[0]
         angles = (P, self.head_dim // 2)
         tp, ts, tw, n = self._table(table)
+        ps, pi, pp = self._ints("seqs", seqs, T), self._ints("index", index, T), self._ints("positions", positions, T)
+        pl = None
+        if lens is not None:
+            pl = self._ints("lens", lens, n)
+            end, size = pl + 4 * n, 4 * T
+            if (pl < ps + size and ps < end) or (pl < pi + size and pi < end) or (pl < pp + size and pp < end):
+                raise ValueError("lens must not share memory with seqs, index or positions")
         rc = self._append(self._h, qkv.data_ptr(), qs, self._floats("cos", cos, angles), self._floats("sin", sin, angles), P,
-                          int(interleaved), self._ints("seqs", seqs, T), self._ints("index", index, T),
-                          self._ints("positions", positions, T), T, tp, ts, tw, n,
-                          None if lens is None else self._ints("lens", lens, n), q_out.data_ptr(), os_, self._stream(stream))
+                          int(interleaved), ps, pi, pp, T, tp, ts, tw, n, pl, q_out.data_ptr(), os_, self._stream(stream))
         if rc:
             _check(rc)
 

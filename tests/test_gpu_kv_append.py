@@ -251,3 +251,26 @@ def test_refusals(torch):
     cache.append(**(ok | {"lens": None}))
     assert lens.tolist() == [4, 4]
     cache.close()
+
+
+def test_lens_apart_from_the_integers_that_are_read_beside_it(torch):
+    """index and positions of a decode step are the lengths: copies of them."""
+    dc = DrawnCache([4, 4], 1, 64, 16, seed=3, room=1)
+    cache, table, lens = dc.device(n_q_heads=2)
+    qkv, q_out = (torch.zeros(2, n, dtype=torch.bfloat16, device="cuda") for n in (256, 128))
+    c, s = (torch.from_numpy(x).cuda() for x in _tables(64, 8))
+    both = torch.zeros(4, dtype=torch.int32, device="cuda")
+    both[:2] = lens
+    lens, after, across = both[:2], both[2:], both[1:3]
+    i = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    ok = dict(qkv=qkv, cos=c, sin=s, seqs=i, index=lens.clone(), positions=lens.clone(), table=table, lens=lens, q_out=q_out)
+    for name in ("seqs", "index", "positions"):
+        for x in (lens, across):
+            with pytest.raises(ValueError):
+                cache.append(**(ok | {name: x}))
+    assert lens.tolist() == [4, 4]
+    cache.append(**(ok | {"positions": after}))
+    assert lens.tolist() == [5, 5] and cache.device_error() == 0
+    cache.append(**(ok | {"index": lens, "positions": lens, "lens": None}))         # not written: may be the same
+    assert lens.tolist() == [5, 5]
+    cache.close()
