@@ -180,20 +180,23 @@ class KVCache:
 
     def attend(self, q, table, lens, out, starts=None, scale=None, lse=None, accumulate: bool = False, stream=None):
         """Attention of row b of ``q [B, n_q_heads head_dim]`` over entries
-        ``starts[b]`` (0) to ``lens[b]`` of table row b, into ``out``;
-        ``scale`` defaults to ``head_dim ** -0.5``.  ``lse``: fp32 ``[B,
-        n_q_heads]``, receives the log of the sum of the scores'
-        exponentials.  ``accumulate`` adds the entries' probabilities to
-        ``weight``."""
+        ``starts[b]`` (0) to ``lens[b]`` of table row b, into ``out`` (not
+        q's memory: several workgroups read a query); ``scale`` defaults to
+        ``head_dim ** -0.5``.  ``lse``: fp32 ``[B, n_q_heads]``, receives the
+        log of the sum of the scores' exponentials.  ``accumulate`` adds the
+        entries' probabilities to ``weight``."""
         B = q.shape[0]
         qs = self._rows("q", q, B, self._qw)
         os_ = self._rows("out", out, B, self._qw)
         tp, ts, tw, n = self._table(table)
         if n < B:
             raise ValueError(f"table has {n} rows for {B} sequences")
-        rc = self._attend(self._h, q.data_ptr(), qs, B, tp, ts, tw, self._ints("lens", lens, B),
+        qp, op = q.data_ptr(), out.data_ptr()
+        if qp == op and B:
+            raise ValueError("out must not be q's memory")
+        rc = self._attend(self._h, qp, qs, B, tp, ts, tw, self._ints("lens", lens, B),
                           None if starts is None else self._ints("starts", starts, B),
-                          self._scale if scale is None else scale, int(accumulate), out.data_ptr(), os_,
+                          self._scale if scale is None else scale, int(accumulate), op, os_,
                           None if lse is None else self._floats("lse", lse, (B, self.n_q_heads)), self._stream(stream))
         if rc:
             _check(rc)

@@ -473,3 +473,20 @@ def test_many_query_heads_over_long_sequences(torch, hq, hkv, d, fp8):
         assert torch.equal(out.view(torch.int16), runs[0][0].view(torch.int16)) and torch.equal(lse, runs[0][1])
     assert cache.device_error() == 0
     cache.close()
+
+
+def test_out_apart_from_the_queries(torch):
+    dc = DrawnCache([20, 30], 1, 64, 16, seed=17)
+    cache, table, dl = dc.device(n_q_heads=4, weights=False)
+    q, _ = _queries(torch, 2, 4, 64, seed=1)
+    same = q.clone()
+    with pytest.raises(ValueError):
+        cache.attend(q, table, dl, q)
+    assert torch.equal(q.view(torch.int16), same.view(torch.int16))
+    rows = torch.zeros(2, 512, dtype=torch.bfloat16, device="cuda")
+    rows[:, :256] = q
+    cache.attend(rows[:, :256], table, dl, rows[:, 256:])              # columns of the same rows
+    out = torch.empty_like(q)
+    cache.attend(q, table, dl, out)
+    assert torch.equal(rows[:, 256:].contiguous().view(torch.int16), out.view(torch.int16))
+    cache.close()
