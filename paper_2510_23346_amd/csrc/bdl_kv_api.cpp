@@ -18,7 +18,6 @@ struct bdlora_kv {
     float* weight = nullptr;
     int* pos = nullptr;
     char* ws = nullptr;            // the workspace, one allocation
-    long long bytes = 0;
     int* err = nullptr;
     int n_cu = 0;
     float* lse2 = nullptr;         // [max_seqs][n_q_heads]
@@ -185,7 +184,6 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
         c->weight = weight;
         c->pos = pos;
         c->ws = ws;
-        c->bytes = p.total;
         c->err = (int*)(ws + p.err);
         c->n_cu = std::max(1, prop.multiProcessorCount);
         c->count = (unsigned*)(ws + p.count);
