@@ -7,7 +7,8 @@ every request names its own adapter: the qkv projection (Pool.forward_shard),
 the rotary embedding and entry into the cache (KVCache.append), attention over
 the cache (KVCache.attend) and the o projection, whose output is the shard's
 partial of the tensor-parallel sum.  With a budget the steps keep account of
-the attention that every entry gets and evict what got least.  The step is
+the attention that every entry gets and evict what got least (a prompt's
+entries begin with none: its own attention is not computed here).  The step is
 captured once into a HIP graph and replayed.  Weights, adapters and
 activations are random, the shapes those of the Llama models.
 """

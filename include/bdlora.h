@@ -456,9 +456,9 @@ int bdlora_last_path(bdlora_pool_t pool, int32_t* path);
  *     weight, pos:  [n_pages][n_kv_heads][page_size], fp32 and int32
  * A sequence's entries 0 .. len - 1 lie in the pages that its row of the page
  * table names: entry i in place i mod page_size of page table[row][i /
- * page_size].  Places of a row from ceil(len / page_size) on are never read,
- * and what pages hold from entry len on, or before the first entry attended
- * to, affects no result (it may be anything, NaN as well).  Page tables, and
+ * page_size].  What a row holds from place ceil(len / page_size) on, and what
+ * pages hold from entry len on, or before the first entry attended to, affects
+ * no result (it may be anything: numbers that name no page, NaN).  Page tables, and
  * lens, starts, seqs, index and positions, are int32 device arrays: calls can
  * be captured in a HIP graph and replayed over changed contents.
  *
@@ -471,7 +471,9 @@ int bdlora_last_path(bdlora_pool_t pool, int32_t* path);
  * token's position.  A cache without them (both null) attends but does not
  * accumulate or evict.  A page may be named by several sequences (a shared
  * prefix) where it is only attended to; a call that accumulates, appends or
- * evicts writes pages, which only one of its sequences may name.
+ * evicts writes pages, which only one of its sequences may name.  New entries
+ * have weight 0, and only attend adds to it: entries that nothing attended to
+ * yet (a prompt's, unless the caller sets their weights) rank by their order.
  *
  * Device-side errors (a page number outside 0 .. n_pages - 1 under an entry
  * that is used, a length or index beyond the table's row, a position outside

@@ -17,8 +17,8 @@ namespace {
 // token, those whose pairs it needs: two 16-byte loads, two 16-byte stores (8
 // bytes each into an 8-bit cache).  A workgroup's threads are units x tokens
 // (x, y), so that no index needs a division by the number of heads.
-// Measured: 64 tokens of 4 + 1 + 1 heads of 128 4.2 us, of which an empty
-// kernel takes 3.0; 4288 tokens of 8 + 1 + 1 heads into an 8-bit cache 8.3 us,
+// Measured: 64 tokens of 4 + 1 + 1 heads of 128 4.1 us, of which an empty
+// kernel takes 3.0; 4288 tokens of 8 + 1 + 1 heads into an 8-bit cache 8.5 us,
 // 21 MB read and written.
 __device__ __forceinline__ void unpack8(u32x4 v, float (&x)[8]) {
 #pragma unroll
@@ -154,13 +154,14 @@ hipError_t append(const KvAppendArgs& a, hipStream_t s) {
 // kept in registers (up to 24576 entries of a sequence), or the first 8192 there
 // and 28672 more in LDS, and what is left is read again in each pass.
 //
-// Measured: 64 sequences from 2049 to 2048 entries 9.8 us, of which 2 are the
+// Measured: 64 sequences from 2049 to 2048 entries 9.7 us, of which 2 are the
 // way to lengths, pages and weights, 1.1 to 1.5 each pass, 1.3 the places and 1
-// the one row that moves: a chain of waits, 64 workgroups.  8 sequences of two
-// kv heads from 8192 to 2048 18.3 us, 10 of them the same chain over four
+// the one row that moves: a chain of waits, 64 workgroups, and all of it the
+// general selection, though one entry is looked for.  8 sequences of two
+// kv heads from 8192 to 2048 18.2 us, 10 of them the same chain over four
 // times the entries and 5 the 25 MB that move.
-// One of 16384 to 4096 23 us, of 32768 42; of 131072 to 8192 234, most of it the
-// keys read again in each pass, a thread's at a time.
+// One of 16384 to 4096 23 us, of 32768 43, of 65536 92; of 131072 to 8192 237,
+// most of it the keys read again in each pass, a thread's at a time.
 constexpr int kET = 1024, kEW = kET / 64;
 constexpr int kFewGroups = 2, kRegGroups = 6, kLdsGroups = 7;      // groups of four entries a thread keeps
 constexpr int kFewEntries = 4 * kFewGroups * kET, kRegEntries = 4 * kRegGroups * kET;
@@ -593,9 +594,13 @@ void evict(const KvEvictArgs& a, const dim3& grid, bool many, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_kv_evict(const KvEvictArgs& a, int head_dim, bool fp8, hipStream_t s) {
-    // a workgroup per compute unit, and no more of a head than its moves could
-    // feed.  (Up to 256 moves: one; the counting that several need costs what
-    // they save, 11.1 against 12.4 us at 236 moves, and 15.1 against 15.7 at 1024)
+    // a workgroup per compute unit, and no more of a head than the moves could
+    // feed that a row of this width allows.  (Up to 256 moves: one; the counting
+    // that several need costs what they save, 11.1 against 12.4 us at 236 moves,
+    // and 15.1 against 15.7 at 1024.  Lengths are not known here: where rows are
+    // wider than their sequences, few moves get several workgroups all the same:
+    // 64 sequences from 2049 to 2048 take 11.9 us in rows of 2064 entries, 13.1 to
+    // 13.4 in rows of 8192 to 131072)
     const long long heads = (long long)a.B * a.c.hkv, cap = (long long)a.c.width << a.c.ps_shift;
     const long long most = std::min<long long>(a.budget, std::max(0LL, cap - a.budget));
     const int z = most <= 256 ? 1 : (int)std::max(1LL, std::min({a.n_cu / heads, (most + 63) / 64, 64LL}));

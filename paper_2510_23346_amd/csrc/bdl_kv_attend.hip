@@ -25,12 +25,14 @@
 // operands; between waves nothing is waited for until the end.
 //
 // Measured, one launch: 305 MB of keys and values in bf16 (256 sequences of up
-// to 4353 entries, 8 query heads of 128 on one kv head) 63.5 us, 4.8 TB/s; 134 MB of
-// one sequence of 131072 33.6 us; 72 MB of 64 sequences 20.8 us, in 8 bits
-// 21.6 us; one sequence of 509 entries 8.6 us.  Without joining anything the
-// 72 MB take 16.7 us: what is over the copy's rate there is the wait for the
-// last wave's loads, the pieces in LDS (1.3 us), their way through memory
-// (1 us) and the sum of the shares (1.3 to 2 us).
+// to 4353 entries, 8 query heads of 128 on one kv head) 63.9 us, 4.8 TB/s; 134 MB of
+// one sequence of 131072 34.4 us; 72 MB of 64 sequences 21.2 us, in 8 bits
+// 22.3 us; one sequence of 509 entries 8.6 us.  What is over the copy's rate in
+// the 72 MB is the join (pieces in LDS, their way through memory, the sum of the
+// shares: 4 us) and that stretches are whole tiles: 4440 tiles on 2048 waves
+// are 2.2 a wave, but 3 for a sixth of them, and a tile of one entry counts
+// like a full one.  (The third matrix instruction of the second product: 0.1 to
+// 0.5 us.)
 #include "bdl_kv_device.h"
 
 namespace bdl {
@@ -765,7 +767,9 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
 // above.  A launch of its own, since a sequence's sum is known only when its last
 // workgroup has joined it; it reads 4 G + 8 bytes an entry, 3 MB for 32
 // sequences of 2049 entries and two kv heads: 5.5 us, of which 3 are any
-// launch's.  (The workgroup that finishes a sequence could add its weights: 6.6
+// launch's.  Bound by waits, one after the other: the lengths, the page number,
+// then lse and score of each head in turn, in the end the weight itself (2 G + 3
+// trips to memory).  (The workgroup that finishes a sequence could add its weights: 6.6
 // against 10.5 us where a wave has a sequence to itself, but 29.4 against
 // 26.8 us at 32 of 2049 entries and 101 against 19 at one of 32768, which one
 // workgroup then reads alone.)
