@@ -477,7 +477,7 @@ int bdlora_last_path(bdlora_pool_t pool, int32_t* path);
  *
  * Device-side errors (a page number outside 0 .. n_pages - 1 under an entry
  * that is used, a length or index beyond the table's row, a position outside
- * the tables, a seq outside the table) raise the cache's sticky error flag
+ * the tables, a seq outside the table, rows that are not ascending) raise the cache's sticky error flag
  * (bdlora_kv_get_device_error); nothing outside the arrays is read or
  * written: the entry counts as not there, the length is cut to what the row
  * can name, the token is not stored.
@@ -492,10 +492,27 @@ typedef struct bdlora_kv* bdlora_kv_t;
 #define BDLORA_KV_BF16     0
 #define BDLORA_KV_FP8_E4M3 1
 
+/* Or 8-bit integers with a scale for each block of BDLORA_KV_BLOCK entries of a
+ * kv head (entries 16 i .. 16 i + 15 of a page), which an array of the caller's
+ * holds beside k and v:
+ *     scales:       [n_pages][n_kv_heads][page_size / 16][2], fp32: K's, V's
+ * An entry's number stands for itself times its block's scale.  append sets the
+ * scale of a block that it writes into to
+ *     s = max(m, 2^-64) / 127,  m = the largest magnitude in the call's rows of the block,
+ * or to max(s, the scale before) where the block's first entry is not among
+ * them, and stores rint(x / s) (both as products with the fp32 reciprocal).
+ * Where the scale grows the entries that were there are rounded again, by up to
+ * half a step each time.  The scales of a block whose first entry was never
+ * appended must be valid (0 where it is new).  A block that has been given an
+ * infinity or NaN stands for NaN, all of it.  Such a cache tracks no weights (it
+ * does not accumulate or evict). */
+#define BDLORA_KV_INT8_BLOCK 3
+#define BDLORA_KV_BLOCK      16
+
 /* n_q_heads: 1..1024, a multiple of n_kv_heads (the shard's own heads).
  * head_dim: 64 or 128.  page_size: a power of two, 16..65536.  max_seqs:
- * 1..65535, the most sequences of a call.  k_scale, v_scale: positive (1 for
- * a bf16 cache). */
+ * 1..65535, the most sequences of a call.  k_scale, v_scale: positive (1
+ * but for an e4m3 cache). */
 typedef struct {
     int32_t n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs;
     int32_t format;
@@ -509,10 +526,14 @@ typedef struct {
 int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight, int32_t* pos, int32_t device,
                      bdlora_kv_t* out);
 
+/* The same for a cache of BDLORA_KV_INT8_BLOCK, with its array of scales (8-byte
+ * aligned). */
+int bdlora_kv_create_blocks(const bdlora_kv_desc* desc, void* k, void* v, float* scales, int32_t device, bdlora_kv_t* out);
+
 /* Free the workspace (waits for the device's work). */
 int bdlora_kv_destroy(bdlora_kv_t cache);
 
-/* Bytes of one page (k and v, with `weights` weight and pos too) and of the
+/* Bytes of one page (k and v and a block cache's scales, with `weights` weight and pos too) and of the
  * workspace.  Pure host function; either pointer may be null. */
 int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_bytes, int64_t* workspace_bytes);
 
@@ -530,7 +551,9 @@ int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_b
  * seqs[t] (0..n_seqs - 1; -1: it is not stored, its query is rotated all the
  * same), with weight 0 and pos positions[t]; lens (int32 [n_seqs], may be
  * null, and not the memory of seqs, index or positions, which are still read
- * while it changes): lens[seqs[t]] = max(lens[seqs[t]], index[t] + 1).  No two tokens of a call may become the same entry.  A token whose position is outside the
+ * while it changes): lens[seqs[t]] = max(lens[seqs[t]], index[t] + 1).  No two tokens of a call may become the same entry.  (Cache with a scale for
+ * each block: those of one sequence that become entries of one block stand one
+ * after the other in the call, by ascending entry.)  A token whose position is outside the
  * tables is not stored and its query row is zero.  Strides: multiples of 8;
  * qkv, q_out, cos, sin 16-byte aligned.
  * Errors: INVALID_ARG, SHAPE, HIP. */
@@ -538,6 +561,28 @@ int bdlora_kv_append(bdlora_kv_t cache, const void* qkv, int64_t qkv_stride, con
                      int32_t n_positions, int32_t interleaved, const int32_t* seqs, const int32_t* index,
                      const int32_t* positions, int32_t T, const int32_t* table, int64_t table_stride, int32_t table_width,
                      int32_t n_seqs, int32_t* lens, void* q_out, int64_t q_stride, void* stream);
+
+/* The same with a norm of every query and key head before its rotation:
+ *     x <- x (1 / sqrt(mean x^2 + eps)) w
+ * over the head's head_dim numbers, in fp32, each step rounded by itself, and
+ * rounded no further before the rotation (squares that pass the range of fp32
+ * give zeros).  q_norm, k_norm: w, device bf16 [head_dim], 16-byte aligned;
+ * eps >= 0.  Errors: INVALID_ARG, SHAPE, HIP. */
+int bdlora_kv_append_norm(bdlora_kv_t cache, const void* qkv, int64_t qkv_stride, const void* q_norm, const void* k_norm,
+                          float eps, const float* cos, const float* sin, int32_t n_positions, int32_t interleaved,
+                          const int32_t* seqs, const int32_t* index, const int32_t* positions, int32_t T, const int32_t* table,
+                          int64_t table_stride, int32_t table_width, int32_t n_seqs, int32_t* lens, void* q_out,
+                          int64_t q_stride, void* stream);
+
+/* Entries read back: row t of k_out and v_out (bf16 [T], kv heads side by side,
+ * strides multiples of 8, 16-byte aligned) is entry index[t] of table row
+ * seqs[t], in any order: the number that it stands for, rounded to bf16.  -1 in
+ * seqs, and what names no entry of a row (error flag), gives zeros; lengths are
+ * not looked at.  k_out and v_out must not overlap each other or what the call
+ * reads.  Errors: INVALID_ARG, SHAPE, HIP. */
+int bdlora_kv_read(bdlora_kv_t cache, const int32_t* seqs, const int32_t* index, int32_t T, const int32_t* table,
+                   int64_t table_stride, int32_t table_width, int32_t n_seqs, void* k_out, int64_t k_stride, void* v_out,
+                   int64_t v_stride, void* stream);
 
 /* Attention of one new token for each of B sequences (0..max_seqs): row b of
  * q (bf16, rows q_stride elements apart, heads side by side) over entries
@@ -555,6 +600,29 @@ int bdlora_kv_append(bdlora_kv_t cache, const void* qkv, int64_t qkv_stride, con
 int bdlora_kv_attend(bdlora_kv_t cache, const void* q, int64_t q_stride, int32_t B, const int32_t* table,
                      int64_t table_stride, int32_t table_width, const int32_t* lens, const int32_t* starts, float scale,
                      int32_t accumulate, void* out, int64_t out_stride, float* lse, void* stream);
+
+/* The same where the first `sinks` >= 0 entries stay visible beside a window:
+ * entries j < sinks and those from starts[b] on, each once.  (starts null: all
+ * entries, whatever sinks.) */
+int bdlora_kv_attend_sinks(bdlora_kv_t cache, const void* q, int64_t q_stride, int32_t B, const int32_t* table,
+                           int64_t table_stride, int32_t table_width, const int32_t* lens, const int32_t* starts, int32_t sinks,
+                           float scale, int32_t accumulate, void* out, int64_t out_stride, float* lse, void* stream);
+
+/* Attention of many new tokens of each sequence, whose keys and values have been
+ * appended: a prompt, a chunk of one, drafted tokens, single tokens among them.
+ * Rows q_starts[b] .. q_starts[b + 1] - 1 of q (int32 device [B + 1], ascending,
+ * within 0..T; 0 <= B <= max_seqs) are the last entries of table row b in order:
+ * the last of them is entry lens[b] - 1.  The row of entry p attends to
+ *     entries j <= p with window = 0, or j > p - window, or j < sinks,
+ * and out, lse are as in bdlora_kv_attend, rows of `out` as those of q (they must
+ * not overlap).  A row without an entry of its own (more rows than entries: error
+ * flag) gives 0 and lse -infinity; rows of no sequence are left as they are.
+ * Probabilities enter the sum over values as bf16 (8 significant bits), their
+ * sum and lse do not.  Nothing is accumulated.  T x n_q_heads <= 2^30.
+ * Errors: INVALID_ARG, SHAPE, HIP. */
+int bdlora_kv_attend_prompt(bdlora_kv_t cache, const void* q, int64_t q_stride, int32_t T, const int32_t* q_starts, int32_t B,
+                            const int32_t* table, int64_t table_stride, int32_t table_width, const int32_t* lens, int32_t window,
+                            int32_t sinks, float scale, void* out, int64_t out_stride, float* lse, void* stream);
 
 /* Cut each of B sequences (table rows 0..B - 1) to at most `budget` >= 1
  * entries, in place, for each kv head by itself: first in rank are the

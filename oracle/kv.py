@@ -84,3 +84,60 @@ def evict_plan(weight, pos, budget, recent):
 
     kept = set(sorted(range(n), key=rank)[:budget])
     return [i for i in range(budget) if i not in kept], [i for i in range(budget, n) if i in kept]
+
+
+def sees(n, new, window=0, sinks=0):
+    """Which of n entries the tokens of the last `new` of them attend to:
+    ``[new, n]`` truth values."""
+    p = np.arange(n - new, n)[:, None]
+    j = np.arange(n)[None, :]
+    seen = j <= p
+    if window:
+        seen &= (j > p - window) | (j < sinks)
+    return seen
+
+
+def attend_rows(q, k, v, scale, seen):
+    """Many tokens: ``q [T, n_q_heads, d]``, ``seen [T, n]``.  Returns out, lse
+    and sum p |v|, the size that errors of the probabilities go by."""
+    T, hq, _ = q.shape
+    hkv, n, dv = v.shape
+    out, mag = np.zeros((T, hq, dv)), np.zeros((T, hq, dv))
+    lse = np.full((T, hq), -np.inf)
+    some = seen.any(1)
+    for h in range(hq):
+        g = h // (hq // hkv)
+        s = np.where(seen, scale * (q[:, h] @ k[g].T), -np.inf)[some]
+        top = s.max(1, keepdims=True) if s.size else np.zeros((0, 1))
+        p = np.exp(s - top)
+        total = p.sum(1, keepdims=True)
+        lse[some, h] = (top + np.log(total))[:, 0]
+        out[some, h] = (p / total) @ v[g]
+        mag[some, h] = (p / total) @ np.abs(v[g])
+    return out, lse, mag
+
+
+def head_norm(x, w, eps):
+    """Rows ``x [..., d]`` over the root of their mean square, times w."""
+    x = np.asarray(x, np.float64)
+    return x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * np.asarray(w, np.float64)
+
+
+def int8_blocks(stored, scales, rows, index, dtype=np.float32):
+    """Entries ``index`` (ascending) of one head of one sequence become ``rows
+    [T, d]``: ``stored [n, d]`` integers and ``scales [n / 16]``, n a multiple of
+    16, are changed in place, the arithmetic in ``dtype``."""
+    f = dtype
+    rows = np.asarray(rows, f)
+    index = np.asarray(index)
+    for b in np.unique(index // 16):
+        mine = index // 16 == b
+        s = f(max(np.abs(rows[mine]).max(), f(2.0 ** -64)) * (f(1) / f(127)))
+        at = slice(16 * b, 16 * b + 16)
+        if not (index[mine] % 16 == 0).any():
+            before = f(scales[b])
+            s = max(s, before)
+            if s != before:
+                stored[at] = np.clip(np.rint(stored[at].astype(f) * (before / s)), -127, 127)
+        scales[b] = s
+        stored[index[mine]] = np.clip(np.rint(rows[mine] * (f(1) / s)), -127, 127)

@@ -21,7 +21,7 @@ __all__ = [
     "DECODE_PLAN_IN_MAIN_BYTES", "decode_plans_in_main",
     "ACT_NONE", "ACT_SILU_MUL", "WEIGHT_BF16", "WEIGHT_INT4_G128", "pack_weight_int4",
     "packed_weight_bytes", "MAX_SEGMENTS", "Segments", "layout_slot_bytes", "pack_adapter_layout",
-    "KVCache", "KVDesc", "KV_BF16", "KV_FP8_E4M3", "kv_bytes",
+    "KVCache", "KVDesc", "KV_BF16", "KV_FP8_E4M3", "KV_INT8", "KV_BLOCK", "kv_bytes",
 ]
 
 COLUMN, ROW = 0, 1
@@ -43,7 +43,8 @@ ACT_NONE, ACT_SILU_MUL = 0, 1   # BDLORA_ACT_*: activation between the MLP's pro
 # BDLORA_PATH_*: launch sequence of a forward (0: none yet)
 PATHS = {0: "", 1: "decode", 2: "tile64", 3: "medium", 4: "large"}
 WEIGHT_BF16, WEIGHT_INT4_G128 = 0, 1   # BDLORA_WEIGHT_*: base weight formats
-KV_BF16, KV_FP8_E4M3 = 0, 1   # BDLORA_KV_*: key-value cache formats
+KV_BF16, KV_FP8_E4M3, KV_INT8 = 0, 1, 3   # BDLORA_KV_*: key-value cache formats (KV_INT8: BDLORA_KV_INT8_BLOCK)
+KV_BLOCK = 16           # BDLORA_KV_BLOCK: entries of a head that share the scales of an int8 cache
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libbdlora.so")
 _LIB = None
@@ -107,9 +108,15 @@ _SIGS = {
     "bdlora_profile_end": (_I, [_P, _c.POINTER(_c.c_float), _IP]),
     "bdlora_last_path": (_I, [_P, _IP]),
     "bdlora_kv_create": (_I, [_c.POINTER(KVDesc), _P, _P, _P, _P, _I, _c.POINTER(_P)]),
+    "bdlora_kv_create_blocks": (_I, [_c.POINTER(KVDesc), _P, _P, _P, _I, _c.POINTER(_P)]),
     "bdlora_kv_destroy": (_I, [_P]),
     "bdlora_kv_bytes": (_I, [_c.POINTER(KVDesc), _I, _LP, _LP]),
     "bdlora_kv_append": (_I, [_P, _P, _L, _P, _P, _I, _I, _P, _P, _P, _I, _P, _L, _I, _I, _P, _P, _L, _P]),
+    "bdlora_kv_append_norm": (_I, [_P, _P, _L, _P, _P, _c.c_float, _P, _P, _I, _I, _P, _P, _P, _I, _P, _L, _I, _I, _P, _P, _L,
+                                   _P]),
+    "bdlora_kv_read": (_I, [_P, _P, _P, _I, _P, _L, _I, _I, _P, _L, _P, _L, _P]),
+    "bdlora_kv_attend_sinks": (_I, [_P, _P, _L, _I, _P, _L, _I, _P, _P, _I, _c.c_float, _I, _P, _L, _P, _P]),
+    "bdlora_kv_attend_prompt": (_I, [_P, _P, _L, _I, _P, _I, _P, _L, _I, _P, _I, _I, _c.c_float, _P, _L, _P, _P]),
     "bdlora_kv_attend": (_I, [_P, _P, _L, _I, _P, _L, _I, _P, _P, _c.c_float, _I, _P, _L, _P, _P]),
     "bdlora_kv_evict": (_I, [_P, _I, _P, _L, _I, _P, _I, _I, _P]),
     "bdlora_kv_get_device_error": (_I, [_P, _P, _IP]),

@@ -21,7 +21,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libbdlora.so")
 
 SOURCES = ["bdl_prep.hip", "bdl_decode.hip", "bdl_kernels.hip", "bdl_gemm.hip", "bdl_static.hip", "bdl_api.cpp",
-           "bdl_kv.hip", "bdl_kv_attend.hip", "bdl_kv_api.cpp"]
+           "bdl_kv.hip", "bdl_kv_store.hip", "bdl_kv_attend.hip", "bdl_kv_prompt.hip", "bdl_kv_api.cpp", "bdl_kv_rows_api.cpp"]
 ARCH = "gfx950"
 
 

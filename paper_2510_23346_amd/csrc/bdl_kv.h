@@ -14,6 +14,7 @@ int api_fail(int code, const std::string& msg);
 
 constexpr int kKvMaxHeads = 1024;      // query heads
 constexpr int kKvMinPage = 16, kKvMaxPage = 65536;
+constexpr int kKvBlock = 16;           // entries of a head that share the scales of an int8 cache
 
 // attend: the most workgroups of a launch, heads a workgroup takes at once,
 // and what one leaves for a sequence that it shares with others: unnormalised
@@ -34,6 +35,7 @@ struct KvCache {
     char *K, *V;
     float* weight;
     int* pos;
+    float* scales;        // int8 caches: [n_pages][hkv][page / kKvBlock][2], of K and of V
     int hq, hkv, ps_shift, n_pages;
     const int* table;     // [rows][tstride], `width` pages of a row used
     int tstride, width;
@@ -50,7 +52,18 @@ struct KvAppendArgs {
     const int *seqs, *index, *positions;
     int* lens;            // may be null
     int T, n_seqs;
-    float k_inv, v_inv;   // 8-bit cache: 1 / scale
+    float k_inv, v_inv;   // e4m3 cache: 1 / scale
+    const uint16_t *q_norm, *k_norm;   // [head size] each; null: no norm
+    float eps;
+};
+
+struct KvReadArgs {
+    KvCache c;
+    const int *seqs, *index;
+    int T, n_seqs;
+    uint16_t *k_out, *v_out;
+    long long k_stride, v_stride;
+    float k_scale, v_scale;
 };
 
 struct KvAttendArgs {
@@ -60,6 +73,7 @@ struct KvAttendArgs {
     long long q_stride, out_stride;
     const int *lens, *starts;
     int has_starts;             // 0: starts is there to be read, and means nothing
+    int sinks;                  // first entries that are attended to before starts
     float* lse;                 // may be null
     int B;
     float* part;                // [2 kKvAttendGrid][kv_part_floats(D)]
@@ -79,8 +93,27 @@ struct KvEvictArgs {
     unsigned* count;      // B hkv counters, then B: zero between calls
 };
 
+// Attention of many new tokens of each sequence
+struct KvPromptArgs {
+    KvCache c;
+    const uint16_t* q;
+    uint16_t* out;
+    long long q_stride, out_stride;
+    const int *q_starts, *lens;
+    float* lse;                 // may be null
+    int T, B, window, sinks;    // window 0: none
+    float score_scale;          // as above
+    unsigned q_sign;
+    float v_scale;
+};
+
+// (fp8: the cache is e4m3; one with scales is int8, else bf16)
 hipError_t launch_kv_append(const KvAppendArgs& a, int head_dim, bool fp8, hipStream_t s);
+// into an int8 cache
+hipError_t launch_kv_store(const KvAppendArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_kv_attend(const KvAttendArgs& a, int head_dim, bool fp8, bool accumulate, hipStream_t s);
+hipError_t launch_kv_read(const KvReadArgs& a, int head_dim, bool fp8, hipStream_t s);
+hipError_t launch_kv_prompt(const KvPromptArgs& a, int head_dim, bool fp8, hipStream_t s);
 hipError_t launch_kv_evict(const KvEvictArgs& a, int head_dim, bool fp8, hipStream_t s);
 
 }  // namespace bdl

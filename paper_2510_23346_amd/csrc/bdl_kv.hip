@@ -20,21 +20,6 @@ namespace {
 // Measured: 64 tokens of 4 + 1 + 1 heads of 128 4.1 us, of which an empty
 // kernel takes 3.0; 4288 tokens of 8 + 1 + 1 heads into an 8-bit cache 8.5 us,
 // 21 MB read and written.
-__device__ __forceinline__ void unpack8(u32x4 v, float (&x)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(v[i] << 16);
-        x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-    }
-}
-
-__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
-    u32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pk_bf16(x[2 * i], x[2 * i + 1]);
-    return v;
-}
-
 __device__ __forceinline__ uint2 pack8_e4m3(const float (&x)[8], float inv) {
     uint32_t w[2];
 #pragma unroll
@@ -48,8 +33,12 @@ __device__ __forceinline__ uint2 pack8_e4m3(const float (&x)[8], float inv) {
     return uint2{w[0], w[1]};
 }
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
+// With norms (NORM) a query or key is first taken times 1 / sqrt(mean x^2 + eps)
+// and its weight, in fp32 and not rounded before the rotation.  The threads of a
+// head (4 or 8 neighbours in a wave) add their squares by exchanges, in an
+// order that depends on nothing.
+template <int D, bool FP8, bool NORM>
+__device__ __forceinline__ void append(const KvAppendArgs& a) {
 #pragma clang fp contract(off)
     const int t = blockIdx.x * blockDim.y + threadIdx.y, u = blockIdx.y * blockDim.x + threadIdx.x;
     const int H = a.c.hq + 2 * a.c.hkv, h = u / (D / 16), j = u % (D / 16);
@@ -64,33 +53,13 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
     float y0[8], y1[8];
     unpack8(x0, y0);
     unpack8(x1, y1);
+    if (NORM && !v) {
+        const uint16_t* const w = h < a.c.hq ? a.q_norm : a.k_norm;
+        const u32x4 w0 = ld16(w + d0), w1 = ld16(w + d1);
+        head_norm<D>(y0, y1, w0, w1, a.eps);
+    }
     if (!v) {
-        const long long at = (long long)(pos_ok ? pos : 0) * (D / 2) + 8 * j;
-        float c[8], s[8];
-#pragma unroll
-        for (int k = 0; k < 8; k += 4) {
-            const float4 cc = *reinterpret_cast<const float4*>(a.cos + at + k), ss = *reinterpret_cast<const float4*>(a.sin + at + k);
-            c[k] = cc.x, c[k + 1] = cc.y, c[k + 2] = cc.z, c[k + 3] = cc.w;
-            s[k] = ss.x, s[k + 1] = ss.y, s[k + 2] = ss.z, s[k + 3] = ss.w;
-        }
-        if (a.interleaved) {
-            // pairs (2k, 2k + 1): y0 holds pairs 0..3, y1 pairs 4..7
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float a0 = y0[2 * k], b0 = y0[2 * k + 1], a1 = y1[2 * k], b1 = y1[2 * k + 1];
-                y0[2 * k] = a0 * c[k] - b0 * s[k];
-                y0[2 * k + 1] = b0 * c[k] + a0 * s[k];
-                y1[2 * k] = a1 * c[k + 4] - b1 * s[k + 4];
-                y1[2 * k + 1] = b1 * c[k + 4] + a1 * s[k + 4];
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float a0 = y0[k], b0 = y1[k];
-                y0[k] = a0 * c[k] - b0 * s[k];
-                y1[k] = b0 * c[k] + a0 * s[k];
-            }
-        }
+        rotate16(y0, y1, a.cos, a.sin, (long long)(pos_ok ? pos : 0) * (D / 2) + 8 * j, a.interleaved);
         if (!pos_ok)
 #pragma unroll
             for (int k = 0; k < 8; ++k) y0[k] = y1[k] = 0.f;
@@ -134,9 +103,23 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
 }
 
 template <int D, bool FP8>
+__global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
+    append<D, FP8, false>(a);
+}
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(256) void kv_append_norm_kernel(const KvAppendArgs a) {
+    append<D, FP8, true>(a);
+}
+
+template <int D, bool FP8>
 hipError_t append(const KvAppendArgs& a, hipStream_t s) {
     const int units = (a.c.hq + 2 * a.c.hkv) * (D / 16), x = std::min(units, 256), y = 256 / x;
-    kv_append_kernel<D, FP8><<<dim3((a.T + y - 1) / y, (units + x - 1) / x), dim3(x, y), 0, s>>>(a);
+    const dim3 grid((a.T + y - 1) / y, (units + x - 1) / x), block(x, y);
+    if (a.q_norm)
+        kv_append_norm_kernel<D, FP8><<<grid, block, 0, s>>>(a);
+    else
+        kv_append_kernel<D, FP8><<<grid, block, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -577,6 +560,7 @@ __global__ __launch_bounds__(kET) void kv_evict_kernel(const KvEvictArgs a) {
 }  // namespace
 
 hipError_t launch_kv_append(const KvAppendArgs& a, int head_dim, bool fp8, hipStream_t s) {
+    if (a.c.scales) return launch_kv_store(a, head_dim, s);
     if (head_dim == 64) return fp8 ? append<64, true>(a, s) : append<64, false>(a, s);
     return fp8 ? append<128, true>(a, s) : append<128, false>(a, s);
 }

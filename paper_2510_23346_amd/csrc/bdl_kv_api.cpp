@@ -1,64 +1,7 @@
 // C ABI of the key-value cache: validation, workspace and launches.
-#include "bdlora.h"
-
-#include <hip/hip_runtime.h>
-
-#include <algorithm>
-#include <cmath>
-#include <cstring>
-#include <exception>
-#include <string>
-
-#include "bdl_kv.h"
-
-struct bdlora_kv {
-    int device = 0;
-    bdlora_kv_desc d;
-    char *k = nullptr, *v = nullptr;
-    float* weight = nullptr;
-    int* pos = nullptr;
-    char* ws = nullptr;            // the workspace, one allocation
-    int* err = nullptr;
-    int n_cu = 0;
-    float* lse2 = nullptr;         // [max_seqs][n_q_heads]
-    float* part = nullptr;         // attend's shares of sequences
-    unsigned* count = nullptr;     // kKvAttendCounts counters
-    float* logits = nullptr;       // [n_pages][n_q_heads][page_size]
-    unsigned* evict_count = nullptr;   // [max_seqs][n_kv_heads + 1] counters
-    int* scratch = nullptr;        // [n_pages][n_kv_heads][page_size], where logits lie too
-};
+#include "bdl_kv_cache.h"
 
 namespace {
-
-using bdl::api_fail;
-
-// the thread's current device for the length of a call
-struct Device {
-    int old = -1;
-    bool ok = false;
-    explicit Device(int dev) { ok = hipGetDevice(&old) == hipSuccess && (old == dev || hipSetDevice(dev) == hipSuccess); dev_ = dev; }
-    ~Device() {
-        if (old >= 0 && old != dev_) (void)hipSetDevice(old);
-    }
-    int dev_;
-};
-
-int hip_fail(const char* what, hipError_t e) {
-    (void)hipGetLastError();
-    return api_fail(e == hipErrorOutOfMemory ? BDLORA_ERR_OOM : BDLORA_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
-
-// no C++ exception (an allocation of a message's string) leaves the C ABI
-template <class F>
-int guarded(F f) noexcept {
-    try {
-        return f();
-    } catch (...) {
-        return BDLORA_ERR_OOM;
-    }
-}
-
-bool aligned(const void* p, unsigned n) { return ((uintptr_t)p & (n - 1u)) == 0; }
 
 int check_desc(const bdlora_kv_desc* d) {
     if (!d) return api_fail(BDLORA_ERR_INVALID_ARG, "null description");
@@ -69,13 +12,13 @@ int check_desc(const bdlora_kv_desc* d) {
         return api_fail(BDLORA_ERR_SHAPE, "page_size must be a power of two, 16..65536");
     if (d->n_pages < 1) return api_fail(BDLORA_ERR_INVALID_ARG, "n_pages must be positive");
     if (d->max_seqs < 1 || d->max_seqs > 65535) return api_fail(BDLORA_ERR_INVALID_ARG, "max_seqs must be 1..65535");
-    if (d->format != BDLORA_KV_BF16 && d->format != BDLORA_KV_FP8_E4M3)
+    if (d->format != BDLORA_KV_BF16 && d->format != BDLORA_KV_FP8_E4M3 && d->format != BDLORA_KV_INT8_BLOCK)
         return api_fail(BDLORA_ERR_INVALID_ARG, "unknown cache format");
     if (!(d->k_scale > 0.f && d->v_scale > 0.f) || !std::isfinite(d->k_scale) || !std::isfinite(d->v_scale) ||
         !std::isfinite(1.f / d->k_scale) || !std::isfinite(1.f / d->v_scale))
         return api_fail(BDLORA_ERR_INVALID_ARG, "k_scale and v_scale must be positive and finite, and so their reciprocals");
-    if (d->format == BDLORA_KV_BF16 && (d->k_scale != 1.f || d->v_scale != 1.f))
-        return api_fail(BDLORA_ERR_INVALID_ARG, "a bf16 cache has scales of 1");
+    if (d->format != BDLORA_KV_FP8_E4M3 && (d->k_scale != 1.f || d->v_scale != 1.f))
+        return api_fail(BDLORA_ERR_INVALID_ARG, "a bf16 cache, and one with a scale for each block, has k_scale and v_scale of 1");
     return BDLORA_OK;
 }
 
@@ -102,49 +45,15 @@ Parts layout(const bdlora_kv_desc& d, bool weights) {
     return p;
 }
 
-int check_table(const bdlora_kv* c, const int32_t* table, int64_t stride, int32_t width) {
-    if (!table || !aligned(table, 4)) return api_fail(BDLORA_ERR_INVALID_ARG, "null or misaligned page table");
-    if (width < 1 || stride < width || stride > INT32_MAX) return api_fail(BDLORA_ERR_INVALID_ARG, "a page table row needs 1 <= width <= stride");
-    if (((long long)width * c->d.page_size) > (1LL << 30))
-        return api_fail(BDLORA_ERR_SHAPE, "a page table row may name at most 2^30 entries");
-    return BDLORA_OK;
-}
-
-// rows of bf16 values that the kernels take in 16-byte pieces
-int check_rows(const void* p, int64_t stride, long long row, const char* name) {
-    if (!p || !aligned(p, 16)) return api_fail(BDLORA_ERR_INVALID_ARG, std::string(name) + " must be 16-byte aligned");
-    if (stride < row || stride % 8 || stride > (1LL << 31))
-        return api_fail(BDLORA_ERR_INVALID_ARG, std::string(name) + " needs a row stride of at least its row, a multiple of 8 elements");
-    return BDLORA_OK;
-}
-
-bdl::KvCache view(const bdlora_kv* c, const int32_t* table, int64_t stride, int32_t width) {
-    bdl::KvCache v;
-    v.K = c->k;
-    v.V = c->v;
-    v.weight = c->weight;
-    v.pos = c->pos;
-    v.hq = c->d.n_q_heads;
-    v.hkv = c->d.n_kv_heads;
-    v.ps_shift = __builtin_ctz((unsigned)c->d.page_size);
-    v.n_pages = c->d.n_pages;
-    v.table = table;
-    v.tstride = (int)stride;
-    v.width = width;
-    v.err = c->err;
-    return v;
-}
-
-}  // namespace
-
-extern "C" {
-
-int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight, int32_t* pos, int32_t device,
-                     bdlora_kv_t* out) {
+int create(const bdlora_kv_desc* desc, void* k, void* v, float* scales, float* weight, int32_t* pos, int32_t device,
+           bdlora_kv_t* out) {
     return guarded([&]() -> int {
         if (!out) return api_fail(BDLORA_ERR_INVALID_ARG, "null output handle");
         *out = nullptr;
         if (int rc = check_desc(desc)) return rc;
+        if ((desc->format == BDLORA_KV_INT8_BLOCK) != (scales != nullptr))
+            return api_fail(BDLORA_ERR_INVALID_ARG, "a cache with a scale for each block, and no other, is made with its array of scales");
+        if (!aligned(scales, 8)) return api_fail(BDLORA_ERR_INVALID_ARG, "scales must be 8-byte aligned device memory");
         if (!k || !v || !aligned(k, 16) || !aligned(v, 16))
             return api_fail(BDLORA_ERR_INVALID_ARG, "k and v must be 16-byte aligned device memory");
         if ((weight == nullptr) != (pos == nullptr))
@@ -183,6 +92,7 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
         c->v = (char*)v;
         c->weight = weight;
         c->pos = pos;
+        c->scales = scales;
         c->ws = ws;
         c->err = (int*)(ws + p.err);
         c->n_cu = std::max(1, prop.multiProcessorCount);
@@ -197,32 +107,10 @@ int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight
     });
 }
 
-int bdlora_kv_destroy(bdlora_kv_t c) {
-    return guarded([&]() -> int {
-        if (!c) return api_fail(BDLORA_ERR_INVALID_ARG, "null cache");
-        Device guard(c->device);
-        (void)hipDeviceSynchronize();
-        (void)hipFree(c->ws);
-        delete c;
-        return BDLORA_OK;
-    });
-}
-
-int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_bytes, int64_t* workspace_bytes) {
-    return guarded([&]() -> int {
-        if (int rc = check_desc(desc)) return rc;
-        const long long size = desc->format == BDLORA_KV_BF16 ? 2 : 1;
-        if (page_bytes)
-            *page_bytes = (2LL * desc->head_dim * size + (weights ? 8 : 0)) * desc->n_kv_heads * desc->page_size;
-        if (workspace_bytes) *workspace_bytes = layout(*desc, weights != 0).total;
-        return BDLORA_OK;
-    });
-}
-
-int bdlora_kv_append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const float* cos, const float* sin,
-                     int32_t n_positions, int32_t interleaved, const int32_t* seqs, const int32_t* index,
-                     const int32_t* positions, int32_t T, const int32_t* table, int64_t table_stride, int32_t table_width,
-                     int32_t n_seqs, int32_t* lens, void* q_out, int64_t q_stride, void* stream) {
+int append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const void* q_norm, const void* k_norm, float eps, const float* cos,
+           const float* sin, int32_t n_positions, int32_t interleaved, const int32_t* seqs, const int32_t* index,
+           const int32_t* positions, int32_t T, const int32_t* table, int64_t table_stride, int32_t table_width,
+           int32_t n_seqs, int32_t* lens, void* q_out, int64_t q_stride, void* stream) {
     return guarded([&]() -> int {
         if (!c) return api_fail(BDLORA_ERR_INVALID_ARG, "null cache");
         if (T < 0) return api_fail(BDLORA_ERR_INVALID_ARG, "negative T");
@@ -234,6 +122,12 @@ int bdlora_kv_append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const f
             return api_fail(BDLORA_ERR_INVALID_ARG, "cos and sin must be 16-byte aligned, of at least one position");
         if (!seqs || !index || !positions || !aligned(seqs, 4) || !aligned(index, 4) || !aligned(positions, 4) || !aligned(lens, 4))
             return api_fail(BDLORA_ERR_INVALID_ARG, "seqs, index and positions must be int32 device arrays");
+        if ((q_norm == nullptr) != (k_norm == nullptr))
+            return api_fail(BDLORA_ERR_INVALID_ARG, "q_norm and k_norm come together or not at all");
+        if (!aligned(q_norm, 16) || !aligned(k_norm, 16))
+            return api_fail(BDLORA_ERR_INVALID_ARG, "q_norm and k_norm must be 16-byte aligned");
+        if (q_norm && !(eps >= 0.f && std::isfinite(eps)))
+            return api_fail(BDLORA_ERR_INVALID_ARG, "eps must be finite and not negative");
         if (n_seqs < 1) return api_fail(BDLORA_ERR_INVALID_ARG, "n_seqs must be positive");
         if (int rc = check_table(c, table, table_stride, table_width)) return rc;
         Device guard(c->device);
@@ -254,6 +148,9 @@ int bdlora_kv_append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const f
         a.lens = lens;
         a.T = T;
         a.n_seqs = n_seqs;
+        a.q_norm = (const uint16_t*)q_norm;
+        a.k_norm = (const uint16_t*)k_norm;
+        a.eps = eps;
         a.k_inv = 1.f / c->d.k_scale;
         a.v_inv = 1.f / c->d.v_scale;
         if (hipError_t e = bdl::launch_kv_append(a, c->d.head_dim, c->d.format == BDLORA_KV_FP8_E4M3, (hipStream_t)stream))
@@ -262,14 +159,15 @@ int bdlora_kv_append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const f
     });
 }
 
-int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, const int32_t* table, int64_t table_stride,
-                     int32_t table_width, const int32_t* lens, const int32_t* starts, float scale, int32_t accumulate,
-                     void* out, int64_t out_stride, float* lse, void* stream) {
+int attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, const int32_t* table, int64_t table_stride,
+           int32_t table_width, const int32_t* lens, const int32_t* starts, int32_t sinks, float scale, int32_t accumulate,
+           void* out, int64_t out_stride, float* lse, void* stream) {
     return guarded([&]() -> int {
         if (!c) return api_fail(BDLORA_ERR_INVALID_ARG, "null cache");
         if (B < 0 || B > c->d.max_seqs) return api_fail(BDLORA_ERR_INVALID_ARG, "B must be 0..max_seqs");
         if (accumulate && !c->weight) return api_fail(BDLORA_ERR_INVALID_ARG, "this cache tracks no weights");
         if (!std::isfinite(scale)) return api_fail(BDLORA_ERR_INVALID_ARG, "scale must be finite");
+        if (sinks < 0) return api_fail(BDLORA_ERR_INVALID_ARG, "sinks must not be negative");
         if (B == 0) return BDLORA_OK;
         const long long row = (long long)c->d.n_q_heads * c->d.head_dim;
         if (int rc = check_rows(q, q_stride, row, "q")) return rc;
@@ -279,7 +177,7 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         if (int rc = check_table(c, table, table_stride, table_width)) return rc;
         // (the kernel counts tiles of 32 entries in 32 bits)
         const long long heads = (long long)c->d.n_kv_heads * ((c->d.n_q_heads / c->d.n_kv_heads + bdl::kKvHeads - 1) / bdl::kKvHeads);
-        if (((long long)table_width * c->d.page_size + 63) / 32 * B * heads > INT32_MAX)
+        if (((long long)table_width * c->d.page_size + (sinks ? 127 : 63)) / 32 * B * heads > INT32_MAX)
             return api_fail(BDLORA_ERR_SHAPE, "more than 2^31 tiles: B x kv heads x a row's entries / 32");
         Device guard(c->device);
         if (!guard.ok) return api_fail(BDLORA_ERR_HIP, "hipSetDevice failed");
@@ -292,6 +190,7 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
         a.lens = lens;
         a.starts = starts ? starts : lens;
         a.has_starts = starts != nullptr;
+        a.sinks = starts ? sinks : 0;         // (without a window every entry is attended to)
         a.lse = lse;
         a.B = B;
         a.part = c->part;
@@ -306,6 +205,74 @@ int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, 
             return hip_fail("attend launch", e);
         return BDLORA_OK;
     });
+}
+
+}  // namespace
+
+extern "C" {
+
+int bdlora_kv_create(const bdlora_kv_desc* desc, void* k, void* v, float* weight, int32_t* pos, int32_t device,
+                     bdlora_kv_t* out) {
+    return create(desc, k, v, nullptr, weight, pos, device, out);
+}
+
+int bdlora_kv_create_blocks(const bdlora_kv_desc* desc, void* k, void* v, float* scales, int32_t device, bdlora_kv_t* out) {
+    return create(desc, k, v, scales, nullptr, nullptr, device, out);
+}
+
+int bdlora_kv_destroy(bdlora_kv_t c) {
+    return guarded([&]() -> int {
+        if (!c) return api_fail(BDLORA_ERR_INVALID_ARG, "null cache");
+        Device guard(c->device);
+        (void)hipDeviceSynchronize();
+        (void)hipFree(c->ws);
+        delete c;
+        return BDLORA_OK;
+    });
+}
+
+int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_bytes, int64_t* workspace_bytes) {
+    return guarded([&]() -> int {
+        if (int rc = check_desc(desc)) return rc;
+        if (weights && desc->format == BDLORA_KV_INT8_BLOCK)
+            return api_fail(BDLORA_ERR_INVALID_ARG, "a cache with a scale for each block tracks no weights");
+        const long long size = desc->format == BDLORA_KV_BF16 ? 2 : 1;
+        if (page_bytes)
+            *page_bytes = (2LL * desc->head_dim * size + (weights ? 8 : 0)) * desc->n_kv_heads * desc->page_size +
+                          (desc->format == BDLORA_KV_INT8_BLOCK ? 8LL * desc->n_kv_heads * (desc->page_size / bdl::kKvBlock) : 0);
+        if (workspace_bytes) *workspace_bytes = layout(*desc, weights != 0).total;
+        return BDLORA_OK;
+    });
+}
+
+int bdlora_kv_append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const float* cos, const float* sin,
+                     int32_t n_positions, int32_t interleaved, const int32_t* seqs, const int32_t* index,
+                     const int32_t* positions, int32_t T, const int32_t* table, int64_t table_stride, int32_t table_width,
+                     int32_t n_seqs, int32_t* lens, void* q_out, int64_t q_stride, void* stream) {
+    return append(c, qkv, qkv_stride, nullptr, nullptr, 0.f, cos, sin, n_positions, interleaved, seqs, index, positions, T, table,
+                  table_stride, table_width, n_seqs, lens, q_out, q_stride, stream);
+}
+
+int bdlora_kv_append_norm(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const void* q_norm, const void* k_norm, float eps,
+                          const float* cos, const float* sin, int32_t n_positions, int32_t interleaved, const int32_t* seqs,
+                          const int32_t* index, const int32_t* positions, int32_t T, const int32_t* table, int64_t table_stride,
+                          int32_t table_width, int32_t n_seqs, int32_t* lens, void* q_out, int64_t q_stride, void* stream) {
+    if (!q_norm || !k_norm) return guarded([]() -> int { return api_fail(BDLORA_ERR_INVALID_ARG, "null q_norm or k_norm"); });
+    return append(c, qkv, qkv_stride, q_norm, k_norm, eps, cos, sin, n_positions, interleaved, seqs, index, positions, T, table,
+                  table_stride, table_width, n_seqs, lens, q_out, q_stride, stream);
+}
+
+int bdlora_kv_attend(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, const int32_t* table, int64_t table_stride,
+                     int32_t table_width, const int32_t* lens, const int32_t* starts, float scale, int32_t accumulate,
+                     void* out, int64_t out_stride, float* lse, void* stream) {
+    return attend(c, q, q_stride, B, table, table_stride, table_width, lens, starts, 0, scale, accumulate, out, out_stride, lse, stream);
+}
+
+int bdlora_kv_attend_sinks(bdlora_kv_t c, const void* q, int64_t q_stride, int32_t B, const int32_t* table, int64_t table_stride,
+                           int32_t table_width, const int32_t* lens, const int32_t* starts, int32_t sinks, float scale,
+                           int32_t accumulate, void* out, int64_t out_stride, float* lse, void* stream) {
+    return attend(c, q, q_stride, B, table, table_stride, table_width, lens, starts, sinks, scale, accumulate, out, out_stride, lse,
+                  stream);
 }
 
 int bdlora_kv_evict(bdlora_kv_t c, int32_t B, const int32_t* table, int64_t table_stride, int32_t table_width, int32_t* lens,

@@ -39,17 +39,20 @@ namespace bdl {
 
 namespace {
 
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int NW = 4, NT = NW * 64;     // waves and threads of a workgroup, of which a compute unit holds two
 
 // A sequence: entries first .. len - 1 in tiles that begin at a multiple of 16
 // (an empty one has a tile too, which writes its row)
 struct Seq {
     int len, first;
+    int sinks;        // SINKS: entries 0 .. sinks - 1 too, in tiles of their own before the others; at most first
     unsigned tiles;
     bool bad;         // the given length was none
 };
 
+__device__ __forceinline__ int sink_tiles(int sinks) { return (sinks + 31) >> 5; }
+
+template <bool SINKS>
 __device__ __forceinline__ Seq seq_of(const KvAttendArgs& a, int b) {
     const int at = min(b, a.B - 1), cap = a.c.width << a.c.ps_shift;     // (at most 2^30)
     const int n = a.lens[at], st = a.starts[at];
@@ -57,8 +60,18 @@ __device__ __forceinline__ Seq seq_of(const KvAttendArgs& a, int b) {
     s.len = min(max(n, 0), cap);
     s.bad = s.len != n;
     s.first = a.has_starts ? max(st, 0) : 0;
-    if (s.first >= s.len) s.len = s.first = 0;
-    s.tiles = b < a.B ? max(1u, (unsigned)(s.len - (s.first & ~15) + 31) >> 5) : 0u;
+    s.sinks = 0;
+    if constexpr (SINKS) {
+        s.first = min(s.first, s.len);
+        s.sinks = min(a.sinks, s.first);
+        if (s.sinks == s.first) s.sinks = s.first = 0;             // (no gap behind them)
+        if (s.first == s.len && s.sinks == 0) s.len = s.first = 0;
+        const int rest = s.first < s.len ? (s.len - (s.first & ~15) + 31) >> 5 : 0;
+        s.tiles = b < a.B ? max(1u, (unsigned)(sink_tiles(s.sinks) + rest)) : 0u;
+    } else {
+        if (s.first >= s.len) s.len = s.first = 0;
+        s.tiles = b < a.B ? max(1u, (unsigned)(s.len - (s.first & ~15) + 31) >> 5) : 0u;
+    }
     return s;
 }
 
@@ -77,17 +90,9 @@ struct Line {
     }
 };
 
-__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-
 // What is left of a number without its upper 16 bits, those of two numbers side
 // by side, and the smaller or larger one of each half
 __device__ __forceinline__ float below_bf16(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-
-__device__ __forceinline__ uint32_t upper_halves(float x, float y) {
-    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
-}
 
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
@@ -121,33 +126,6 @@ __device__ __forceinline__ float2 load_through2(__amdgpu_buffer_rsrc_t r, unsign
     return float2{__uint_as_float(v[0]), __uint_as_float(v[1])};
 }
 
-// Where a 16-byte chunk c of row r of a tile lies in LDS: rows of D bf16
-// numbers whose chunks are exchanged within the row so that both the 16-byte
-// reads of keys (16 rows, one chunk each) and the transposing reads of values
-// (8 rows, the two chunks of 16 columns) meet every bank once.
-template <int D>
-__device__ __forceinline__ int k_at(int r, int c) {
-    return r * (D / 8) + (c ^ (D == 128 ? r & 15 : (r >> 1) & 7));
-}
-template <int D>
-__device__ __forceinline__ int v_at(int r, int c) {
-    return r * (D / 8) + (c ^ (D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3)));
-}
-
-// 8 numbers of an 8-bit cache as bf16 (exact)
-__device__ __forceinline__ u32x4 bf16_of(uint32_t a, uint32_t b) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    u32x4 r;
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true));
-    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false));
-    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true));
-    return r;
-}
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
 // A tile: two blocks of 16 entries, each within one page, of one head of one
 // sequence
 struct Tile {
@@ -158,6 +136,7 @@ struct Tile {
     int lo[2], n[2];      // rows lo .. n - 1 of a block are attended to
     int page[2];
     unsigned long long at[2];   // where the blocks begin in K and V, in bytes
+    float ks[2], vs[2];         // int8: their scales
 };
 
 // A share's way through the workspace: up to kDirect shares of a sequence are
@@ -166,9 +145,9 @@ struct Tile {
 // at once, 11.2 in groups; 64: 12.0 and 10.6)
 constexpr unsigned kDirect = 32, kGroup = 16;
 
-template <int D, bool FP8, bool ACC, bool WIDE>
-__global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArgs a) {
-    constexpr int SZ = FP8 ? 1 : 2, ROW = D * SZ;
+template <int D, int FMT, bool ACC, bool WIDE, bool SINKS>
+__device__ __forceinline__ void attend(const KvAttendArgs& a) {
+    constexpr int SZ = FMT == kBf16 ? 2 : 1, ROW = D * SZ;
     constexpr int NL = 16 * ROW / 1024;             // 16-byte loads of a block
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int BUF = 32 * D / 8;                 // 16-byte pieces of a tile in LDS, or of a wave's sums
@@ -191,7 +170,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
     auto look_four = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            four[i] = seq_of(a, c0 + 64 * i + l);
+            four[i] = seq_of<SINKS>(a, c0 + 64 * i + l);
             bad |= four[i].bad;
         }
 #pragma unroll
@@ -201,7 +180,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
         }
     };
     if (a.B <= 64) {
-        four[0] = seq_of(a, l);
+        four[0] = seq_of<SINKS>(a, l);
         bad = four[0].bad;
         incl[0] = (unsigned)wave_incl_scan((int)four[0].tiles);
         total = sum4[0] = (unsigned)wave_total((int)incl[0]);
@@ -232,7 +211,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
 
     // The cursor: the tile whose pages are looked up, two ahead of the one
     // being worked on.  Sequences b0 .. b0 + 63 are in the lanes.
-    int b0 = 0, cb, ch, clen, cfirst;
+    int b0 = 0, cb, ch, clen, cfirst, csinks = 0;
     unsigned ct, ctiles;
     Seq mine;
     unsigned head0;                                 // the first tile of the first sequence and head
@@ -258,6 +237,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
         ctiles = (unsigned)__builtin_amdgcn_readlane((int)mine.tiles, bi);
         clen = __builtin_amdgcn_readlane(mine.len, bi);
         cfirst = __builtin_amdgcn_readlane(mine.first, bi);
+        if (SINKS) csinks = __builtin_amdgcn_readlane(mine.sinks, bi);
         const unsigned off = r0 - seq0;
         unsigned q = 0;
         if (HH > 1) {
@@ -278,11 +258,12 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
         if (++cb >= a.B) --cb;                      // (behind the last tile: never used)
         if (cb - b0 == 64) {
             b0 += 64;
-            mine = seq_of(a, b0 + l);
+            mine = seq_of<SINKS>(a, b0 + l);
         }
         ctiles = (unsigned)__builtin_amdgcn_readlane((int)mine.tiles, cb - b0);
         clen = __builtin_amdgcn_readlane(mine.len, cb - b0);
         cfirst = __builtin_amdgcn_readlane(mine.first, cb - b0);
+        if (SINKS) csinks = __builtin_amdgcn_readlane(mine.sinks, cb - b0);
     };
     // the cursor's tile, its page numbers on their way
     auto look = [&](bool used) __attribute__((always_inline)) {
@@ -294,13 +275,16 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
         x.tiles = ctiles;
         x.first = ct == 0;
         x.last = ct + 1 == ctiles;
-        x.e = (cfirst & ~15) + 32 * (int)ct;
+        const int before = SINKS ? sink_tiles(csinks) : 0;
+        const bool sink = SINKS && (int)ct < before;
+        const int from = sink ? 0 : cfirst, end = sink ? csinks : clen;
+        x.e = (from & ~15) + 32 * ((int)ct - (sink ? 0 : before));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int e = x.e + 16 * j, rows = used ? clen - e : 0;
+            const int e = x.e + 16 * j, rows = used ? end - e : 0;
             x.page[j] = trow[uni(rows > 0 ? e >> psh : 0)];
             x.n[j] = min(16, max(0, rows));
-            x.lo[j] = max(0, cfirst - e);
+            x.lo[j] = max(0, from - e);
         }
         return x;
     };
@@ -318,6 +302,16 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
             if (x.n[j] == 0) x.page[j] = 0;
             x.at[j] = ((unsigned long long)(unsigned)x.page[j] * (page16 * row16) +
                        (((unsigned)kvh << psh) + ((unsigned)(x.e + 16 * j) & pmask)) * row16) * 16;
+            if constexpr (FMT == kInt8) {
+                // (a block is 16 entries of 16 row16 bytes each)
+                const unsigned long long blk = x.at[j] / (16ull * ROW);
+                const unsigned lo = (unsigned)uni((int)(unsigned)blk), hi = (unsigned)uni((int)(unsigned)(blk >> 32));
+                typedef const __attribute__((address_space(4))) float* cfloat;
+                const cfloat sc = (cfloat)(a.c.scales + 2 * ((unsigned long long)hi << 32 | lo));
+                x.ks[j] = sc[0];
+                x.vs[j] = sc[1];
+                if (x.n[j] == 0) x.ks[j] = x.vs[j] = 1.f;
+            }
         }
     };
     u32x4 kr[2][NL], vr[2][NL];
@@ -364,8 +358,9 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
             for (int i = 0; i < NL; ++i) {
                 const int row = i * (64 / LPR) + l / LPR, c = l % LPR, rr = j * 16 + row;
                 const u32x4 v = x[j][i];
-                if constexpr (FP8) {
-                    const u32x4 y0 = bf16_of(v[0], v[1]), y1 = bf16_of(v[2], v[3]);
+                if constexpr (FMT != kBf16) {
+                    const u32x4 y0 = FMT == kFp8 ? bf16_of(v[0], v[1]) : bf16_of_int8(v[0], v[1]);
+                    const u32x4 y1 = FMT == kFp8 ? bf16_of(v[2], v[3]) : bf16_of_int8(v[2], v[3]);
                     buf[value ? v_at<D>(rr, 2 * c) : k_at<D>(rr, 2 * c)] = y0;
                     buf[value ? v_at<D>(rr, 2 * c + 1) : k_at<D>(rr, 2 * c + 1)] = y1;
                 } else {
@@ -439,14 +434,32 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
                 const Heads hd = heads_of(cur.h);
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    if (lr < hd.n && cur.n[j] > 0)
-                        *reinterpret_cast<f32x4*>(a.logits + ((((size_t)cur.page[j] * a.c.hq + hd.hq0 + lr) << psh) +
-                                                              ((cur.e + 16 * j) & pmask) + 4 * lg)) = s[j];
+                    if (lr < hd.n && cur.n[j] > 0) {
+                        float* const at = a.logits + ((((size_t)cur.page[j] * a.c.hq + hd.hq0 + lr) << psh) +
+                                                      ((cur.e + 16 * j) & pmask) + 4 * lg);
+                        // (the last of the sinks and the first behind the gap can
+                        // lie in one block, which two tiles then have a part of)
+                        if (!SINKS || (cur.lo[j] <= 4 * lg && cur.n[j] >= 4 * lg + 4)) {
+                            *reinterpret_cast<f32x4*>(at) = s[j];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (4 * lg + e >= cur.lo[j] && 4 * lg + e < cur.n[j]) at[e] = s[j][e];
+                        }
+                    }
             }
             // the maximum follows only where a score passes it by 8 (in units of
             // log 2): until then no exponential exceeds 2^8
-            float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                              fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * a.score_scale;
+            float scale[2];
+            if constexpr (FMT == kInt8) {
+                scale[0] = a.score_scale * cur.ks[0];
+                scale[1] = a.score_scale * cur.ks[1];
+            } else {
+                scale[0] = scale[1] = a.score_scale;
+            }
+            float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+            const float top1 = fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
+            top = FMT == kInt8 ? fmaxf(top * scale[0], top1 * scale[1]) : fmaxf(top, top1) * scale[0];
             if (__any(top > m + 8.f)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -468,8 +481,9 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
-                    const float x = exp2_(fmaf(s[j][e], a.score_scale, -mm)), y = exp2_(fmaf(s[j][e + 1], a.score_scale, -mm));
+                    float x = exp2_(fmaf(s[j][e], scale[j], -mm)), y = exp2_(fmaf(s[j][e + 1], scale[j], -mm));
                     sum += x + y;
+                    if constexpr (FMT == kInt8) x *= cur.vs[j], y *= cur.vs[j];
                     const float x1 = below_bf16(x), y1 = below_bf16(y);
                     const uint32_t h = upper_halves(x, y), some = min_u16x2(h, 0x00010001u);
                     hi[j * 2 + e / 2] = h;
@@ -773,12 +787,18 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArg
 // against 10.5 us where a wave has a sequence to itself, but 29.4 against
 // 26.8 us at 32 of 2049 entries and 101 against 19 at one of 32768, which one
 // workgroup then reads alone.)
-__global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) {
+template <bool SINKS>
+__device__ __forceinline__ void weigh(const KvAttendArgs& a) {
     const int l = threadIdx.x & 63, G = a.c.hq / a.c.hkv, hkv = a.c.hkv, psh = a.c.ps_shift, pmask = (1 << psh) - 1;
-    auto blocks = [&](const Seq& s) { return (unsigned)(s.len - (s.first & ~15) + 255) >> 8; };
+    // (the sinks' blocks before the others)
+    auto sink_blocks = [&](const Seq& s) { return SINKS ? (unsigned)(s.sinks + 255) >> 8 : 0u; };
+    auto blocks = [&](const Seq& s) {
+        if (SINKS && s.first == s.len) return sink_blocks(s);
+        return sink_blocks(s) + ((unsigned)(s.len - (s.first & ~15) + 255) >> 8);
+    };
     unsigned long long at = 0;              // blocks before sequence b0, all heads
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const Seq mine = seq_of(a, b0 + l);
+        const Seq mine = seq_of<SINKS>(a, b0 + l);
         const unsigned nb = b0 + l < a.B ? blocks(mine) : 0u;
         const unsigned incl = (unsigned)wave_incl_scan((int)nb), total = (unsigned)wave_total((int)incl);
         // this workgroup's blocks: at + x with (at + x) mod gridDim = blockIdx
@@ -790,8 +810,14 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) {
             const unsigned off = (unsigned)(x - (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(incl - nb), bi) * hkv);
             const int h = off / nbb, blk = off - h * nbb, b = b0 + bi;
             const int len = __builtin_amdgcn_readlane(mine.len, bi), first = __builtin_amdgcn_readlane(mine.first, bi);
-            const long long e = (first & ~15) + 256LL * blk + threadIdx.x;
-            if (e >= first && e < len) {
+            long long e = (first & ~15) + 256LL * blk + threadIdx.x;
+            bool in = e >= first && e < len;
+            if constexpr (SINKS) {
+                const int sinks = __builtin_amdgcn_readlane(mine.sinks, bi), sb = (sinks + 255) >> 8;
+                e = blk < sb ? 256LL * blk + threadIdx.x : e - 256LL * sb;
+                in = blk < sb ? e < sinks : e >= first && e < len;
+            }
+            if (in) {
                 const int pg = a.c.table[(long long)b * a.c.tstride + (e >> psh)];
                 if ((unsigned)pg < (unsigned)a.c.n_pages) {
                     float v = 0.f;
@@ -808,6 +834,21 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) {
     }
 }
 
+// The kernels: without sinks of the formats with one scale, and with sinks (or
+// none) of all
+template <int D, bool FP8, bool ACC, bool WIDE>
+__global__ __launch_bounds__(NW * 64, 2) void kv_attend_kernel(const KvAttendArgs a) {
+    attend<D, FP8 ? kFp8 : kBf16, ACC, WIDE, false>(a);
+}
+
+template <int D, int FMT, bool ACC, bool WIDE>
+__global__ __launch_bounds__(NW * 64, 2) void kv_attend_sinks_kernel(const KvAttendArgs a) {
+    attend<D, FMT, ACC, WIDE, true>(a);
+}
+
+__global__ __launch_bounds__(256) void kv_weigh_kernel(const KvAttendArgs a) { weigh<false>(a); }
+__global__ __launch_bounds__(256) void kv_weigh_sinks_kernel(const KvAttendArgs a) { weigh<true>(a); }
+
 template <int D, bool FP8, bool WIDE>
 hipError_t launch(const KvAttendArgs& a, bool accumulate, hipStream_t s) {
     // no more workgroups than the table rows could have work for
@@ -815,13 +856,28 @@ hipError_t launch(const KvAttendArgs& a, bool accumulate, hipStream_t s) {
     const long long tiles = (((long long)a.c.width << a.c.ps_shift) + 31) / 32 * a.B * HH;
     int grid = 1;
     while (grid < kKvAttendGrid && (long long)grid * NW < tiles) grid *= 2;
-    if (!accumulate) {
-        kv_attend_kernel<D, FP8, false, WIDE><<<grid, NT, 0, s>>>(a);
+    const bool sinks = a.sinks > 0;
+    constexpr int FMT = FP8 ? kFp8 : kBf16;
+    if (a.c.scales) {
+        kv_attend_sinks_kernel<D, kInt8, false, WIDE><<<grid, NT, 0, s>>>(a);
         return hipGetLastError();
     }
-    kv_attend_kernel<D, FP8, true, WIDE><<<grid, NT, 0, s>>>(a);
+    if (!accumulate) {
+        if (sinks)
+            kv_attend_sinks_kernel<D, FMT, false, WIDE><<<grid, NT, 0, s>>>(a);
+        else
+            kv_attend_kernel<D, FP8, false, WIDE><<<grid, NT, 0, s>>>(a);
+        return hipGetLastError();
+    }
     const long long blocks = (((long long)a.c.width << a.c.ps_shift) + 255) / 256 * a.B * a.c.hkv;
-    kv_weigh_kernel<<<(int)std::min(blocks, 1024LL), 256, 0, s>>>(a);
+    const int weigh_grid = (int)std::min(blocks, 1024LL);
+    if (sinks) {
+        kv_attend_sinks_kernel<D, FMT, true, WIDE><<<grid, NT, 0, s>>>(a);
+        kv_weigh_sinks_kernel<<<weigh_grid, 256, 0, s>>>(a);
+    } else {
+        kv_attend_kernel<D, FP8, true, WIDE><<<grid, NT, 0, s>>>(a);
+        kv_weigh_kernel<<<weigh_grid, 256, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 

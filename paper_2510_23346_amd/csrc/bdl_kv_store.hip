@@ -1,0 +1,326 @@
+// Key-value cache in 8-bit integers with a scale for each block of 16 entries
+// of a head: append, and reading any cache back (gfx950, wave64).
+#include "bdl_kv_device.h"
+
+namespace bdl {
+
+namespace {
+
+// ------------------------------------------------------------------ append
+// A block's scale is that of its largest magnitude so far:
+//
+//     m = max(|x| over the call's rows of the block, 2^-64),  s = m / 127,
+//
+// or max(s, the scale before) where the block's first entry is not among the
+// call's; x is stored as rint(x / s).  Where the scale grows, the entries that
+// were there are rounded again, rint(q s_before / s).  (m / 127 and x / s are
+// products with the fp32 reciprocals.)  So a block has one owner: the wave of
+// the first token of its run, tokens of one sequence that follow each other in
+// the call and in the block.  It has all 16 rows of the block, those that are
+// new in registers, four lanes a row; its other tokens' waves leave.
+//
+// Rotation and norm are those of the bf16 cache, and queries are dealt with by
+// threads of the same launch as there.
+template <int N>
+struct Piece {
+    float x[N];
+};
+
+// N numbers of a row
+template <int N>
+__device__ __forceinline__ Piece<N> load_piece(const uint16_t* p) {
+    Piece<N> r;
+#pragma unroll
+    for (int k = 0; k < N; k += 8) {
+        float y[8];
+        unpack8(ld16(p + k), y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.x[k + i] = y[i];
+    }
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ Piece<N> load_piece(const float* p) {
+    Piece<N> r;
+#pragma unroll
+    for (int k = 0; k < N; k += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + k);
+        r.x[k] = v.x, r.x[k + 1] = v.y, r.x[k + 2] = v.z, r.x[k + 3] = v.w;
+    }
+    return r;
+}
+
+// four numbers to the nearest integers, within +-127 (NaN: any of them)
+__device__ __forceinline__ uint32_t pack4_int8(const float* x, float f) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        r |= ((uint32_t)(int)__builtin_amdgcn_fmed3f(rintf(x[k] * f), -127.f, 127.f) & 255u) << (8 * k);
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ void unpack_int8(const uint32_t (&w)[N / 4], Piece<N>& r) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) r.x[k] = (float)(int8_t)(w[k / 4] >> (8 * (k % 4)));
+}
+
+constexpr float kLeast = 5.421010862427522e-20f;     // 2^-64
+
+// One block: token t (of an entry there is) and the tokens of its run behind it
+template <int D, bool NORM>
+__device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int kh, bool value) {
+#pragma clang fp contract(off)
+    constexpr int N = D / 8;
+    const int l = threadIdx.x & 63, r = l >> 2, c = l & 3, cap = a.c.width << a.c.ps_shift;
+    const int seq = a.seqs[t], i0 = a.index[t];
+    if (seq < 0 || seq >= a.n_seqs || i0 < 0 || i0 >= cap) return;
+    if (t > 0 && (i0 & (kKvBlock - 1)) && a.seqs[t - 1] == seq && a.index[t - 1] == i0 - 1) return;    // not the run's first
+    const long long e0 = kv_entry(a.c, seq, kh, i0 & ~(kKvBlock - 1));
+    if (e0 < 0) return;
+    // the row's token, if the run goes as far
+    const int j = r - (i0 & (kKvBlock - 1)), tok = min(t + max(j, 0), a.T - 1);
+    const bool follows = j >= 0 && j < a.T - t && a.seqs[tok] == seq && a.index[tok] == i0 + j;
+    const unsigned long long breaks = __ballot(j >= 0 && !follows);
+    const bool in_run = follows && (breaks == 0 || l < (int)__builtin_ctzll(breaks));
+    const int pos = in_run ? a.positions[tok] : -1;
+    const bool mine = in_run && pos >= 0 && pos < a.n_positions;
+    const unsigned long long rows = __ballot(mine);
+    if (rows == 0) return;
+    const bool anew = rows & 1;
+    const bool old_rows = rows != ~0ull;
+    float* const scale_at = a.c.scales + (e0 >> 4) * 2 + value;
+    const float before = *scale_at;
+    char* const base = (value ? a.c.V : a.c.K) + (e0 + r) * D;
+    const int d0 = N * c, d1 = D / 2 + N * c;
+    uint32_t q0[N / 4], q1[N / 4];
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) q0[k] = q1[k] = 0;
+    if (old_rows && !mine) {
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) {
+            q0[k] = reinterpret_cast<const uint32_t*>(base + d0)[k];
+            q1[k] = reinterpret_cast<const uint32_t*>(base + d1)[k];
+        }
+    }
+    Piece<N> y0, y1;
+#pragma unroll
+    for (int k = 0; k < N; ++k) y0.x[k] = y1.x[k] = 0.f;
+    if (mine) {
+        const uint16_t* x = a.qkv + tok * a.qkv_stride + (a.c.hq + (value ? a.c.hkv : 0) + kh) * D;
+        y0 = load_piece<N>(x + d0);
+        y1 = load_piece<N>(x + d1);
+    }
+    if (!value) {
+        if constexpr (NORM) {
+            float ss = 0.f;
+#pragma unroll
+            for (int k = 0; k < N; ++k) ss += y0.x[k] * y0.x[k] + y1.x[k] * y1.x[k];
+            ss += __shfl_xor(ss, 1);
+            ss += __shfl_xor(ss, 2);
+            const float f = 1.f / sqrtf(ss * (1.f / D) + a.eps);
+            const Piece<N> w0 = load_piece<N>(a.k_norm + d0), w1 = load_piece<N>(a.k_norm + d1);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                y0.x[k] = y0.x[k] * f * w0.x[k];
+                y1.x[k] = y1.x[k] * f * w1.x[k];
+            }
+        }
+        if (mine) {
+            const long long at = (long long)pos * (D / 2);
+            if (a.interleaved) {
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    float* const y = part ? y1.x : y0.x;
+                    const Piece<N / 2> cc = load_piece<N / 2>(a.cos + at + (part ? d1 : d0) / 2), ss = load_piece<N / 2>(a.sin + at + (part ? d1 : d0) / 2);
+#pragma unroll
+                    for (int k = 0; k < N / 2; ++k) {
+                        const float u = y[2 * k], v = y[2 * k + 1];
+                        y[2 * k] = u * cc.x[k] - v * ss.x[k];
+                        y[2 * k + 1] = v * cc.x[k] + u * ss.x[k];
+                    }
+                }
+            } else {
+                const Piece<N> cc = load_piece<N>(a.cos + at + d0), ss = load_piece<N>(a.sin + at + d0);
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float u = y0.x[k], v = y1.x[k];
+                    y0.x[k] = u * cc.x[k] - v * ss.x[k];
+                    y1.x[k] = v * cc.x[k] + u * ss.x[k];
+                }
+            }
+        }
+    }
+    // the largest magnitude, as an integer: infinities and NaN above all numbers
+    unsigned top = 0;
+    if (mine)
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            top = max(top, max(__float_as_uint(y0.x[k]) & 0x7fffffffu, __float_as_uint(y1.x[k]) & 0x7fffffffu));
+#pragma unroll
+    for (int x = 32; x; x >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, x));
+    float s = top >= 0x7f800000u ? NAN : fmaxf(__uint_as_float(top), kLeast) * (1.f / 127.f);
+    if (!anew) s = s != s || before != before ? NAN : fmaxf(s, before);
+    if (mine) {
+        const float f = 1.f / s;
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) {
+            q0[k] = pack4_int8(y0.x + 4 * k, f);
+            q1[k] = pack4_int8(y1.x + 4 * k, f);
+        }
+    } else if (!anew && s != before) {
+        const float f = before / s;
+        Piece<N> z;
+        unpack_int8<N>(q0, z);
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) q0[k] = pack4_int8(z.x + 4 * k, f);
+        unpack_int8<N>(q1, z);
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) q1[k] = pack4_int8(z.x + 4 * k, f);
+    }
+    if (mine || (!anew && s != before)) {
+#pragma unroll
+        for (int k = 0; k < N / 4; ++k) {
+            reinterpret_cast<uint32_t*>(base + d0)[k] = q0[k];
+            reinterpret_cast<uint32_t*>(base + d1)[k] = q1[k];
+        }
+    }
+    if (l == 0) *scale_at = s;
+    if (kh == 0 && value && a.lens) {
+        const int last = (63 - __builtin_clzll(rows)) >> 2;
+        if (l == 0) atomicMax(a.lens + seq, (i0 & ~(kKvBlock - 1)) + last + 1);
+    }
+}
+
+// Workgroups z = 0 take 256 / units tokens' queries, as append does; the others
+// (z > 0) four waves: of token x / 2 hkv .. the head and whether keys or values
+template <int D, bool NORM>
+__global__ __launch_bounds__(256) void kv_store_kernel(const KvAppendArgs a, int q_groups, int q_rows) {
+#pragma clang fp contract(off)
+    if ((int)blockIdx.x >= q_groups) {
+        const long long unit = (long long)(blockIdx.x - q_groups) * 4 + wave_id();
+        const int per = 2 * a.c.hkv, t = (int)(unit / per), u = (int)(unit - (long long)t * per);
+        if (t < a.T) store_block<D, NORM>(a, t, u >> 1, u & 1);
+        return;
+    }
+    constexpr int P = D / 16;
+    const int units = a.c.hq * P;
+    for (int i = threadIdx.x; i < units * q_rows; i += 256) {
+        const int row = i / units, u = i - row * units, h = u / P, j = u % P;
+        const int t = blockIdx.x * q_rows + row;
+        if (t >= a.T) return;
+        const int d0 = a.interleaved ? 16 * j : 8 * j, d1 = a.interleaved ? 16 * j + 8 : D / 2 + 8 * j;
+        const uint16_t* x = a.qkv + t * a.qkv_stride + h * D;
+        const int pos = a.positions[t];
+        const bool pos_ok = pos >= 0 && pos < a.n_positions;
+        float y0[8], y1[8];
+        unpack8(ld16(x + d0), y0);
+        unpack8(ld16(x + d1), y1);
+        if (NORM) {
+            const u32x4 w0 = ld16(a.q_norm + d0), w1 = ld16(a.q_norm + d1);
+            head_norm<D>(y0, y1, w0, w1, a.eps);
+        }
+        rotate16(y0, y1, a.cos, a.sin, (long long)(pos_ok ? pos : 0) * (D / 2) + 8 * j, a.interleaved);
+        if (!pos_ok)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y0[k] = y1[k] = 0.f;
+        uint16_t* q = a.q_out + t * a.q_stride + h * D;
+        *reinterpret_cast<u32x4*>(q + d0) = pack8(y0);
+        *reinterpret_cast<u32x4*>(q + d1) = pack8(y1);
+        if (u == 0) {
+            const int seq = a.seqs[t], at = a.index[t], cap = a.c.width << a.c.ps_shift;
+            if (!pos_ok || (seq != -1 && !(seq >= 0 && seq < a.n_seqs && at >= 0 && at < cap))) kv_error(a.c);
+        }
+    }
+}
+
+template <int D>
+hipError_t store(const KvAppendArgs& a, hipStream_t s) {
+    const int units = a.c.hq * (D / 16), rows = std::max(1, 256 / units);
+    const long long q_groups = ((long long)a.T + rows - 1) / rows, blocks = ((long long)a.T * 2 * a.c.hkv + 3) / 4;
+    if (q_groups + blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (a.q_norm)
+        kv_store_kernel<D, true><<<(int)(q_groups + blocks), 256, 0, s>>>(a, (int)q_groups, rows);
+    else
+        kv_store_kernel<D, false><<<(int)(q_groups + blocks), 256, 0, s>>>(a, (int)q_groups, rows);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ read
+// Entries as bf16: the stored number times its scale, rounded once.  A thread
+// takes 16 numbers: one 16-byte load (two in bf16), two 16-byte stores.  Bound
+// by its memory traffic.
+template <int D, int FMT>
+__global__ __launch_bounds__(256) void kv_read_kernel(const KvReadArgs a) {
+#pragma clang fp contract(off)
+    const long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    const int u = blockIdx.y * blockDim.x + threadIdx.x, h2 = u / (D / 16), j = u % (D / 16);
+    if (t >= a.T || h2 >= 2 * a.c.hkv) return;
+    const bool v = h2 >= a.c.hkv;
+    const int h = v ? h2 - a.c.hkv : h2, seq = a.seqs[t], i = a.index[t], cap = a.c.width << a.c.ps_shift;
+    long long e = -1;
+    if (seq >= 0 && seq < a.n_seqs && i >= 0 && i < cap)
+        e = kv_entry(a.c, seq, h, i);
+    else if (seq != -1)
+        kv_error(a.c);
+    u32x4 o0 = u32x4{0, 0, 0, 0}, o1 = o0;
+    if (e >= 0) {
+        const char* p = (v ? a.c.V : a.c.K) + e * (D * (FMT == kBf16 ? 2 : 1)) + 16 * j * (FMT == kBf16 ? 2 : 1);
+        const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+        if constexpr (FMT == kBf16) {
+            o0 = x;
+            o1 = *reinterpret_cast<const u32x4*>(p + 16);
+        } else {
+            const float f = FMT == kInt8 ? a.c.scales[(e >> 4) * 2 + v] : v ? a.v_scale : a.k_scale;
+            float y[16];
+#pragma unroll
+            for (int k = 0; k < 16; k += 4) {
+                const uint32_t w = x[k / 4];
+                if constexpr (FMT == kInt8) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) y[k + b] = (float)(int8_t)(w >> (8 * b));
+                } else {
+                    typedef float f32x2 __attribute__((ext_vector_type(2)));
+                    const f32x2 p0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+                    y[k] = p0[0], y[k + 1] = p0[1], y[k + 2] = p1[0], y[k + 3] = p1[1];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) y[k] *= f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                o0[k] = pk_bf16(y[2 * k], y[2 * k + 1]);
+                o1[k] = pk_bf16(y[8 + 2 * k], y[9 + 2 * k]);
+            }
+        }
+    }
+    uint16_t* const o = (v ? a.v_out + t * a.v_stride : a.k_out + t * a.k_stride) + h * D + 16 * j;
+    *reinterpret_cast<u32x4*>(o) = o0;
+    *reinterpret_cast<u32x4*>(o + 8) = o1;
+}
+
+template <int D>
+hipError_t read(const KvReadArgs& a, bool fp8, hipStream_t s) {
+    const int units = 2 * a.c.hkv * (D / 16), x = std::min(units, 256), y = 256 / x;
+    const dim3 grid((a.T + y - 1) / y, (units + x - 1) / x), block(x, y);
+    if (a.c.scales)
+        kv_read_kernel<D, kInt8><<<grid, block, 0, s>>>(a);
+    else if (fp8)
+        kv_read_kernel<D, kFp8><<<grid, block, 0, s>>>(a);
+    else
+        kv_read_kernel<D, kBf16><<<grid, block, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_store(const KvAppendArgs& a, int head_dim, hipStream_t s) {
+    return head_dim == 64 ? store<64>(a, s) : store<128>(a, s);
+}
+
+hipError_t launch_kv_read(const KvReadArgs& a, int head_dim, bool fp8, hipStream_t s) {
+    return head_dim == 64 ? read<64>(a, fp8, s) : read<128>(a, fp8, s);
+}
+
+}  // namespace bdl

@@ -16,13 +16,15 @@ class DrawnCache:
     order.  ``k[b]``, ``v[b]``: float64 ``[n_kv_heads, len, head_dim]``, the
     stored values (an 8-bit cache: times their scale); ``weight[b]``,
     ``pos[b]``.  ``spare`` pages belong to no sequence, ``room[b]`` more
-    entries have pages already (``room``: int or per sequence)."""
+    entries have pages already (``room``: int or per sequence).  ``int8``: a
+    cache with a scale for each block of 16 entries (``S``), drawn log-normal."""
 
     def __init__(self, lens, n_kv_heads, head_dim, page_size, seed, fp8=False, k_scale=1.0, v_scale=1.0, spare=2, room=0,
-                 wide=2):
+                 wide=2, int8=False):
         from oracle.kv import e4m3_encode, e4m3_values
         rng = np.random.default_rng([seed, 11])
         self.lens = np.asarray(lens, np.int32)
+        self.int8 = int8
         self.fp8, self.ps, self.hkv, self.d = fp8, page_size, n_kv_heads, head_dim
         self.scales = (k_scale, v_scale)
         B = len(self.lens)
@@ -37,8 +39,9 @@ class DrawnCache:
             self.table[b, :need[b]] = order[at:at + need[b]]
             at += need[b]
         shape = (self.n_pages, n_kv_heads, page_size)
-        nan = 0xFF if fp8 else 0x7FFF
-        self.K, self.V = (np.full(shape + (head_dim,), nan, np.uint8 if fp8 else np.uint16) for _ in range(2))
+        nan = 0x7F if int8 else 0xFF if fp8 else 0x7FFF
+        self.K, self.V = (np.full(shape + (head_dim,), nan, np.int8 if int8 else np.uint8 if fp8 else np.uint16) for _ in range(2))
+        self.S = np.full(shape[:2] + (page_size // 16, 2), np.nan, np.float32) if int8 else None
         self.W = np.full(shape, np.nan, np.float32)
         self.P = np.full(shape, 2 ** 31 - 1, np.int32)
         self.k, self.v, self.weight, self.pos = [], [], [], []
@@ -46,7 +49,13 @@ class DrawnCache:
         for b, n in enumerate(self.lens):
             for stored, plain, scale in ((self.K, self.k, k_scale), (self.V, self.v, v_scale)):
                 x = rng.standard_normal((n_kv_heads, n, head_dim))
-                if fp8:
+                if int8:
+                    bits = rng.integers(-127, 128, (n_kv_heads, n, head_dim)).astype(np.int8)
+                    f = np.exp(0.3 * rng.standard_normal((n_kv_heads, -(-n // 16)))).astype(np.float32) / np.float32(127)
+                    plain.append(bits * np.repeat(f, 16, 1)[:, :n, None].astype(np.float64))
+                    page, place = self.where(b, n)
+                    self.S[page[::16], :, place[::16] // 16, 0 if stored is self.K else 1] = f.T
+                elif fp8:
                     bits = e4m3_encode(x / scale)
                     plain.append(values[bits] * np.float64(np.float32(scale)))
                 else:
@@ -80,11 +89,14 @@ class DrawnCache:
         import torch
 
         import paper_2510_23346_amd as bd
-        kind = torch.float8_e4m3fn if self.fp8 else torch.bfloat16
-        dt = np.uint8 if self.fp8 else np.int16
+        kind = torch.int8 if self.int8 else torch.float8_e4m3fn if self.fp8 else torch.bfloat16
+        dt = np.int8 if self.int8 else np.uint8 if self.fp8 else np.int16
         k, v = (torch.from_numpy(x.view(dt).copy()).cuda().view(kind) for x in (self.K, self.V))
+        if self.int8:
+            weights = False
+            kw["scales"] = torch.from_numpy(self.S.copy()).cuda()
         cache = bd.KVCache(n_q_heads or self.hkv, self.hkv, self.d, self.n_pages, self.ps, max_seqs or max(1, len(self.lens)),
-                           fmt=bd.KV_FP8_E4M3 if self.fp8 else bd.KV_BF16, k_scale=self.scales[0], v_scale=self.scales[1], k=k,
+                           fmt=bd.KV_INT8 if self.int8 else bd.KV_FP8_E4M3 if self.fp8 else bd.KV_BF16, k_scale=self.scales[0], v_scale=self.scales[1], k=k,
                            v=v, weight=torch.from_numpy(self.W.copy()).cuda() if weights else None,
                            pos=torch.from_numpy(self.P.copy()).cuda() if weights else None, **kw)
         return cache, torch.from_numpy(self.table.copy()).cuda(), torch.from_numpy(self.lens.copy()).cuda()
