@@ -28,6 +28,9 @@ constexpr int kKvAttendGrid = 512, kKvHeads = 16;
 constexpr int kKvCount = 32, kKvAttendCounts = 3 * kKvAttendGrid;
 constexpr int kv_part_floats(int D) { return kKvHeads * (D + 2); }
 
+// attention of many tokens: shares of up to 16 rows' sums in the same place
+constexpr int kKvPromptSlots = 1536;
+
 // What every kernel knows of the cache and of the call's page table.  Pages
 // are [n_pages][hkv][1 << ps_shift] entries: K and V of D elements each,
 // weight and pos (null when the cache does not track weights) of one.
@@ -102,6 +105,9 @@ struct KvPromptArgs {
     const int *q_starts, *lens;
     float* lse;                 // may be null
     int T, B, window, sinks;    // window 0: none
+    float* part;                // kKvPromptSlots x kv_part_floats(D)
+    unsigned* count;            // as above: one of a tile of rows that is shared
+    int split;                  // whether tiles may be cut (the launch's choice)
     float score_scale;          // as above
     unsigned q_sign;
     float v_scale;

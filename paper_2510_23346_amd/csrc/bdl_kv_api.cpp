@@ -38,7 +38,7 @@ Parts layout(const bdlora_kv_desc& d, bool weights) {
     p.count = take(4LL * bdl::kKvCount * bdl::kKvAttendCounts);
     p.evict_count = take(weights ? 4LL * bdl::kKvCount * d.max_seqs * (d.n_kv_heads + 1) : 0);
     p.clear = at;
-    p.part = take(2LL * bdl::kKvAttendGrid * bdl::kv_part_floats(d.head_dim) * 4);
+    p.part = take((long long)std::max(2 * bdl::kKvAttendGrid, bdl::kKvPromptSlots) * bdl::kv_part_floats(d.head_dim) * 4);
     p.lse2 = take(weights ? 4LL * d.max_seqs * d.n_q_heads : 0);
     p.logits = take(weights ? 4LL * d.n_pages * d.n_q_heads * d.page_size : 0);
     p.total = at;

@@ -104,28 +104,6 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t x, uint32_t y) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
 }
 
-// Shares go past the caches that the compute units do not have in common
-// (device scope), 8 or 16 bytes at byte `at` of the workspace
-constexpr int kDeviceScope = 16;
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ void store_through(__amdgpu_buffer_rsrc_t r, unsigned at, f32x4 v) {
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, (int)at, 0, kDeviceScope);
-}
-
-__device__ __forceinline__ void store_through(__amdgpu_buffer_rsrc_t r, unsigned at, float2 v) {
-    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v.x), __float_as_uint(v.y)}, r, (int)at, 0, kDeviceScope);
-}
-
-__device__ __forceinline__ f32x4 load_through4(__amdgpu_buffer_rsrc_t r, unsigned at) {
-    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, kDeviceScope));
-}
-
-__device__ __forceinline__ float2 load_through2(__amdgpu_buffer_rsrc_t r, unsigned at) {
-    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, 0, kDeviceScope));
-    return float2{__uint_as_float(v[0]), __uint_as_float(v[1])};
-}
-
 // A tile: two blocks of 16 entries, each within one page, of one head of one
 // sequence
 struct Tile {

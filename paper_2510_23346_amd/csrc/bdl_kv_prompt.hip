@@ -8,14 +8,25 @@
 // running maximum m.
 //
 // The rows of a kv head are (token, query head), heads of one token side by
-// side, so that a tile of 128 rows reads an entry's key and value once for all
-// its heads.  A workgroup has a tile: four waves of 32 rows, which share tiles
-// of 64 entries in LDS, two of them in turn (one is worked on while the next
-// one's loads are in flight).
+// side, so that a tile of rows reads an entry's key and value once for all its
+// heads.  A wave's products are S^T = K Q^T and O^T = V^T P^T (32x32x16, bf16): a
+// row's scores lie in one lane (and the one 32 further), so that maximum and sum
+// need no exchange, and they are already those of the second product's operand.
+// The probabilities are rounded to bf16 for it (their sum is not).
 //
-// A wave's products are S^T = K Q^T and O^T = V^T P^T (32x32x16, bf16): a row's
-// scores lie in one lane (and the one 32 further), so that maximum and sum need
-// no exchange, and they are already those of the second product's operand.
+// Wide tiles: a workgroup has 128 (or 64) rows, 32 a wave, whose four waves share
+// tiles of 64 entries in LDS, two of them in turn: one is worked on while the next
+// one's loads are in flight.  (64 rows: two waves share a tile's entries, half each.)
+// Narrow tiles, of sequences of up to 32 rows: the four waves have the same rows and
+// every fourth tile of 32 entries each, through their own parts of LDS, and wait for
+// each other at the end only.
+//
+// Where there are few tiles of rows, or a long sequence among short ones, a tile's
+// entries are cut into stretches for several workgroups.  They leave sums, maxima and
+// outputs in the workspace; the last one to come adds them, in the order of the
+// entries.
+#include <type_traits>
+
 #include "bdl_kv_device.h"
 
 namespace bdl {
@@ -25,20 +36,91 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int NW = 4, NT = NW * 64;     // waves and threads of a workgroup, of which a compute unit holds two
-constexpr int kRows = NW * 32;          // rows of a tile
-constexpr int kKeys = 64;               // entries of a tile
+constexpr int kKeys = 64;               // entries of a wide tile
+constexpr int kNarrow = 32;             // rows, and entries of a wave's tile, of a narrow one
+
+// Stretches: as many as give this many workgroups work.  A share takes a slot of 16
+// rows' sums for each 16 rows, and half of the slots are for wide tiles where there
+// are both kinds
+constexpr int share_items(int rows) { return kKvPromptSlots / (rows / 16) / 2; }
 
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// A sequence's rows of q (of a kv head: `rows`, n tokens' G each) and length
-struct Prompt {
-    int t0, n, len;
-    unsigned tiles;
-    bool bad;
+// Where chunk c of row r of a tile's values lies in LDS: the transposing reads of
+// 32 lanes (4 rows, 4 chunks) meet every bank once
+template <int D>
+__device__ __forceinline__ int v32_at(int r, int c) {
+    return r * (D / 8) + (c ^ (D == 128 ? 4 * (r & 3) : 2 * (r & 2)));
+}
+
+// x y, but 0 where x is 0 whatever y
+__device__ __forceinline__ float times_legacy(float x, float y) {
+    float r;
+    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "s"(y), "v"(x));
+    return r;
+}
+
+// 64 pieces of 16 bytes, the lanes' at byte offsets `off` of a buffer, into LDS at
+// `to` (the wave's; lane l's lands 16 l bytes on).  Written out because the compiler
+// waits for all such copies before it reads LDS at all, the other buffer's too; here
+// copies_done waits, and what a wait of the compiler's own finds under way besides
+// can only make it longer
+__device__ __forceinline__ u32x4 rsrc_of(const char* p, unsigned bytes) {
+    return u32x4{(unsigned)(uintptr_t)p, (unsigned)((uintptr_t)p >> 32), bytes, (unsigned)kRawBufferWord3};
+}
+
+__device__ __forceinline__ unsigned lds_address(const void* p) {
+    return (unsigned)uni((int)(unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
+}
+
+__device__ __forceinline__ void copy_to_lds(u32x4 rsrc, unsigned off, unsigned at) {
+    // (the pause: a vector instruction may just have written the descriptor; the
+    // kernel has no other use of m0)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(rsrc) : "memory");
+}
+
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ unsigned lane_of(unsigned v, int i) { return (unsigned)__builtin_amdgcn_readlane((int)v, i); }
+
+// Entries that some row of entries p_first .. p_last sees: 0 .. sinks - 1 and
+// begin .. end - 1, in tiles of `size` that begin at its multiples
+struct Span {
+    int end, begin, sinks;
+    __device__ __forceinline__ Span(const KvPromptArgs& a, int p_first, int p_last) {
+        end = max(0, p_last + 1);
+        begin = a.window ? min(end, max(0, p_first - a.window + 1)) : 0;
+        sinks = min(a.sinks, begin);
+        if (sinks == begin) sinks = begin = 0;
+    }
+    __device__ __forceinline__ int sink_tiles(int size) const { return (sinks + size - 1) / size; }
+    __device__ __forceinline__ int tiles(int size) const {
+        return sink_tiles(size) + (end > begin ? (end - (begin & -size) + size - 1) / size : 0);
+    }
 };
 
+// A tile of entries: its first; those lo .. hi - 1 count
+struct Tile {
+    int e, lo, hi;
+};
+
+__device__ __forceinline__ Tile tile_at(const Span& s, int size, int ct) {
+    const int ns = s.sink_tiles(size);
+    const bool sink = ct < ns;
+    return Tile{sink ? size * ct : (s.begin & -size) + size * (ct - ns), sink ? 0 : s.begin, sink ? s.sinks : s.end};
+}
+
+// A sequence: its first row of q, new tokens, length; its tiles of rows and the
+// stretches' units (of 64 entries, narrow 128) of the last of them
+struct Prompt {
+    int t0, n, len;
+    unsigned tiles, units;
+    bool narrow, bad;
+};
+
+template <int ROWS>
 __device__ __forceinline__ Prompt prompt_of(const KvPromptArgs& a, int b, int G) {
     const int at = min(max(b, 0), a.B - 1), cap = a.c.width << a.c.ps_shift;
     const int u0 = a.q_starts[at], u1 = a.q_starts[at + 1], n = a.lens[at];
@@ -48,280 +130,846 @@ __device__ __forceinline__ Prompt prompt_of(const KvPromptArgs& a, int b, int G)
     p.n = t1 - p.t0;
     p.len = min(max(n, 0), cap);
     p.bad = p.t0 != u0 || t1 != u1 || p.len != n || p.n > p.len;
-    p.tiles = b >= 0 && b < a.B ? (unsigned)(p.n * G + kRows - 1) / kRows : 0u;
+    const int rows = b >= 0 && b < a.B ? p.n * G : 0;
+    p.narrow = rows <= kNarrow;
+    const int size = p.narrow ? kNarrow : ROWS;
+    p.tiles = (unsigned)(rows + size - 1) / size;
+    const Span s(a, p.len - p.n + (int)((max(p.tiles, 1u) - 1) * size / (unsigned)G), p.len - 1);
+    p.units = p.tiles == 0 ? 0u : p.narrow ? (unsigned)(s.tiles(kNarrow) + NW - 1) / NW : (unsigned)s.tiles(kKeys);
     return p;
 }
 
-template <int D, int FMT>
-__global__ __launch_bounds__(NT, 2) void kv_prompt_kernel(const KvPromptArgs a) {
-    constexpr int SZ = FMT == kBf16 ? 2 : 1, ROW = D * SZ, CPR = ROW / 16;
-    constexpr int LPT = kKeys * CPR / NT;           // 16-byte loads of a thread for a tile's keys
-    constexpr int KS = D / 16, DT = D / 32;
-    constexpr int BUF = kKeys * D / 8;              // 16-byte pieces of a tile's keys in LDS
-    __shared__ u32x4 lds[2][2][BUF];
-    const int w = wave_id(), l = threadIdx.x & 63, lr = l & 31, lh = l >> 5;
-    const int hkv = a.c.hkv, G = a.c.hq / hkv, psh = a.c.ps_shift, pmask = (1 << psh) - 1;
-    const int kvh = blockIdx.x % hkv;
-    const unsigned item = blockIdx.x / hkv;
+// Stretches of a tile of `units`, where `part` units each give all the workgroups
+// that the workspace has shares for work: no more than about the root of the units,
+// since the last one reads all shares, and none of short tiles, since leaving and
+// joining takes about 8 us, and a unit 1 to 1.2.  (64 tokens of 4 heads behind 2048, 4096 and
+// 32768 entries: 24, 27 and 55 us; up to twice as many stretches 27, 33 and 75, none
+// 33, 56 and 380)
+__device__ __forceinline__ unsigned parts_of(float units, float part, int narrow, int split) {
+    if (!split || units < (narrow ? 8.f : 16.f)) return 1;
+    return max(1u, (unsigned)fminf(ceilf(units / part), (narrow ? 1.4f : 1.f) * __fsqrt_rn(units)));
+}
 
-    // the workgroup's sequence and tile: the last sequence's last tile, which
-    // sees most, comes first
-    int b = -1, t0 = 0, n = 0, len = 0, r0 = 0;
-    {
-        unsigned base = 0;
-        bool bad = false;
-        for (int c0 = 0; c0 < a.B && b < 0; c0 += 64) {
-            const Prompt p = prompt_of(a, a.B - 1 - c0 - l, G);
-            bad |= p.bad;
-            const unsigned incl = base + (unsigned)wave_incl_scan((int)p.tiles);
-            const unsigned long long over = __ballot(incl > item);
-            if (over) {
-                const int i = __ffsll((long long)over) - 1;
-                b = a.B - 1 - c0 - i;
-                t0 = __builtin_amdgcn_readlane(p.t0, i);
-                n = __builtin_amdgcn_readlane(p.n, i);
-                len = __builtin_amdgcn_readlane(p.len, i);
-                r0 = (int)((unsigned)__builtin_amdgcn_readlane((int)incl, i) - 1 - item) * kRows;
-            }
-            base = (unsigned)__builtin_amdgcn_readlane((int)incl, 63);
+// What a workgroup does: a tile of rows (r0 on) of sequence b, of its entries'
+// tiles the part-th of `parts` stretches
+struct Item {
+    int b, t0, n, len, r0;
+    unsigned part, parts;
+    int slot;             // the first share's, of the tile's
+    bool narrow;
+};
+
+// The workgroup's item; b -1: there is none.  All workgroups see the same plan.
+// Wide tiles come first; the last sequence's last tile, which sees most, before
+// the others
+template <int ROWS>
+__device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned item, int kvh) {
+    constexpr int C = 4;                // sequences a lane has at once (more are looked up again)
+    const int l = threadIdx.x & 63, hkv = a.c.hkv;
+    const float heads = (float)hkv;
+    Prompt p[C];
+    auto at = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < C; ++x) p[x] = prompt_of<ROWS>(a, a.B - 1 - c0 - 64 * x - l, G);
+    };
+    Item it;
+    it.b = -1;
+    it.t0 = it.n = it.len = it.r0 = 0;
+    it.part = 0;
+    it.parts = 1;
+    it.slot = 0;
+    it.narrow = false;
+    // units of work of either kind
+    float units[2] = {0.f, 0.f};
+    bool bad = false;
+    for (int c0 = 0; c0 < a.B; c0 += 64 * C) {
+        at(c0);
+        float x[2] = {0.f, 0.f};
+#pragma unroll
+        for (int y = 0; y < C; ++y) {
+            bad |= p[y].bad;
+            const float u = (float)p[y].tiles * (float)p[y].units;
+            x[0] += p[y].narrow ? 0.f : u;
+            x[1] += p[y].narrow ? u : 0.f;
         }
-        if (bad) kv_error(a.c);
-        if (b < 0) return;
+        if (a.split)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                for (int y = 32; y; y >>= 1) x[k] += __shfl_xor(x[k], y);
+                units[k] += x[k];
+            }
     }
-    const int rows = min(kRows, n * G - r0), at0 = len - n;
-    const int p_first = at0 + r0 / G, p_last = at0 + (r0 + rows - 1) / G;
-    // entries that some row sees: 0 .. sk - 1 and k_begin .. k_end - 1
-    const int k_end = max(0, p_last + 1);
-    int k_begin = a.window ? min(k_end, max(0, p_first - a.window + 1)) : 0, sk = min(a.sinks, k_begin);
-    if (sk == k_begin) sk = k_begin = 0;
-    const int nS = (sk + kKeys - 1) / kKeys, base = k_begin & ~15;
-    const int tiles = nS + (k_end > k_begin ? (k_end - base + kKeys - 1) / kKeys : 0);
+    if (bad) kv_error(a.c);
+    const int both = units[0] > 0.f && units[1] > 0.f ? 2 : 1;
+    const float part_of[2] = {fmaxf(1.f, units[0] * heads / (float)(share_items(ROWS) / both)),
+                              fmaxf(1.f, units[1] * heads / (float)(share_items(kNarrow) / both))};
+    unsigned before = 0, slots = 0;
+#pragma unroll 1
+    for (int kind = 0; kind < 2; ++kind) {
+        const unsigned per = kind ? 2 : ROWS / 16;                // slots of a share
+#pragma unroll 1
+        for (int c0 = 0; c0 < a.B; c0 += 64 * C) {
+            if (a.B > 64 * C) at(c0);
+#pragma unroll
+            for (int x = 0; x < C; ++x) {
+                if (x > 0 && c0 + 64 * x >= a.B) continue;
+                const unsigned tiles = p[x].narrow == (kind == 1) ? p[x].tiles : 0u;
+                unsigned parts = tiles ? parts_of((float)p[x].units, part_of[kind], kind, a.split) : 1u;
+                const unsigned need = parts > 1 ? (unsigned)fminf((float)tiles * (float)parts * heads * (float)per, 1e6f) : 0u;
+                const unsigned slot_incl = slots + (unsigned)wave_incl_scan((int)need);
+                if (slot_incl > (unsigned)kKvPromptSlots) parts = 1;          // (what finds no slots is not cut)
+                const unsigned incl = before + (unsigned)wave_incl_scan((int)(tiles * parts));
+                const unsigned long long over = __ballot(incl > item);
+                if (over) {
+                    const int i = __ffsll((long long)over) - 1;
+                    it.b = a.B - 1 - c0 - 64 * x - i;
+                    it.t0 = __builtin_amdgcn_readlane(p[x].t0, i);
+                    it.n = __builtin_amdgcn_readlane(p[x].n, i);
+                    it.len = __builtin_amdgcn_readlane(p[x].len, i);
+                    it.parts = lane_of(parts, i);
+                    it.narrow = kind == 1;
+                    const unsigned z = lane_of(incl, i) - 1 - item, tile = z / it.parts;
+                    it.part = z - tile * it.parts;
+                    it.r0 = (int)(tile * (kind ? kNarrow : ROWS));
+                    it.slot = (int)(lane_of(slot_incl - need, i) + (tile * (unsigned)hkv + (unsigned)kvh) * it.parts * per);
+                    return it;
+                }
+                before = lane_of(incl, 63);
+                slots = min(lane_of(slot_incl, 63), 2u * kKvPromptSlots);
+            }
+        }
+    }
+    return it;
+}
 
-    // this lane's row
-    const bool busy = 32 * w < rows;                // the wave has rows
-    const int wr0 = r0 + min(32 * w, rows - 1), wr1 = r0 + min(32 * w + 31, rows - 1);
-    const int row = min(wr0 + lr, wr1), tok = row / G, hd = row - tok * G, p = at0 + tok;
-    const int pw_first = at0 + wr0 / G, pw_last = at0 + wr1 / G;
+// A wave's 32 rows: queries, running maximum and sum, output.  Lane: row lr = l % 32
+// (both halves of the wave; they have the sum in parts); o[dt][i]: number
+// 32 dt + 8 (i / 4) + 4 (l / 32) + i % 4 of it
+template <int D, int FMT>
+struct Rows {
+    static constexpr int KS = D / 16, DT = D / 32;
     u32x4 q[KS];
-    {
-        const uint16_t* const qp = a.q + (long long)(t0 + tok) * a.q_stride + (kvh * G + hd) * D + 8 * lh;
+    f32x16 o[DT];
+    float m, sum;
+    int l, lr, lh;
+    int p;                    // the row's own entry
+    long long row;            // of q and out
+    int hq;                   // its query head
+    int first, last;          // own entries of the wave's first and last row
+
+    // rows r0 + lr of a tile's, those from r1 on are r1 - 1 again
+    __device__ __forceinline__ void init(const KvPromptArgs& a, const Item& it, int kvh, int G, int r0, int r1) {
+        l = threadIdx.x & 63;
+        lr = l & 31;
+        lh = l >> 5;
+        const int r = min(r0 + lr, r1 - 1), tok = r / G, h = r - tok * G, at0 = it.len - it.n;
+        p = at0 + tok;
+        first = at0 + r0 / G;
+        last = at0 + min(r0 + 31, r1 - 1) / G;
+        row = it.t0 + tok;
+        hq = kvh * G + h;
+        const uint16_t* const qp = a.q + row * a.q_stride + hq * D + 8 * lh;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             q[ks] = ld16(qp + 16 * ks);
 #pragma unroll
             for (int i = 0; i < 4; ++i) q[ks][i] ^= a.q_sign;
         }
+        m = -INFINITY;
+        sum = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] = f32x16{};
     }
 
-    struct Tile {
-        int e, lo, hi;        // first entry; those lo .. hi - 1 count
+    // products with 32 keys of LDS, rows r on: lane has entries 8 (i / 4) + 4 lh + i % 4
+    __device__ __forceinline__ void read(const u32x4* keys, int r, u32x4 (&k)[KS]) const {
+#pragma unroll
+        for (int x = 0; x < KS; ++x) k[x] = keys[k_at<D>(r + lr, 2 * x + lh)];
+    }
+    __device__ __forceinline__ f32x16 products(const u32x4 (&k)[KS]) const {
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int x = 0; x < KS; ++x) s = mfma32(k[x], q[x], s);
+        return s;
+    }
+    // those of entries e0 on, blocks of 16 that are there in `there`, to be seen or not;
+    // times the scales of an int8 cache's blocks (which may be NaN: what does not see
+    // the block must not)
+    __device__ __forceinline__ void mask(const KvPromptArgs& a, f32x16& s, const Tile& t, int e0, unsigned there, const float* ks) const {
+        asm volatile("");                       // (a branch: not done and thrown away where all are seen)
+        const int to = min(t.hi - 1, p), from = a.window ? p - a.window + 1 : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int e = e0 + 8 * (i / 4) + 4 * lh + i % 4;
+            const bool sees = (e <= to) & (e >= t.lo) & ((e >= from) | (e < a.sinks)) & (bool)(there >> (i / 8) & 1);
+            s[i] = sees ? FMT == kInt8 ? s[i] * ks[i / 8] : s[i] : -INFINITY;
+        }
+    }
+    __device__ __forceinline__ float top_of(const f32x16& s, float scale0, float scale1) const {
+        float x[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            x[k] = s[8 * k];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) x[k] = fmaxf(x[k], s[8 * k + i]);
+        }
+        return FMT == kInt8 ? fmaxf(x[0] * scale0, x[1] * scale1) : fmaxf(x[0], x[1]) * scale0;
+    }
+    // The maximum follows only where a score passes it by 8 (in units of log 2):
+    // until then no exponential exceeds 2^8.  follow: the factor of the output so far
+    __device__ __forceinline__ bool passes(float top) const { return __any(top > m + 8.f); }
+    __device__ __forceinline__ float follow(float top) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m, top), f = m == -INFINITY ? 0.f : exp2_(m - mn);
+        m = mn;
+        sum *= f;
+        return f;
+    }
+    __device__ __forceinline__ void rescale(float f) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
+    }
+    // exponentials, summed, and as the second product's operand; vs: an int8 cache's
+    // scales of the values
+    __device__ __forceinline__ void exponentials(const f32x16& s, float scale0, float scale1, const float* vs, u32x4 (&pb)[2]) {
+        const float mm = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const float f = FMT == kInt8 && k ? scale1 : scale0;
+                float x = exp2_(fmaf(s[8 * k + i], f, -mm)), y = exp2_(fmaf(s[8 * k + i + 1], f, -mm));
+                sum += x + y;
+                if constexpr (FMT == kInt8) x = times_legacy(x, vs[k]), y = times_legacy(y, vs[k]);
+                pb[k][i / 2] = pk_bf16(x, y);
+            }
+        // (computed here, beside the products that go on, and not where they are used)
+        asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(sum));
+    }
+    // out^T += V^T P^T over 32 values of LDS, rows r on
+    __device__ __forceinline__ void add(const u32x4* values, int r, const u32x4 (&pb)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                s16x4 v[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int at = v32_at<D>(r + 16 * k + 8 * x + 4 * lh + ((l & 15) >> 2), 4 * dt + 2 * ((l >> 4) & 1) + ((l >> 1) & 1));
+                    v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(reinterpret_cast<const short*>(values + at) + 4 * (l & 1)));
+                }
+                o[dt] = mfma32(__builtin_bit_cast(u32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), pb[k], o[dt]);
+            }
+    }
+    // output numbers of part dt of the row, and with the first its lse
+    __device__ __forceinline__ void finish(const KvPromptArgs& a, int dt, const f32x16& v, float top, float total) const {
+        const bool none = total == 0.f;
+        const float g = a.v_scale / total;
+        uint16_t* const out = a.out + row * a.out_stride + hq * D + 32 * dt + 4 * lh;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint2*>(out + 8 * i) =
+                uint2{none ? 0u : pk_bf16(v[4 * i] * g, v[4 * i + 1] * g), none ? 0u : pk_bf16(v[4 * i + 2] * g, v[4 * i + 3] * g)};
+        if (dt == 0 && lh == 0 && a.lse) a.lse[row * a.c.hq + hq] = none ? -INFINITY : (top + __log2f(total)) * kLn2;
+    }
+};
+
+// A tile's shares in the workspace: [part][rows][D] sums, then [rows][2] maxima and
+// sums.  Byte offset of part x's, and how its rows are written and read
+template <int D>
+struct Shares {
+    __amdgpu_buffer_rsrc_t r;
+    unsigned base, size, stats;
+    __device__ __forceinline__ Shares(const KvPromptArgs& a, const Item& it, int rows16) {
+        r = buf_rsrc(a.part, (unsigned)kKvPromptSlots * 16u * (D + 2) * 4u);
+        size = (unsigned)rows16 * 16u * (D + 2) * 4u;
+        stats = (unsigned)rows16 * 16u * D * 4u;
+        base = (unsigned)it.slot * (16u * (D + 2) * 4u);
+    }
+    __device__ __forceinline__ unsigned at(unsigned part, int row, int dt, int lh) const {
+        return base + part * size + (unsigned)(row * D + 32 * dt + 4 * lh) * 4u;
+    }
+    __device__ __forceinline__ void put(unsigned part, int row, int dt, int lh, const f32x16& v) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_through(r, at(part, row, dt, lh) + 32 * i, f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]});
+    }
+    __device__ __forceinline__ void put_stat(unsigned part, int row, float m, float sum) const {
+        store_through(r, base + part * size + stats + row * 8u, float2{m, sum});
+    }
+    __device__ __forceinline__ float2 stat(unsigned part, int row) const { return load_through2(r, base + part * size + stats + row * 8u); }
+    // N parts of the output from dt on, of a row from all of its shares, in their order
+    template <int N>
+    __device__ __forceinline__ void sum(unsigned parts, int row, int dt, int lh, f32x16 (&v)[N], float& top, float& total) const {
+        constexpr int U = N == 1 ? 8 : N == 2 ? 4 : 2;      // shares whose loads are in flight at once
+#pragma unroll
+        for (int z = 0; z < N; ++z) v[z] = f32x16{};
+        top = -INFINITY;
+        total = 0.f;
+#pragma unroll 1
+        for (unsigned x0 = 0; x0 < parts; x0 += U) {
+            float2 ms[U];
+            f32x4 y[U][N][4];
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                const bool in = x0 + x < parts;
+                ms[x] = stat(in ? x0 + x : x0, row);
+                if (!in) ms[x] = float2{-INFINITY, 0.f};
+#pragma unroll
+                for (int z = 0; z < N; ++z)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[x][z][i] = load_through4(r, in ? at(x0 + x, row, dt + z, lh) + 32 * i : kOob);
+            }
+            float tn = top;
+#pragma unroll
+            for (int x = 0; x < U; ++x) tn = fmaxf(tn, ms[x].x);
+            const float fo = top == -INFINITY ? 0.f : exp2_(top - tn);
+            top = tn;
+            total *= fo;
+#pragma unroll
+            for (int z = 0; z < N; ++z) v[z] *= fo;
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                const float f = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
+                total += f * ms[x].y;
+                if (f != 0.f)
+#pragma unroll
+                    for (int z = 0; z < N; ++z)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[z][i] += f * y[x][z][i / 4][i % 4];
+            }
+        }
+    }
+};
+
+// this workgroup's share has reached memory: whether it is the tile's last
+__device__ __forceinline__ bool last_share(const KvPromptArgs& a, const Item& it, int* flag) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        unsigned* const c = a.count + (it.slot >> 1) * kKvCount;
+        const bool last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.parts - 1;
+        if (last) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = last;
+    }
+    __syncthreads();
+    return uni(*flag);
+}
+
+// Where the blocks of 16 entries of several tiles lie (and an int8 cache's scales), a
+// block a lane; in `ok` those that are there.  `bytes`: what counts from the block on,
+// of up to SPAN entries
+template <int D, int FMT, int SPAN>
+struct Blocks {
+    static constexpr int ROW = D * (FMT == kBf16 ? 2 : 1);
+    int page_next = -1;
+    unsigned at_lo = 0, at_hi = 0, bytes = 0;
+    float2 scale = float2{1.f, 1.f};
+    unsigned long long ok = 0;
+    // in: whether the lane's block at entry e, of a tile whose entries lo .. hi - 1
+    // count, will be loaded: its page's number is asked for
+    __device__ __forceinline__ bool counts(bool in, int e, const Tile& t) const { return in && e < t.hi && e + SPAN > t.lo; }
+    __device__ __forceinline__ void look(const KvPromptArgs& a, int b, bool in, int e, const Tile& t) {
+        page_next = counts(in, e, t) ? a.c.table[(long long)b * a.c.tstride + (e >> a.c.ps_shift)] : -1;
+    }
+    __device__ __forceinline__ void turn(const KvPromptArgs& a, int kvh, bool in, int e, const Tile& t) {
+        const int page = page_next;
+        const bool some = counts(in, e, t), there = some && (unsigned)page < (unsigned)a.c.n_pages;
+        if (some && !there) kv_error(a.c);
+        ok = __ballot(there);
+        const unsigned long long entry = there ? (((unsigned long long)(unsigned)page * (unsigned)a.c.hkv + (unsigned)kvh) << a.c.ps_shift) +
+                                                     (unsigned)(e & ((1 << a.c.ps_shift) - 1)) : 0ull;
+        at_lo = (unsigned)(entry * ROW);
+        at_hi = (unsigned)(entry * ROW >> 32);
+        bytes = there ? (unsigned)min(SPAN, t.hi - e) * ROW : 0u;
+        if constexpr (FMT == kInt8) scale = there ? *reinterpret_cast<const float2*>(a.c.scales + 2 * (entry >> 4)) : float2{1.f, 1.f};
+    }
+    __device__ __forceinline__ unsigned long long at(int x) const { return (unsigned long long)lane_of(at_hi, x) << 32 | lane_of(at_lo, x); }
+};
+
+template <int FMT>
+__device__ __forceinline__ u32x4 widen(u32x4 v, int half) {
+    return FMT == kFp8 ? bf16_of(v[2 * half], v[2 * half + 1]) : bf16_of_int8(v[2 * half], v[2 * half + 1]);
+}
+
+// ------------------------------------------------------------------ wide
+// PAGE: pages hold whole tiles (64 entries or more), else blocks of 16.  RW waves
+// have rows of their own, and 4 / RW the same rows and a part of a tile's entries each
+template <int D, int FMT, bool PAGE, int RW>
+__device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int kvh, int G, u32x4 (*lds)[2][kKeys * D / 8], float2 (*stat)[32],
+                                     int* flag) {
+    constexpr int ROWS = RW * 32, SPAN = PAGE ? kKeys : 16;
+    constexpr int ROW = D * (FMT == kBf16 ? 2 : 1), CPR = ROW / 16;
+    constexpr int LPT = kKeys * CPR / NT;           // 16-byte loads of a thread for a tile's keys
+    constexpr int DT = D / 32;
+    const int w = wave_id(), l = threadIdx.x & 63, rw = w % RW, half = w / RW;
+    const int rows = min(ROWS, it.n * G - it.r0), at0 = it.len - it.n;
+    const Span span(a, at0 + it.r0 / G, at0 + (it.r0 + rows - 1) / G);
+    const int tiles = span.tiles(kKeys), nS = span.sink_tiles(kKeys), base = span.begin & -kKeys;
+    const int c0 = (int)((unsigned long long)tiles * it.part / it.parts), c1 = (int)((unsigned long long)tiles * (it.part + 1) / it.parts);
+    const bool busy = 32 * rw < rows;               // the wave has rows
+    const int wr0 = it.r0 + min(32 * rw, rows - 1), r1 = it.r0 + rows;
+    Rows<D, FMT> R;
+    R.init(a, it, kvh, G, wr0, r1);
+    // tiles that no row of the wave sees are passed over: those before `gone` (but
+    // the sinks') and from `past` on; those from whole0 to whole1 are seen whole by all
+    // of them (rounded down, numbers may be < 0)
+    const int past = nS + ((R.last - base) >> 6) + 1;
+    const int gone = a.window && a.sinks <= base ? nS + ((R.first - a.window + 1 - base) >> 6) : nS;
+    const int whole1 = nS + ((R.first + 1 - base) >> 6);
+    const int whole0 = nS + ((max(span.begin, a.window ? R.last - a.window + 1 : 0) - base + kKeys - 1) >> 6);
+
+    // 16 tiles' blocks.  Tiles are loaded in order; the pages of the next 16 are asked
+    // for when the first of these is loaded
+    Blocks<D, FMT, SPAN> blocks;
+    auto look = [&](int x0) __attribute__((always_inline)) {
+        const Tile t = tile_at(span, kKeys, x0 + (l >> 2));
+        blocks.look(a, it.b, x0 + (l >> 2) < c1, t.e + 16 * (l & 3), t);
     };
-    auto tile_at = [&](int ct) __attribute__((always_inline)) {
-        const bool s = ct < nS;
-        return Tile{s ? kKeys * ct : base + kKeys * (ct - nS), s ? 0 : k_begin, s ? sk : k_end};
+    auto turn = [&](int x0) __attribute__((always_inline)) {
+        const Tile t = tile_at(span, kKeys, x0 + (l >> 2));
+        blocks.turn(a, kvh, x0 + (l >> 2) < c1, t.e + 16 * (l & 3), t);
+        look(x0 + 16);
     };
-    // a thread's loads of a tile: 64 pieces of 16 bytes a wave, of one block of 16 entries
-    auto block_of = [&](int i) __attribute__((always_inline)) { return (i * NT + w * 64) / CPR / 16; };
-    // Pages (and an int8 cache's scales) of 16 tiles at once, a block of 16 entries
-    // a lane; in `ok` those blocks that are there.  Tiles are loaded in order, the
-    // next 16 looked up when the first of these is
-    const int* const trow = a.c.table + (long long)b * a.c.tstride;
-    int page_ = 0, page_next = 0;
-    float2 scale_ = float2{1.f, 1.f}, scale_next = scale_;
-    unsigned long long ok_ = 0;
-    auto look = [&](int ct0) __attribute__((always_inline)) {
-        const int ct = ct0 + (l >> 2);
-        const Tile t = tile_at(ct);
-        const int e = t.e + 16 * (l & 3);
-        page_next = ct < tiles && e < t.hi ? trow[e >> psh] : -1;
-    };
-    auto entry_of = [&](int page, int e) __attribute__((always_inline)) {
-        return (((unsigned long long)(unsigned)page * (unsigned)hkv + (unsigned)kvh) << psh) + (unsigned)(e & pmask);
-    };
-    auto turn = [&](int ct0) __attribute__((always_inline)) {
-        page_ = page_next;
-        const int ct = ct0 + (l >> 2);
-        const Tile t = tile_at(ct);
-        const int e = t.e + 16 * (l & 3);
-        const bool in = ct < tiles && e < t.hi, there = in && (unsigned)page_ < (unsigned)a.c.n_pages;
-        if (in && !there) kv_error(a.c);
-        ok_ = __ballot(there);
-        if constexpr (FMT == kInt8) scale_ = there ? *reinterpret_cast<const float2*>(a.c.scales + 2 * (entry_of(page_, e) >> 4)) : float2{1.f, 1.f};
-        look(ct0 + 16);
-    };
-    u32x4 kr[LPT], vr[LPT];
     // of the tile being worked on: blocks that are there, and their scales
     unsigned there = 0, there_next = 0;
     float ks[4], vs[4], ks_next[4], vs_next[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) ks[k] = vs[k] = ks_next[k] = vs_next[k] = 1.f;
-    auto load = [&](int ct) __attribute__((always_inline)) {
-        if ((ct & 15) == 0) turn(ct);
-        const Tile t = tile_at(ct);
-        const int l0 = 4 * (ct & 15);
-        there_next = (unsigned)(ok_ >> l0) & 15u;
+    u32x4 kr[LPT], vr[LPT];                         // (8-bit formats)
+    // Where this lane's pieces lie in a tile, or in a block.  bf16 goes straight into
+    // LDS, lane after lane, and the pieces of a row are exchanged on the way; what
+    // lies before the first entry may be NaN, and 0 times NaN is one: zeros in its place
+    constexpr int BUF = kKeys * D / 8;
+    const unsigned lds_w = lds_address(lds) + (unsigned)w * 1024u;
+    unsigned ko[LPT], vo[LPT];
 #pragma unroll
-        for (int i = 0; i < LPT; ++i) {
-            const int blk = block_of(i), e = t.e + 16 * blk;
-            const bool ok = there_next >> blk & 1;
-            const unsigned long long ent = entry_of(ok ? __builtin_amdgcn_readlane(page_, l0 + blk) : 0, e);
-            const unsigned lo = (unsigned)uni((int)(unsigned)ent), hi = (unsigned)uni((int)(unsigned)(ent >> 32));
-            const unsigned long long at = ((unsigned long long)hi << 32 | lo) * ROW;
-            const unsigned bytes = (unsigned)uni(ok ? min(16, t.hi - e) : 0) * ROW;
-            const unsigned off = (unsigned)((((i * NT + (int)threadIdx.x) / CPR & 15) * CPR + threadIdx.x % CPR) * 16);
-            kr[i] = buf16(buf_rsrc(a.c.K + at, bytes), off);
-            vr[i] = buf16(buf_rsrc(a.c.V + at, bytes), off);
+    for (int i = 0; i < LPT; ++i) {
+        const int id = i * NT + (int)threadIdx.x, r = id / CPR, c = id % CPR, from = (PAGE ? r : r & 15) * CPR;
+        ko[i] = (unsigned)(from + (FMT == kBf16 ? k_at<D>(r, c) % CPR : c)) * 16;
+        vo[i] = (unsigned)(from + v32_at<D>(r, c) % CPR) * 16;
+    }
+    // the next tile: where it is, then its loads piece by piece
+    const char *pk = nullptr, *pv = nullptr;
+    unsigned size = 0;
+    int from = 0;                                   // (its place in the tile of the first entry that counts)
+    auto find = [&](int ct) __attribute__((always_inline)) {
+        if ((ct & 15) == 0 && ct > c0) turn(ct);
+        const int l0 = 4 * (ct & 15);
+        there_next = (unsigned)(blocks.ok >> l0) & 15u;
+        if constexpr (FMT == kBf16) {
+            const Tile t = tile_at(span, kKeys, ct);
+            from = t.lo - t.e;
+        }
+        if constexpr (PAGE) {
+            const unsigned long long at = blocks.at(l0);
+            size = lane_of(blocks.bytes, l0);
+            pk = a.c.K + at;
+            pv = a.c.V + at;
         }
         if constexpr (FMT == kInt8)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                ks_next[k] = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(scale_.x), l0 + k));
-                vs_next[k] = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(scale_.y), l0 + k));
+                ks_next[k] = __uint_as_float(lane_of(__float_as_uint(blocks.scale.x), l0 + k));
+                vs_next[k] = __uint_as_float(lane_of(__float_as_uint(blocks.scale.y), l0 + k));
             }
     };
-    auto next = [&]() __attribute__((always_inline)) {
+    constexpr int PIECES = 2 * LPT;
+    auto piece = [&](auto buf, int ct, int x) __attribute__((always_inline)) {
+        const int i = x >> 1;
+        if (!PAGE && (x & 1) == 0) {
+            // 64 pieces of 16 bytes a wave, of one block of 16 entries
+            const int y = 4 * (ct & 15) + (i * NT + w * 64) / CPR / 16;
+            const unsigned long long at = blocks.at(y);
+            size = lane_of(blocks.bytes, y);
+            pk = a.c.K + at;
+            pv = a.c.V + at;
+        }
+        if constexpr (FMT == kBf16) {
+            const unsigned to = lds_w + (unsigned)(buf * 2 * BUF + i * NT) * 16u;
+            if (x & 1)
+                copy_to_lds(rsrc_of(pv, size), (i * NT + (int)threadIdx.x) / CPR < from ? kOob : vo[i], to + BUF * 16u);
+            else
+                copy_to_lds(rsrc_of(pk, size), ko[i], to);
+        } else if (x & 1) {
+            vr[i] = buf16(buf_rsrc(pv, size), ko[i]);
+        } else {
+            kr[i] = buf16(buf_rsrc(pk, size), ko[i]);
+        }
+    };
+    auto load = [&](auto buf, int ct) __attribute__((always_inline)) {
+        find(ct);
+#pragma unroll
+        for (int x = 0; x < PIECES; ++x) piece(buf, ct, x);
+    };
+    // the loaded tile is in LDS for all waves
+    auto arrive = [&](auto buf, int ct) __attribute__((always_inline)) {
+        if constexpr (FMT != kBf16) {
+            const Tile t = tile_at(span, kKeys, ct);
+#pragma unroll
+            for (int i = 0; i < LPT; ++i) {
+                const int id = i * NT + (int)threadIdx.x, r = id / CPR, c = id % CPR;
+                u32x4 v = vr[i];
+                if (FMT == kFp8 && t.e + r < t.lo) v = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    lds[buf][0][k_at<D>(r, 2 * c + x)] = widen<FMT>(kr[i], x);
+                    lds[buf][1][v32_at<D>(r, 2 * c + x)] = widen<FMT>(v, x);
+                }
+            }
+        } else {
+            copies_done();
+        }
         there = there_next;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             ks[k] = ks_next[k];
             vs[k] = vs_next[k];
         }
+        __syncthreads();
     };
-    auto put = [&](int buf, int ct) __attribute__((always_inline)) {
-        const Tile t = tile_at(ct);
+    // A tile that all rows of the wave see whole, and the next one's loads, spread
+    // among the products
+    auto whole = [&](auto buf, int ct) __attribute__((always_inline)) {
+        constexpr std::integral_constant<int, 1 - decltype(buf)::value> other{};
+        const u32x4 *const keys = lds[buf][0], *const values = lds[buf][1];
+        constexpr int KS = Rows<D, FMT>::KS, HALVES = RW == 4 ? 2 : 1, PER = HALVES * KS / PIECES;
+        auto scale = [&](int k) __attribute__((always_inline)) { return FMT == kInt8 ? a.score_scale * ks[k] : a.score_scale; };
+        find(ct + 1);
+        if constexpr (RW == 4) {
+            // two halves of 32 entries, so that the matrix products of one go on
+            // beside the exponentials of the other
+            u32x4 k0[KS], k1[KS], p0[2], p1[2];
+            R.read(keys, 0, k0);
+            if (FMT == kBf16) R.read(keys, 32, k1);
+            f32x16 s0 = f32x16{}, s1 = f32x16{};
 #pragma unroll
-        for (int i = 0; i < LPT; ++i) {
-            const int id = i * NT + (int)threadIdx.x, r = id / CPR, c = id % CPR;
-            u32x4 v = vr[i];
-            // (what lies before the first entry may be NaN, and 0 times NaN is one)
-            if (t.e + r < t.lo) v = u32x4{0, 0, 0, 0};
-            if constexpr (FMT == kBf16) {
-                lds[buf][0][k_at<D>(r, c)] = kr[i];
-                lds[buf][1][v_at<D>(r, c)] = v;
-            } else {
-                const u32x4 k = kr[i];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    lds[buf][0][k_at<D>(r, 2 * c + x)] = FMT == kFp8 ? bf16_of(k[2 * x], k[2 * x + 1]) : bf16_of_int8(k[2 * x], k[2 * x + 1]);
-                    lds[buf][1][v_at<D>(r, 2 * c + x)] = FMT == kFp8 ? bf16_of(v[2 * x], v[2 * x + 1]) : bf16_of_int8(v[2 * x], v[2 * x + 1]);
+            for (int x = 0; x < 2 * KS; ++x) {
+                // (8-bit formats: the loads' registers leave no room for it sooner)
+                if (FMT != kBf16 && x == KS) R.read(keys, 32, k1);
+                if (x < KS)
+                    s0 = mfma32(k0[x], R.q[x], s0);
+                else
+                    s1 = mfma32(k1[x - KS], R.q[x - KS], s1);
+                if (x % PER == PER - 1 && x / PER < PIECES) {
+                    __builtin_amdgcn_sched_barrier(0x406);
+                    piece(other, ct + 1, x / PER);
+                    __builtin_amdgcn_sched_barrier(0x406);
                 }
             }
+            const float before = R.sum;
+            R.exponentials(s0, scale(0), scale(1), vs, p0);
+            const float top = fmaxf(R.top_of(s0, scale(0), scale(1)), R.top_of(s1, scale(2), scale(3)));
+            if (R.passes(top)) {                    // (rarely: done again with the new maximum)
+                R.sum = before;
+                R.rescale(R.follow(top));
+                R.exponentials(s0, scale(0), scale(1), vs, p0);
+            }
+            R.add(values, 0, p0);
+            R.exponentials(s1, scale(2), scale(3), vs + 2, p1);
+            R.add(values, 32, p1);
+        } else {
+            const float k2[2] = {half ? ks[2] : ks[0], half ? ks[3] : ks[1]}, v2[2] = {half ? vs[2] : vs[0], half ? vs[3] : vs[1]};
+            const float f0 = FMT == kInt8 ? a.score_scale * k2[0] : a.score_scale, f1 = FMT == kInt8 ? a.score_scale * k2[1] : a.score_scale;
+            u32x4 k[KS], pb[2];
+            R.read(keys, 32 * half, k);
+            f32x16 s = f32x16{};
+#pragma unroll
+            for (int x = 0; x < KS; ++x) {
+                s = mfma32(k[x], R.q[x], s);
+                if (x % PER == PER - 1 && x / PER < PIECES) {
+                    __builtin_amdgcn_sched_barrier(0x406);
+                    piece(other, ct + 1, x / PER);
+                    __builtin_amdgcn_sched_barrier(0x406);
+                }
+            }
+            const float top = R.top_of(s, f0, f1);
+            if (R.passes(top)) R.rescale(R.follow(top));
+            R.exponentials(s, f0, f1, v2, pb);
+            R.add(values, 32 * half, pb);
         }
     };
-    float m = -INFINITY, sum = 0.f;
-    f32x16 o[DT];
+    // Any tile: half by half
+    auto any = [&](int buf, int ct) __attribute__((always_inline)) {
+        load(buf ^ 1, ct + 1);
+        if (!busy || ct >= past || (ct >= nS && ct < gone)) return;
+        const u32x4 *const keys = lds[buf][0], *const values = lds[buf][1];
+        const Tile t = tile_at(span, kKeys, ct);
+#pragma unroll 1
+        for (int h = RW == 4 ? 0 : half; h < (RW == 4 ? 2 : half + 1); ++h) {
+            const float k2[2] = {h ? ks[2] : ks[0], h ? ks[3] : ks[1]}, v2[2] = {h ? vs[2] : vs[0], h ? vs[3] : vs[1]};
+            u32x4 k[Rows<D, FMT>::KS], pb[2];
+            R.read(keys, 32 * h, k);
+            f32x16 s = R.products(k);
+            R.mask(a, s, t, t.e + 32 * h, there >> (2 * h), k2);
+            const float top = R.top_of(s, a.score_scale, a.score_scale);
+            if (R.passes(top)) R.rescale(R.follow(top));
+            R.exponentials(s, a.score_scale, a.score_scale, v2, pb);
+            R.add(values, 32 * h, pb);
+        }
+    };
+    constexpr std::integral_constant<int, 0> buf0{};
+    constexpr std::integral_constant<int, 1> buf1{};
+    if (c1 > c0) {
+        look(c0 & ~15);
+        turn(c0 & ~15);
+        load(0, c0);
+    }
+    arrive(0, c0);
+    // (waves leave the loops at tiles of their own: each passes as many barriers)
+    const int from_whole = busy ? max(c0, whole0) : c1, to_whole = busy ? min(c1, whole1) : c0;
+    int ct = c0;
+#pragma unroll 1
+    for (; ct < c1 && (ct < from_whole || ((ct - c0) & 1)); ++ct) {
+        any((ct - c0) & 1, ct);
+        arrive((ct - c0 + 1) & 1, ct + 1);
+    }
+#pragma unroll 1
+    while (ct + 2 <= to_whole && there == 15u) {
+        whole(buf0, ct);
+        arrive(buf1, ++ct);
+        if (there != 15u) break;
+        whole(buf1, ct);
+        arrive(buf0, ++ct);
+    }
+#pragma unroll 1
+    for (; ct < c1; ++ct) {
+        any((ct - c0) & 1, ct);
+        arrive((ct - c0 + 1) & 1, ct + 1);
+    }
+    R.sum += __shfl_xor(R.sum, 32);
+    bool mine = busy && wr0 + R.lr < r1;
+    if constexpr (RW < 4) {
+        // the other half's sums, through LDS (nobody reads tiles any more)
+        f32x4* const x = reinterpret_cast<f32x4*>(lds) + rw * (D / 8 * 64);
+        if (half) {
+            if (l < 32) stat[rw][l] = float2{R.m, R.sum};
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x16{};
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[(4 * dt + i) * 64 + l] = f32x4{R.o[dt][4 * i], R.o[dt][4 * i + 1], R.o[dt][4 * i + 2], R.o[dt][4 * i + 3]};
+        }
+        __syncthreads();
+        mine = mine && half == 0;
+        if (half == 0) {
+            const float2 y = stat[rw][R.lr];
+            const float M = fmaxf(R.m, y.x), f0 = R.m == -INFINITY ? 0.f : exp2_(R.m - M), f1 = y.x == -INFINITY ? 0.f : exp2_(y.x - M);
+            R.m = M;
+            R.sum = f0 * R.sum + f1 * y.y;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 v = x[(4 * dt + i) * 64 + l];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) R.o[dt][4 * i + k] = f0 * R.o[dt][4 * i + k] + f1 * v[k];
+                }
+        }
+    }
+    const int row = wr0 - it.r0 + R.lr;
+    if (it.parts > 1) {
+        const Shares<D> sh(a, it, ROWS / 16);
+        if (mine) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) sh.put(it.part, row, dt, R.lh, R.o[dt]);
+            if (R.lh == 0) sh.put_stat(it.part, row, R.m, R.sum);
+        }
+        // (the waves that have the same rows take their parts of the output)
+        constexpr int N = DT * RW / 4;
+        if (!last_share(a, it, flag) || !busy || wr0 + R.lr >= r1) return;
+        f32x16 v[N];
+        float top, total;
+        sh.template sum<N>(it.parts, row, half * N, R.lh, v, top, total);
+#pragma unroll
+        for (int z = 0; z < N; ++z) R.finish(a, half * N + z, v[z], top, total);
+        return;
+    }
+    if (!mine) return;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) R.finish(a, dt, R.o[dt], R.m, R.sum);
+}
 
-    if (tiles > 0) {
+// ------------------------------------------------------------------ narrow
+template <int D, int FMT>
+__device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, int kvh, int G, u32x4* lds_, float2 (*stat)[32], int* flag) {
+    constexpr int ROW = D * (FMT == kBf16 ? 2 : 1), CPR = ROW / 16;
+    constexpr int LPT = kNarrow * CPR / 64;         // 16-byte loads of a lane for a tile's keys
+    constexpr int DT = D / 32, BUF = kNarrow * D / 8;
+    const int w = wave_id(), l = threadIdx.x & 63;
+    const int rows = min(kNarrow, it.n * G - it.r0), at0 = it.len - it.n;
+    const Span span(a, at0 + it.r0 / G, at0 + (it.r0 + rows - 1) / G);
+    const int tiles = span.tiles(kNarrow), units = (tiles + NW - 1) / NW;
+    const int c0 = NW * (int)((unsigned long long)units * it.part / it.parts) + w;
+    const int c1 = min(tiles, NW * (int)((unsigned long long)units * (it.part + 1) / it.parts));
+    u32x4 *const keys = lds_ + w * 2 * BUF, *const values = keys + BUF;
+    Rows<D, FMT> R;
+    R.init(a, it, kvh, G, it.r0, it.r0 + rows);
+
+    // 32 of the wave's tiles' blocks, two of a tile; tile i is c0 + NW i
+    Blocks<D, FMT, 16> blocks;
+    auto look = [&](int i0) __attribute__((always_inline)) {
+        const int ct = c0 + NW * (i0 + (l >> 1));
+        const Tile t = tile_at(span, kNarrow, ct);
+        blocks.look(a, it.b, ct < c1, t.e + 16 * (l & 1), t);
+    };
+    auto turn = [&](int i0) __attribute__((always_inline)) {
+        const int ct = c0 + NW * (i0 + (l >> 1));
+        const Tile t = tile_at(span, kNarrow, ct);
+        blocks.turn(a, kvh, ct < c1, t.e + 16 * (l & 1), t);
+        look(i0 + 32);
+    };
+    u32x4 kr[LPT], vr[LPT];
+    unsigned there = 0;
+    float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
+    auto load = [&](int i) __attribute__((always_inline)) {
+        if ((i & 31) == 0) turn(i);
+        const int l0 = 2 * (i & 31);
+        there = (unsigned)(blocks.ok >> l0) & 3u;
+#pragma unroll
+        for (int k = 0; k < LPT; ++k) {
+            // (64 pieces, all of one block)
+            const int x = l0 + k * 64 / CPR / 16, id = k * 64 + l;
+            const unsigned off = (unsigned)((id / CPR & 15) * CPR + id % CPR) * 16, size = lane_of(blocks.bytes, x);
+            kr[k] = buf16(buf_rsrc(a.c.K + blocks.at(x), size), off);
+            vr[k] = buf16(buf_rsrc(a.c.V + blocks.at(x), size), off);
+        }
+        if constexpr (FMT == kInt8)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                ks[k] = __uint_as_float(lane_of(__float_as_uint(blocks.scale.x), l0 + k));
+                vs[k] = __uint_as_float(lane_of(__float_as_uint(blocks.scale.y), l0 + k));
+            }
+    };
+    if (c0 < c1) {
         look(0);
         load(0);
-        put(0, 0);
-        next();
     }
-    __syncthreads();
-    for (int ct = 0; ct < tiles; ++ct) {
-        const int buf = ct & 1;
-        load(ct + 1);
-        const Tile t = tile_at(ct);
-        const bool past = t.e > pw_last;                                   // no row of the wave sees it
-        const bool gone = a.window && t.e + kKeys - 1 <= pw_first - a.window && t.e >= a.sinks;
-        if (busy && !past && !gone) {
-            const u32x4* const kb = lds[buf][0];
-            const u32x4* const vb = lds[buf][1];
-            f32x16 s[2] = {f32x16{}, f32x16{}};
+    for (int i = 0, ct = c0; ct < c1; ++i, ct += NW) {
+        const Tile t = tile_at(span, kNarrow, ct);
+        const unsigned here = there;
+        const float k2[2] = {ks[0], ks[1]}, v2[2] = {vs[0], vs[1]};
+        // (the wave's LDS operations run in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                s[0] = mfma32(kb[k_at<D>(lr, 2 * ks + lh)], q[ks], s[0]);
-                s[1] = mfma32(kb[k_at<D>(32 + lr, 2 * ks + lh)], q[ks], s[1]);
-            }
-            const bool whole = t.e >= t.lo && t.e + kKeys <= t.hi && t.e + kKeys - 1 <= pw_first && there == 15u &&
-                               (!a.window || t.e > pw_last - a.window || t.e + kKeys <= a.sinks);
-            if (!whole) {
-                const int last = min(t.hi - 1, p), first = a.window ? p - a.window + 1 : 0;
+        for (int k = 0; k < LPT; ++k) {
+            const int id = k * 64 + l, r = id / CPR, c = id % CPR;
+            u32x4 v = vr[k];
+            if (FMT != kInt8 && t.e + r < t.lo) v = u32x4{0, 0, 0, 0};
+            if constexpr (FMT == kBf16) {
+                keys[k_at<D>(r, c)] = kr[k];
+                values[v32_at<D>(r, c)] = v;
+            } else {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int e = t.e + 32 * j + 8 * (i / 4) + 4 * lh + i % 4;
-                        const bool sees = e <= last && e >= t.lo && (e >= first || e < a.sinks) && (there >> (2 * j + i / 8) & 1);
-                        s[j][i] = sees ? s[j][i] : -INFINITY;
-                    }
-            }
-            float scale[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) scale[k] = FMT == kInt8 ? a.score_scale * ks[k] : a.score_scale;
-            float top = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float x = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x = fmaxf(x, s[k / 2][8 * (k & 1) + i]);
-                top = fmaxf(top, x * scale[k]);
-            }
-            // the maximum follows only where a score passes it by 8 (in units of
-            // log 2): until then no exponential exceeds 2^8
-            if (__any(top > m + 8.f)) {
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float mn = fmaxf(m, top), f = m == -INFINITY ? 0.f : exp2_(m - mn);
-                m = mn;
-                sum *= f;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] *= f;
-            }
-            const float mm = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                u32x4 pb;
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    float x = exp2_(fmaf(s[k / 2][8 * (k & 1) + i], scale[k], -mm)), y = exp2_(fmaf(s[k / 2][8 * (k & 1) + i + 1], scale[k], -mm));
-                    sum += x + y;
-                    if constexpr (FMT == kInt8) x *= vs[k], y *= vs[k];
-                    pb[i / 2] = pk_bf16(x, y);
-                }
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    s16x4 v[2];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int r = 16 * k + 8 * j + 4 * lh + ((l & 15) >> 2);
-                        const short* const at = reinterpret_cast<const short*>(vb + v_at<D>(r, 4 * dt + 2 * ((l >> 4) & 1) + ((l >> 1) & 1))) + 4 * (l & 1);
-                        v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-                    }
-                    const u32x4 va = __builtin_bit_cast(u32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[dt] = mfma32(va, pb, o[dt]);
+                for (int x = 0; x < 2; ++x) {
+                    keys[k_at<D>(r, 2 * c + x)] = widen<FMT>(kr[k], x);
+                    values[v32_at<D>(r, 2 * c + x)] = widen<FMT>(v, x);
                 }
             }
         }
-        put(buf ^ 1, ct + 1);
-        next();
-        __syncthreads();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        load(i + 1);
+        const bool whole = here == 3u && t.e >= t.lo && t.e + kNarrow <= t.hi && t.e + kNarrow - 1 <= R.first &&
+                           (!a.window || t.e > R.last - a.window || t.e + kNarrow <= a.sinks);
+        const float f0 = FMT == kInt8 && whole ? a.score_scale * k2[0] : a.score_scale, f1 = FMT == kInt8 && whole ? a.score_scale * k2[1] : a.score_scale;
+        u32x4 k[Rows<D, FMT>::KS];
+        R.read(keys, 0, k);
+        f32x16 s = R.products(k);
+        if (!whole) R.mask(a, s, t, t.e, here, k2);
+        const float top = R.top_of(s, f0, f1);
+        if (R.passes(top)) R.rescale(R.follow(top));
+        u32x4 pb[2];
+        R.exponentials(s, f0, f1, v2, pb);
+        R.add(values, 0, pb);
     }
-    if (!busy || wr0 + lr > wr1) return;
-    sum += __shfl_xor(sum, 32);
-    const bool none = sum == 0.f;
-    const float g = a.v_scale / sum;
-    uint16_t* const out = a.out + (long long)(t0 + tok) * a.out_stride + (kvh * G + hd) * D + 4 * lh;
+    // the four waves' sums, each in its own part of LDS, added in order; wave dt has
+    // part dt of the outputs
+    R.sum += __shfl_xor(R.sum, 32);
+    f32x4* const x = reinterpret_cast<f32x4*>(lds_);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (l < 32) stat[w][l] = float2{R.m, R.sum};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint2*>(out + 32 * dt + 8 * i) =
-                uint2{none ? 0u : pk_bf16(o[dt][4 * i] * g, o[dt][4 * i + 1] * g), none ? 0u : pk_bf16(o[dt][4 * i + 2] * g, o[dt][4 * i + 3] * g)};
-    if (lh == 0 && a.lse) a.lse[(long long)(t0 + tok) * a.c.hq + kvh * G + hd] = none ? -INFINITY : (m + __log2f(sum)) * kLn2;
+        for (int i = 0; i < 4; ++i) x[w * 2 * BUF + (4 * dt + i) * 64 + l] = f32x4{R.o[dt][4 * i], R.o[dt][4 * i + 1], R.o[dt][4 * i + 2], R.o[dt][4 * i + 3]};
+    __syncthreads();
+    const bool mine = w < DT && R.lr < rows;
+    const int dt = w;
+    f32x16 v = f32x16{};
+    float top = -INFINITY, total = 0.f;
+    if (mine) {
+        float2 st[NW];
+#pragma unroll
+        for (int z = 0; z < NW; ++z) {
+            st[z] = stat[z][R.lr];
+            top = fmaxf(top, st[z].x);
+        }
+#pragma unroll
+        for (int z = 0; z < NW; ++z) {
+            const float f = st[z].x == -INFINITY ? 0.f : exp2_(st[z].x - top);
+            total += f * st[z].y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 y = x[z * 2 * BUF + (4 * dt + i) * 64 + l];
+                if (f != 0.f)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[4 * i + k] += f * y[k];
+            }
+        }
+    }
+    if (it.parts > 1) {
+        const Shares<D> sh(a, it, kNarrow / 16);
+        if (mine) {
+            sh.put(it.part, R.lr, dt, R.lh, v);
+            if (dt == 0 && R.lh == 0) sh.put_stat(it.part, R.lr, top, total);
+        }
+        if (!last_share(a, it, flag) || !mine) return;
+        f32x16 u[1];
+        sh.template sum<1>(it.parts, R.lr, dt, R.lh, u, top, total);
+        v = u[0];
+    }
+    if (mine) R.finish(a, dt, v, top, total);
+}
+
+template <int D, int FMT, bool PAGE, int RW>
+__global__ __launch_bounds__(NT, 2) void kv_prompt_kernel(const KvPromptArgs a) {
+    __shared__ u32x4 lds[2][2][kKeys * D / 8];
+    __shared__ float2 stat[NW][32];
+    __shared__ int flag;
+    const int hkv = a.c.hkv, G = a.c.hq / hkv, kvh = blockIdx.x % hkv;
+    const Item it = item_of<RW * 32>(a, G, blockIdx.x / hkv, kvh);
+    if (it.b < 0) return;
+    if (it.narrow)
+        narrow<D, FMT>(a, it, kvh, G, lds[0][0], stat, &flag);
+    else
+        wide<D, FMT, PAGE, RW>(a, it, kvh, G, lds, stat, &flag);
+}
+
+template <int D, int FMT, bool PAGE>
+hipError_t launch(KvPromptArgs a, hipStream_t s) {
+    const long long G = a.c.hq / a.c.hkv, seqs = std::min(a.T, a.B);
+    auto tiles = [&](int rows) { return (a.T * G / rows + seqs) * a.c.hkv; };
+    // 64 rows a workgroup where 128 would leave compute units without, or with one long
+    // tile beside a short one.  (4 heads of 128 on one kv head, 64 and 128 rows: 8 prompts of
+    // 1024 29.0 and 30.4 us, 12 of them 46.8 and 42.3, 24 71.8 and 61.9; of 4096, 2 72.7 and
+    // 80.3, 4 107 and 119)
+    const long long wide = tiles(128);
+    const bool half = wide < 320 || (wide < 768 && a.T * G / 128 >= 64 * seqs);
+    const long long items = half ? tiles(64) : wide;
+    a.split = items < 1024;
+    // (stretches are at most one a tile more than the items they were made for)
+    const int grid = (int)(items + (a.split ? share_items(half ? 64 : 128) + share_items(kNarrow) + 16 : 0));
+    if (half)
+        kv_prompt_kernel<D, FMT, PAGE, 2><<<grid, NT, 0, s>>>(a);
+    else
+        kv_prompt_kernel<D, FMT, PAGE, 4><<<grid, NT, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch(const KvPromptArgs& a, bool fp8, hipStream_t s) {
-    const long long G = a.c.hq / a.c.hkv, items = (a.T * G / kRows + std::min(a.T, a.B)) * a.c.hkv;
-    if (a.c.scales)
-        kv_prompt_kernel<D, kInt8><<<(int)items, NT, 0, s>>>(a);
-    else if (fp8)
-        kv_prompt_kernel<D, kFp8><<<(int)items, NT, 0, s>>>(a);
-    else
-        kv_prompt_kernel<D, kBf16><<<(int)items, NT, 0, s>>>(a);
-    return hipGetLastError();
+    if (a.c.scales) return launch<D, kInt8, false>(a, s);
+    if (fp8) return launch<D, kFp8, false>(a, s);
+    return 1 << a.c.ps_shift >= kKeys ? launch<D, kBf16, true>(a, s) : launch<D, kBf16, false>(a, s);
 }
 
 }  // namespace

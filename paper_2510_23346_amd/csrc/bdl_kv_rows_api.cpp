@@ -70,6 +70,9 @@ int bdlora_kv_attend_prompt(bdlora_kv_t c, const void* q, int64_t q_stride, int3
         a.lse = lse;
         a.T = T;
         a.B = B;
+        a.part = c->part;
+        a.count = c->count;
+        a.split = 0;
         a.window = window;
         a.sinks = window ? sinks : 0;         // (without a window every entry is attended to)
         // (kept above zero: masked scores are -infinity, times the scale too)
