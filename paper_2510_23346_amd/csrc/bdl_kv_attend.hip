@@ -281,14 +281,14 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
             x.at[j] = ((unsigned long long)(unsigned)x.page[j] * (page16 * row16) +
                        (((unsigned)kvh << psh) + ((unsigned)(x.e + 16 * j) & pmask)) * row16) * 16;
             if constexpr (FMT == kInt8) {
-                // (a block is 16 entries of 16 row16 bytes each)
+                // (a block is 16 entries; vector loads, since a wait for a scalar one
+                // would hold up every read of LDS that follows)
                 const unsigned long long blk = x.at[j] / (16ull * ROW);
                 const unsigned lo = (unsigned)uni((int)(unsigned)blk), hi = (unsigned)uni((int)(unsigned)(blk >> 32));
-                typedef const __attribute__((address_space(4))) float* cfloat;
-                const cfloat sc = (cfloat)(a.c.scales + 2 * ((unsigned long long)hi << 32 | lo));
-                x.ks[j] = sc[0];
-                x.vs[j] = sc[1];
-                if (x.n[j] == 0) x.ks[j] = x.vs[j] = 1.f;
+                const u32x2 sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(
+                    buf_rsrc(a.c.scales + 2 * ((unsigned long long)hi << 32 | lo), 8u), 0, 0, 0));
+                x.ks[j] = __uint_as_float(sc[0]);
+                x.vs[j] = __uint_as_float(sc[1]);
             }
         }
     };
@@ -430,8 +430,12 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
             // log 2): until then no exponential exceeds 2^8
             float scale[2];
             if constexpr (FMT == kInt8) {
-                scale[0] = a.score_scale * cur.ks[0];
-                scale[1] = a.score_scale * cur.ks[1];
+                // (a block that is not there has read another's, which may be NaN)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (cur.n[j] == 0) cur.ks[j] = cur.vs[j] = 1.f;
+                    scale[j] = a.score_scale * cur.ks[j];
+                }
             } else {
                 scale[0] = scale[1] = a.score_scale;
             }
