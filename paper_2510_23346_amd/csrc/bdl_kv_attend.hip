@@ -94,16 +94,6 @@ struct Line {
 // by side, and the smaller or larger one of each half
 __device__ __forceinline__ float below_bf16(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t min_u16x2(uint32_t x, uint32_t y) {
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
-}
-
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t x, uint32_t y) {
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
-}
-
 // A tile: two blocks of 16 entries, each within one page, of one head of one
 // sequence
 struct Tile {

@@ -180,4 +180,14 @@ __device__ __forceinline__ float2 load_through2(__amdgpu_buffer_rsrc_t r, unsign
     return float2{__uint_as_float(v[0]), __uint_as_float(v[1])};
 }
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t x, uint32_t y) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+}
+
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t x, uint32_t y) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+}
+
 }  // namespace bdl

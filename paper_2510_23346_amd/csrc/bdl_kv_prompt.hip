@@ -283,9 +283,10 @@ struct Rows {
     }
 
     // products with 32 keys of LDS, rows r on: lane has entries 8 (i / 4) + 4 lh + i % 4
-    __device__ __forceinline__ void read(const u32x4* keys, int r, u32x4 (&k)[KS]) const {
+    // (ln: the lane, for LDS addresses)
+    __device__ __forceinline__ void read(const u32x4* keys, int r, u32x4 (&k)[KS], int ln) const {
 #pragma unroll
-        for (int x = 0; x < KS; ++x) k[x] = keys[k_at<D>(r + lr, 2 * x + lh)];
+        for (int x = 0; x < KS; ++x) k[x] = keys[k_at<D>(r + (ln & 31), 2 * x + (ln >> 5))];
     }
     __device__ __forceinline__ f32x16 products(const u32x4 (&k)[KS]) const {
         f32x16 s = f32x16{};
@@ -348,7 +349,7 @@ struct Rows {
         asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(sum));
     }
     // out^T += V^T P^T over 32 values of LDS, rows r on
-    __device__ __forceinline__ void add(const u32x4* values, int r, const u32x4 (&pb)[2]) {
+    __device__ __forceinline__ void add(const u32x4* values, int r, const u32x4 (&pb)[2], int ln) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -356,12 +357,35 @@ struct Rows {
                 s16x4 v[2];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int at = v32_at<D>(r + 16 * k + 8 * x + 4 * lh + ((l & 15) >> 2), 4 * dt + 2 * ((l >> 4) & 1) + ((l >> 1) & 1));
-                    v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(reinterpret_cast<const short*>(values + at) + 4 * (l & 1)));
+                    const int at = v32_at<D>(r + 16 * k + 8 * x + 4 * (ln >> 5) + ((ln & 15) >> 2), 4 * dt + 2 * ((ln >> 4) & 1) + ((ln >> 1) & 1));
+                    v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(reinterpret_cast<const short*>(values + at) + 4 * (ln & 1)));
                 }
                 o[dt] = mfma32(__builtin_bit_cast(u32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), pb[k], o[dt]);
             }
     }
+    // Infinities and NaN among `n` values of LDS, those of the entries from e0 on, are
+    // added to the rows that see them as they are (any probability times them is they)
+    __device__ __forceinline__ void poison(const KvPromptArgs& a, const u32x4* values, int n, const Tile& t, int e0, unsigned there) {
+        int hh = lh;
+        asm volatile("" : "+v"(hh));
+#pragma unroll 1
+        for (int k = 0; k < n; ++k) {
+            const int e = e0 + k;
+            const bool in = e <= min(t.hi - 1, p) && e >= t.lo && (!a.window || e > p - a.window || e < a.sinks) && (there >> (k / 16) & 1);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint2 v = reinterpret_cast<const uint2*>(values + v32_at<D>(k, 4 * dt + i))[hh];
+                    const float x[4] = {__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                                        __uint_as_float(v.y & 0xffff0000u)};
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) o[dt][4 * i + z] += in && !(fabsf(x[z]) < INFINITY) ? x[z] : 0.f;
+                    __builtin_amdgcn_sched_barrier(0);          // (registers: one read at a time)
+                }
+        }
+    }
+    // output numbers of part dt of the row, and with the first its lse
     // output numbers of part dt of the row, and with the first its lse
     __device__ __forceinline__ void finish(const KvPromptArgs& a, int dt, const f32x16& v, float top, float total) const {
         const bool none = total == 0.f;
@@ -487,6 +511,20 @@ struct Blocks {
     __device__ __forceinline__ unsigned long long at(int x) const { return (unsigned long long)lane_of(at_hi, x) << 32 | lane_of(at_lo, x); }
 };
 
+// Whether a bf16 number of eight is an infinity or a NaN, and zeros in place of such
+__device__ __forceinline__ uint32_t size_of(u32x4 v) {
+    return max_u16x2(max_u16x2(v[0] & 0x7fff7fffu, v[1] & 0x7fff7fffu), max_u16x2(v[2] & 0x7fff7fffu, v[3] & 0x7fff7fffu));
+}
+__device__ __forceinline__ bool infinite(uint32_t size) { return (size & 0xffffu) >= 0x7f80u || size >= 0x7f800000u; }
+__device__ __forceinline__ u32x4 finite_only(u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
+        if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
+    }
+    return v;
+}
+
 template <int FMT>
 __device__ __forceinline__ u32x4 widen(u32x4 v, int half) {
     return FMT == kFp8 ? bf16_of(v[2 * half], v[2 * half + 1]) : bf16_of_int8(v[2 * half], v[2 * half + 1]);
@@ -602,6 +640,28 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
 #pragma unroll
         for (int x = 0; x < PIECES; ++x) piece(buf, ct, x);
     };
+    // A tile that not all of the workgroup's rows see whole: an infinite value must not
+    // reach those that do not see it, as 0 times it would.  It is added to those that
+    // do apart, and then is zero for the products
+    const int all1 = nS + ((at0 + it.r0 / G + 1 - base) >> 6);
+    const int all0 = nS + ((max(span.begin, a.window ? at0 + (it.r0 + rows - 1) / G - a.window + 1 : 0) - base + kKeys - 1) >> 6);
+    auto edge = [&](int ct) __attribute__((always_inline)) { return FMT != kInt8 && (ct < all0 || ct >= all1); };
+    auto clean = [&](int buf, int ct) __attribute__((always_inline)) {
+        u32x4* const values = lds[buf][1];
+        uint32_t size = 0;
+#pragma unroll 1
+        for (int i = 0; i < BUF / NT; ++i) size = max_u16x2(size, size_of(values[i * NT + (int)threadIdx.x]));
+        if (infinite(size)) *flag = 1;              // (stays so: the tiles behind this one are looked at for nothing)
+        __syncthreads();
+        if (!*flag) return;
+        const Tile t = tile_at(span, kKeys, ct);
+        // (of the waves with the same rows one)
+        if (busy && half == 0) R.poison(a, values, kKeys, t, t.e, there);
+        __syncthreads();
+#pragma unroll 1
+        for (int i = 0; i < BUF / NT; ++i) values[i * NT + (int)threadIdx.x] = finite_only(values[i * NT + (int)threadIdx.x]);
+        __syncthreads();
+    };
     // the loaded tile is in LDS for all waves
     auto arrive = [&](auto buf, int ct) __attribute__((always_inline)) {
         if constexpr (FMT != kBf16) {
@@ -640,13 +700,13 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
             // two halves of 32 entries, so that the matrix products of one go on
             // beside the exponentials of the other
             u32x4 k0[KS], k1[KS], p0[2], p1[2];
-            R.read(keys, 0, k0);
-            if (FMT == kBf16) R.read(keys, 32, k1);
+            R.read(keys, 0, k0, l);
+            if (FMT == kBf16) R.read(keys, 32, k1, l);
             f32x16 s0 = f32x16{}, s1 = f32x16{};
 #pragma unroll
             for (int x = 0; x < 2 * KS; ++x) {
                 // (8-bit formats: the loads' registers leave no room for it sooner)
-                if (FMT != kBf16 && x == KS) R.read(keys, 32, k1);
+                if (FMT != kBf16 && x == KS) R.read(keys, 32, k1, l);
                 if (x < KS)
                     s0 = mfma32(k0[x], R.q[x], s0);
                 else
@@ -665,14 +725,24 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
                 R.rescale(R.follow(top));
                 R.exponentials(s0, scale(0), scale(1), vs, p0);
             }
-            R.add(values, 0, p0);
+            R.add(values, 0, p0, l);
             R.exponentials(s1, scale(2), scale(3), vs + 2, p1);
-            R.add(values, 32, p1);
+            R.add(values, 32, p1, l);
+            // (reads of LDS well ahead of the products, and the exponentials among
+            // them: without this order, which the compiler leaves where registers are
+            // short, 532 us take the place of 517)
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+            for (int x = 0; x < 4 * DT; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);
+            }
         } else {
             const float k2[2] = {half ? ks[2] : ks[0], half ? ks[3] : ks[1]}, v2[2] = {half ? vs[2] : vs[0], half ? vs[3] : vs[1]};
             const float f0 = FMT == kInt8 ? a.score_scale * k2[0] : a.score_scale, f1 = FMT == kInt8 ? a.score_scale * k2[1] : a.score_scale;
             u32x4 k[KS], pb[2];
-            R.read(keys, 32 * half, k);
+            R.read(keys, 32 * half, k, l);
             f32x16 s = f32x16{};
 #pragma unroll
             for (int x = 0; x < KS; ++x) {
@@ -686,56 +756,65 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
             const float top = R.top_of(s, f0, f1);
             if (R.passes(top)) R.rescale(R.follow(top));
             R.exponentials(s, f0, f1, v2, pb);
-            R.add(values, 32 * half, pb);
+            R.add(values, 32 * half, pb, l);
         }
     };
     // Any tile: half by half
     auto any = [&](int buf, int ct) __attribute__((always_inline)) {
-        load(buf ^ 1, ct + 1);
-        if (!busy || ct >= past || (ct >= nS && ct < gone)) return;
+        const bool some = busy && ct < past && (ct < nS || ct >= gone);
+        const bool late = FMT == kBf16 && some;     // the next tile's loads behind the first reads of this one
+        if (!late) load(buf ^ 1, ct + 1);
+        if (edge(ct)) clean(buf, ct);
+        if (!some) return;
         const u32x4 *const keys = lds[buf][0], *const values = lds[buf][1];
         const Tile t = tile_at(span, kKeys, ct);
+        const bool all = there == 15u && ct >= whole0 && ct < whole1;
+        int ln = l;
+        asm volatile("" : "+v"(ln));                // (addresses of its own, that take no registers of the other tiles)
 #pragma unroll 1
         for (int h = RW == 4 ? 0 : half; h < (RW == 4 ? 2 : half + 1); ++h) {
             const float k2[2] = {h ? ks[2] : ks[0], h ? ks[3] : ks[1]}, v2[2] = {h ? vs[2] : vs[0], h ? vs[3] : vs[1]};
+            const float f0 = FMT == kInt8 && all ? a.score_scale * k2[0] : a.score_scale, f1 = FMT == kInt8 && all ? a.score_scale * k2[1] : a.score_scale;
             u32x4 k[Rows<D, FMT>::KS], pb[2];
-            R.read(keys, 32 * h, k);
+            R.read(keys, 32 * h, k, ln);
+            if (late && (RW < 4 || h == 0)) load(buf ^ 1, ct + 1);
             f32x16 s = R.products(k);
-            R.mask(a, s, t, t.e + 32 * h, there >> (2 * h), k2);
-            const float top = R.top_of(s, a.score_scale, a.score_scale);
+            if (!all) R.mask(a, s, t, t.e + 32 * h, there >> (2 * h), k2);
+            const float top = R.top_of(s, f0, f1);
             if (R.passes(top)) R.rescale(R.follow(top));
-            R.exponentials(s, a.score_scale, a.score_scale, v2, pb);
-            R.add(values, 32 * h, pb);
+            R.exponentials(s, f0, f1, v2, pb);
+            R.add(values, 32 * h, pb, ln);
         }
     };
     constexpr std::integral_constant<int, 0> buf0{};
     constexpr std::integral_constant<int, 1> buf1{};
+    if (threadIdx.x == 0) *flag = 0;                // (behind the first tile's barrier it is so for all)
     if (c1 > c0) {
         look(c0 & ~15);
         turn(c0 & ~15);
         load(0, c0);
     }
     arrive(0, c0);
-    // (waves leave the loops at tiles of their own: each passes as many barriers)
-    const int from_whole = busy ? max(c0, whole0) : c1, to_whole = busy ? min(c1, whole1) : c0;
+    // (waves leave the inner loop at tiles of their own: each passes as many barriers.
+    // Tiles that some row of the workgroup does not see whole are not for it)
+    const int from_whole = busy ? max(c0, max(whole0, all0)) : c1, to_whole = busy ? min(c1, min(whole1, all1)) : c0;
     int ct = c0;
 #pragma unroll 1
-    for (; ct < c1 && (ct < from_whole || ((ct - c0) & 1)); ++ct) {
-        any((ct - c0) & 1, ct);
-        arrive((ct - c0 + 1) & 1, ct + 1);
-    }
+    while (ct < c1) {
+        if (ct >= from_whole && ((ct - c0) & 1) == 0) {
 #pragma unroll 1
-    while (ct + 2 <= to_whole && there == 15u) {
-        whole(buf0, ct);
-        arrive(buf1, ++ct);
-        if (there != 15u) break;
-        whole(buf1, ct);
-        arrive(buf0, ++ct);
-    }
-#pragma unroll 1
-    for (; ct < c1; ++ct) {
+            while (ct < to_whole && there == 15u) {
+                whole(buf0, ct);
+                arrive(buf1, ++ct);
+                if (ct >= to_whole || there != 15u) break;
+                whole(buf1, ct);
+                arrive(buf0, ++ct);
+            }
+            if (ct >= c1) break;
+        }
         any((ct - c0) & 1, ct);
-        arrive((ct - c0 + 1) & 1, ct + 1);
+        ++ct;
+        arrive((ct - c0) & 1, ct);
     }
     R.sum += __shfl_xor(R.sum, 32);
     bool mine = busy && wr0 + R.lr < r1;
@@ -867,19 +946,31 @@ __device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, in
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        load(i + 1);
         const bool whole = here == 3u && t.e >= t.lo && t.e + kNarrow <= t.hi && t.e + kNarrow - 1 <= R.first &&
                            (!a.window || t.e > R.last - a.window || t.e + kNarrow <= a.sinks);
+        if (FMT != kInt8 && !whole) {
+            // (as for wide tiles)
+            uint32_t size = 0;
+#pragma unroll 2
+            for (int k = 0; k < BUF / 64; ++k) size = max_u16x2(size, size_of(values[k * 64 + l]));
+            if (__any(infinite(size))) {
+                R.poison(a, values, kNarrow, t, t.e, here);
+#pragma unroll 1
+                for (int k = 0; k < BUF / 64; ++k) values[k * 64 + l] = finite_only(values[k * 64 + l]);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+        }
+        load(i + 1);
         const float f0 = FMT == kInt8 && whole ? a.score_scale * k2[0] : a.score_scale, f1 = FMT == kInt8 && whole ? a.score_scale * k2[1] : a.score_scale;
         u32x4 k[Rows<D, FMT>::KS];
-        R.read(keys, 0, k);
+        R.read(keys, 0, k, l);
         f32x16 s = R.products(k);
         if (!whole) R.mask(a, s, t, t.e, here, k2);
         const float top = R.top_of(s, f0, f1);
         if (R.passes(top)) R.rescale(R.follow(top));
         u32x4 pb[2];
         R.exponentials(s, f0, f1, v2, pb);
-        R.add(values, 0, pb);
+        R.add(values, 0, pb, l);
     }
     // the four waves' sums, each in its own part of LDS, added in order; wave dt has
     // part dt of the outputs

@@ -166,6 +166,49 @@ def test_what_is_not_seen_may_be_anything(torch):
     _prompt(torch, dc, [30, 1], 4, window=50, sinks=7)[0].close()
 
 
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,length,window", [(20, 20, 0), (7, 150, 0), (300, 310, 0), (300, 310, 40), (150, 150, 9)])
+def test_infinite_and_nan_entries_reach_only_the_rows_that_see_them(torch, fmt, d, new, length, window):
+    # an entry in the middle of the new tokens: a NaN among its values, then an infinity, then a NaN key; int8: its whole block
+    for kind in ("value nan", "value inf", "key nan") if fmt == "bf16" else ("value nan", "key nan"):
+        dc = DrawnCache([length, 40], 1, d, 16, seed=length + d, **FORMATS[fmt])
+        at = length - new + 2 * new // 3
+        page, place = dc.where(0)
+        stored, plain = (dc.K, dc.k) if "key" in kind else (dc.V, dc.v)
+        if fmt == "int8":
+            dc.S[page[at], 0, place[at] // 16, 0 if "key" in kind else 1] = np.nan
+            plain[0][0, at // 16 * 16:at // 16 * 16 + 16] = np.nan
+        else:
+            stored[page[at], 0, place[at], 5] = {"bf16": 0x7F80 if "inf" in kind else 0x7FC0, "fp8": 0x7F}[fmt]
+            plain[0][0, at, 5] = np.inf if "inf" in kind else np.nan
+        hq, T = 4, new + 40
+        cache, table, lens = dc.device(n_q_heads=hq, weights=False)
+        q, x = _queries(torch, T, hq, d, 3)
+        out, lse = torch.zeros_like(q), torch.zeros((T, hq), device="cuda")
+        cache.attend_prompt(q, _i32(torch, [0, new, T]), table, lens, out, window=window, lse=lse)
+        o, z = device_to_float(out).astype(np.float64).reshape(T, hq, d), lse.cpu().numpy()
+        _compare(o[new:], z[new:], x[new:], dc.k[1], dc.v[1], d ** -0.5, okv.sees(40, 40, window), 8, "other sequence")
+        seen = okv.sees(length, new, window)
+        hit = seen[:, at // 16 * 16:at // 16 * 16 + 16].any(1) if fmt == "int8" else seen[:, at]
+        assert hit.any() and (fmt == "int8" or not hit.all())
+        k0, v0 = (np.nan_to_num(y[0], nan=0.0, posinf=0.0) for y in (dc.k, dc.v))
+        _compare(o[:new][~hit], z[:new][~hit], x[:new][~hit], k0, v0, d ** -0.5, seen[~hit], 8, kind)
+        mine = o[:new][hit]
+        if kind == "key nan":
+            assert np.isnan(mine).all()
+        elif fmt == "int8":
+            assert np.isnan(mine).all()
+        else:
+            # the number's own column is not finite (where its probability is not nothing), the others are right
+            assert not np.isfinite(mine[..., 5]).all()
+            ref, _, mag = okv.attend_rows(x[:new][hit], k0, v0, d ** -0.5, seen[hit])
+            others = np.arange(d) != 5
+            tol = 2.0 ** -8 * np.abs(ref) + 2.0 ** -7 * mag
+            assert (np.abs(mine - ref) <= tol)[..., others].all(), kind
+        cache.close()
+
+
 def test_scores_far_apart_and_infinite(torch):
     dc = DrawnCache([200], 1, 64, 16, seed=10)
     page, place = dc.where(0)
