@@ -1,6 +1,11 @@
 """Decode steps of one decoder layer's attention block on one shard.
 
-    python examples/decode_layer.py --model 8b --batch 64 --context 2048 --steps 50 [--budget 1024] [--fp8]
+    python examples/decode_layer.py --model 8b --batch 64 --context 2048 --steps 50 [--budget 1024] [--fp8 | --int8]
+        [--window 1024 --sinks 4] [--norm]
+
+A prompt's tokens go through the same in chunks: the qkv projection, the entry
+into the cache, the attention of all of them (KVCache.attend_prompt) and the o
+projection.
 
 A step is what a serving engine runs for each new token of a batch in which
 every request names its own adapter: the qkv projection (Pool.forward_shard),
@@ -8,7 +13,8 @@ the rotary embedding and entry into the cache (KVCache.append), attention over
 the cache (KVCache.attend) and the o projection, whose output is the shard's
 partial of the tensor-parallel sum.  With a budget the steps keep account of
 the attention that every entry gets and evict what got least (a prompt's
-entries begin with none: its own attention is not computed here).  The step is
+entries begin with none: its own attention adds no weights).  With a window they
+attend to the last entries and the first few (sinks).  The step is
 captured once into a HIP graph and replayed.  Weights, adapters and
 activations are random, the shapes those of the Llama models.
 """
@@ -37,9 +43,10 @@ class AttentionBlock:
     ``room``: the most entries a sequence may hold (before an eviction)."""
 
     def __init__(self, projs, head_dim, batch, room, *, page_size=64, slots=4, rank=16, budget=0, recent=0, fp8=False,
-                 theta=500000.0, positions=16384, seed=0):
+                 int8=False, window=0, sinks=0, norm=False, theta=500000.0, positions=16384, seed=0):
         self.qkv, self.o = projs
         self.batch, self.budget, self.recent = batch, budget, recent
+        self.window, self.sinks = window, sinks
         hq, hkv = self.qkv.slices[0] // head_dim, self.qkv.slices[1] // head_dim
         g = torch.Generator(device="cuda").manual_seed(seed)
         rand = lambda shape, std: (torch.randn(shape, generator=g, device="cuda") * std).to(torch.bfloat16)  # noqa: E731
@@ -59,14 +66,18 @@ class AttentionBlock:
         width = -(-room // page_size)
         scale = {"k_scale": 0.02, "v_scale": 0.02} if fp8 else {}
         self.cache = bd.KVCache(hq, hkv, head_dim, batch * width, page_size, batch, weights=budget > 0,
-                                fmt=bd.KV_FP8_E4M3 if fp8 else bd.KV_BF16, **scale)
+                                fmt=bd.KV_INT8 if int8 else bd.KV_FP8_E4M3 if fp8 else bd.KV_BF16, **scale)
+        # weights of the heads' norms, where the model has them
+        self.norms = {}
+        if norm:
+            self.norms = {k: (1 + rand((head_dim,), 0.1).float()).to(torch.bfloat16) for k in ("q_norm", "k_norm")}
         self.table = torch.randperm(batch * width, generator=g, device="cuda").to(torch.int32).view(batch, width)
         f = theta ** (-torch.arange(0, head_dim, 2, device="cuda", dtype=torch.float64) / head_dim)
         angle = torch.arange(positions, device="cuda", dtype=torch.float64)[:, None] * f
         self.cos, self.sin = angle.cos().float(), angle.sin().float()
         # state of the batch, on the device: a captured step reads and updates it
         i32 = lambda: torch.zeros(batch, dtype=torch.int32, device="cuda")  # noqa: E731
-        self.lens, self.index, self.positions = i32(), i32(), i32()
+        self.lens, self.index, self.positions, self.starts = i32(), i32(), i32(), i32()
         self.seqs = torch.arange(batch, dtype=torch.int32, device="cuda")
         self.x = rand((batch, self.qkv.d_in), 1.0)
         self.qkv_out = rand((batch, self.qkv.d_out), 0.0)
@@ -75,15 +86,22 @@ class AttentionBlock:
         self.out = rand((batch, self.o.d_out), 0.0)
 
     def prompt(self, seq, x, slot, start=0):
-        """Enter the keys and values of a prompt's tokens ``start`` on (``x``:
-        their activations [n, d_in]); the prompt's own attention is the
-        engine's business."""
+        """A prompt's tokens ``start`` on (``x``: their activations [n, d_in]):
+        their entry into the cache, their attention to it and the o projection's
+        partial [n, d_out], which is returned."""
         n = x.shape[0]
-        qkv = torch.empty((n, self.qkv.d_out), dtype=torch.bfloat16, device="cuda")
+        rows = lambda p: torch.empty((n, p.d_out), dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        qkv, out = rows(self.qkv), rows(self.o)
+        q = qkv[:, :self.qkv.slices[0]]
         at = torch.arange(start, start + n, dtype=torch.int32, device="cuda")
-        self.pool.forward_shard(0, x, self.packed[0], None, qkv, segs=bd.Segments([0], [n], [slot]))
-        self.cache.append(qkv, self.cos, self.sin, torch.full_like(at, seq), at, at, self.table, self.lens,
-                          qkv[:, :self.qkv.slices[0]])
+        segs = bd.Segments([0], [n], [slot])
+        self.pool.forward_shard(0, x, self.packed[0], None, qkv, segs=segs)
+        self.cache.append(qkv, self.cos, self.sin, torch.full_like(at, seq), at, at, self.table, self.lens, q, **self.norms)
+        attn = torch.empty((n, self.o.d_in), dtype=torch.bfloat16, device="cuda")
+        self.cache.attend_prompt(q, torch.tensor([0, n], dtype=torch.int32, device="cuda"), self.table[seq:seq + 1],
+                                 self.lens[seq:seq + 1], attn, window=self.window, sinks=self.sinks)
+        self.pool.forward_shard(1, attn, self.packed[1], None, out, segs=segs)
+        return out
 
     def begin(self):
         """After the prompts: where the next token of each sequence goes."""
@@ -93,8 +111,11 @@ class AttentionBlock:
     def step(self):
         self.pool.forward_shard(0, self.x, self.packed[0], self.ids, self.qkv_out)
         self.cache.append(self.qkv_out, self.cos, self.sin, self.seqs, self.index, self.positions, self.table, self.lens,
-                          self.q)
-        self.cache.attend(self.q, self.table, self.lens, self.attn, accumulate=self.budget > 0)
+                          self.q, **self.norms)
+        if self.window:
+            torch.sub(self.lens, self.window, out=self.starts)          # (below zero: from the first on)
+        self.cache.attend(self.q, self.table, self.lens, self.attn, starts=self.starts if self.window else None,
+                          sinks=self.sinks, accumulate=self.budget > 0)
         self.pool.forward_shard(1, self.attn, self.packed[1], self.ids, self.out)
         if self.budget:
             self.cache.evict(self.table, self.lens, self.budget, self.recent)
@@ -123,11 +144,16 @@ def main():
     ap.add_argument("--page-size", type=int, default=64)
     ap.add_argument("--budget", type=int, default=0, help="entries to keep per sequence and kv head (0: all)")
     ap.add_argument("--recent", type=int, default=64)
-    ap.add_argument("--fp8", action="store_true", help="8-bit cache")
+    ap.add_argument("--fp8", action="store_true", help="8-bit cache (e4m3, one scale)")
+    ap.add_argument("--int8", action="store_true", help="8-bit cache (a scale for each 16 entries of a head; no budget)")
+    ap.add_argument("--window", type=int, default=0, help="entries that are attended to (0: all)")
+    ap.add_argument("--sinks", type=int, default=0, help="first entries that stay visible beside the window")
+    ap.add_argument("--norm", action="store_true", help="norms of the query and key heads")
     a = ap.parse_args()
     projs, d = shard_projs(a.model, a.tp)
     block = AttentionBlock(projs, d, a.batch, a.context + a.steps + 8, page_size=a.page_size, budget=a.budget,
-                           recent=min(a.recent, a.budget), fp8=a.fp8, positions=a.context + a.steps + 8)
+                           recent=min(a.recent, a.budget), fp8=a.fp8, int8=a.int8, window=a.window,
+                           sinks=a.sinks, norm=a.norm, positions=a.context + a.steps + 8)
     g = torch.Generator(device="cuda").manual_seed(1)
     for s in range(a.batch):
         for at in range(0, a.context, 1024):        # the pool takes 1024 tokens a call: longer prompts in chunks

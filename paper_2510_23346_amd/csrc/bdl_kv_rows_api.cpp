@@ -14,6 +14,7 @@ int bdlora_kv_read(bdlora_kv_t c, const int32_t* seqs, const int32_t* index, int
         const long long row = (long long)c->d.n_kv_heads * c->d.head_dim;
         if (int rc = check_rows(k_out, k_stride, row, "k_out")) return rc;
         if (int rc = check_rows(v_out, v_stride, row, "v_out")) return rc;
+        if (k_out == v_out) return api_fail(BDLORA_ERR_INVALID_ARG, "k_out and v_out must not be the same memory");
         if (!seqs || !index || !aligned(seqs, 4) || !aligned(index, 4))
             return api_fail(BDLORA_ERR_INVALID_ARG, "seqs and index must be int32 device arrays");
         if (n_seqs < 1) return api_fail(BDLORA_ERR_INVALID_ARG, "n_seqs must be positive");
@@ -55,7 +56,7 @@ int bdlora_kv_attend_prompt(bdlora_kv_t c, const void* q, int64_t q_stride, int3
             return api_fail(BDLORA_ERR_INVALID_ARG, "lens and q_starts must be int32, lse fp32 device arrays");
         if (int rc = check_table(c, table, table_stride, table_width)) return rc;
         // (rows of a kv head, one for each token and query head, are counted in 32 bits)
-        if ((long long)T * c->d.n_q_heads > INT32_MAX / 2)
+        if ((long long)T * c->d.n_q_heads > 1LL << 30)
             return api_fail(BDLORA_ERR_SHAPE, "more than 2^30 rows: T x query heads");
         Device guard(c->device);
         if (!guard.ok) return api_fail(BDLORA_ERR_HIP, "hipSetDevice failed");
@@ -73,7 +74,7 @@ int bdlora_kv_attend_prompt(bdlora_kv_t c, const void* q, int64_t q_stride, int3
         a.part = c->part;
         a.count = c->count;
         a.split = 0;
-        a.window = window;
+        a.window = std::min(window, 1 << 30);         // (no row sees more, and an entry's number less it fits 32 bits)
         a.sinks = window ? sinks : 0;         // (without a window every entry is attended to)
         // (kept above zero: masked scores are -infinity, times the scale too)
         a.score_scale = (float)std::max(std::fabs((double)scale * c->d.k_scale * 1.4426950408889634), 1e-37);

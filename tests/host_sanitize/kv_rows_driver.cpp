@@ -141,14 +141,15 @@ int main() {
     pro([](P& x) { x.t = nullptr; }, INV, "null table");
     pro([](P& x) { x.tw = 5; }, INV, "width beyond the stride");
     pro([](P& x) { x.ts = x.tw = 1 << 25; }, SH, "more than 2^30 entries");
-    pro([](P& x) { x.T = 1 << 28; }, SH, "more than 2^30 rows");
+    pro([](P& x) { x.T = (1 << 27) + 1; }, SH, "more than 2^30 rows");
+    pro([](P& x) { x.T = 1 << 27; }, HIP, "2^30 rows");
 
     // read
     struct R {
         bdlora_kv_t c;
         const int *s, *ix; int T; const int* t; int64_t ts; int tw, ns; void* k; int64_t ks; void* v; int64_t vs;
     };
-    const R r0{&c, i, i, 3, i, 4, 4, 2, p, 2 * 128, p, 2 * 128};
+    const R r0{&c, i, i, 3, i, 4, 4, 2, p, 2 * 128, mem + 2048, 2 * 128};
     auto rd = [&](auto change, int want, const char* what) {
         R r = r0;
         change(r);
@@ -165,6 +166,7 @@ int main() {
     rd([](R& r) { r.ks = 2 * 128 - 8; }, INV, "k stride");
     rd([](R& r) { r.vs = 2 * 128 + 1; }, INV, "v stride");
     rd([](R& r) { r.ns = 0; }, INV, "no sequences");
+    rd([](R& r) { r.v = r.k; }, INV, "one memory for both");
     rd([](R& r) { r.tw = 0; }, INV, "no width");
     std::printf("%d checks, %d failed checks\n", checks, failed);
     return failed != 0;

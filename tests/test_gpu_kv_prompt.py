@@ -108,7 +108,7 @@ def test_group_sizes(torch, hq, hkv):
     _prompt(torch, dc, [20, 9, 1], hq, window=11, sinks=3, seed=hq)[0].close()
 
 
-@pytest.mark.parametrize("B", [1, 63, 64, 65, 200])
+@pytest.mark.parametrize("B", [1, 63, 64, 65, 200, 256, 257, 700])
 def test_many_sequences(torch, B):
     rng = np.random.default_rng(B)
     lens = rng.integers(0, 90, B)
@@ -225,10 +225,10 @@ def test_invalid_arguments_on_the_device(torch):
     cache, table, lens = dc.device(n_q_heads=4, weights=False)
     q, x = _queries(torch, 100, 4, 128, 3)
 
-    def call(begin, table=table, lens=lens):
+    def call(begin, table=table, lens=lens, **more):
         out = torch.full((100, 512), 7.0, dtype=torch.bfloat16, device="cuda")
         lse = torch.full((100, 4), 7.0, device="cuda")
-        cache.attend_prompt(q, _i32(torch, begin), table, lens, out, lse=lse)
+        cache.attend_prompt(q, _i32(torch, begin), table, lens, out, lse=lse, **more)
         err = cache.device_error()
         return device_to_float(out).astype(np.float64).reshape(100, 4, 128), lse.cpu().numpy(), err
 
@@ -248,9 +248,10 @@ def test_invalid_arguments_on_the_device(torch):
                 continue                              # rows 60..70 belong to two sequences
             right(o, z, b, r0, r1)
     # more tokens than entries: the first see nothing
-    o, z, err = call([0, 0, 0, 100])
-    assert err == 1 and (o[:60] == 0).all() and (z[:60] == -np.inf).all()
-    right(o, z, 2, 60, 100)
+    for more in ({}, {"window": 2 ** 31 - 1, "sinks": 2 ** 31 - 1}, {"window": 2 ** 31 - 1}):
+        o, z, err = call([0, 0, 0, 100], **more)
+        assert err == 1 and (o[:60] == 0).all() and (z[:60] == -np.inf).all()
+        right(o, z, 2, 60, 100)
     # lengths beyond the row and below zero
     o, z, err = call([0, 10, 20, 30], lens=_i32(torch, [-3, 60, 40]))
     assert err == 1 and (o[:10] == 0).all()

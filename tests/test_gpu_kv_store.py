@@ -292,6 +292,8 @@ def test_refusals(torch):
         cache.attend(q, table, lens, torch.empty_like(q), accumulate=True)
     k, v = (torch.zeros((2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
     i = _i32(torch, [0, 1])
+    with pytest.raises(bd.BDLoRAError):
+        cache.read(i, i, table, k, k)
     for change in (dict(k_out=k[:1]), dict(v_out=v.float()), dict(seqs=i[:1]), dict(index=i.long()), dict(table=table.cpu())):
         with pytest.raises(ValueError):
             cache.read(**{**dict(seqs=i, index=i, table=table, k_out=k, v_out=v), **change})
