@@ -553,7 +553,7 @@ int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_b
  * null, and not the memory of seqs, index or positions, which are still read
  * while it changes): lens[seqs[t]] = max(lens[seqs[t]], index[t] + 1).  No two tokens of a call may become the same entry.  (Cache with a scale for
  * each block: those of one sequence that become entries of one block stand one
- * after the other in the call, by ascending entry.)  A token whose position is outside the
+ * after the other in the call, by ascending entry; T x (n_kv_heads + 2) <= 2^25 - 8.)  A token whose position is outside the
  * tables is not stored and its query row is zero.  Strides: multiples of 8;
  * qkv, q_out, cos, sin 16-byte aligned.
  * Errors: INVALID_ARG, SHAPE, HIP. */
@@ -618,7 +618,8 @@ int bdlora_kv_attend_sinks(bdlora_kv_t cache, const void* q, int64_t q_stride, i
  * not overlap).  A row without an entry of its own (more rows than entries: error
  * flag) gives 0 and lse -infinity; rows of no sequence are left as they are.
  * Probabilities enter the sum over values as bf16 (8 significant bits), their
- * sum and lse do not.  Nothing is accumulated.  T x n_q_heads <= 2^30.
+ * sum and lse do not.  Nothing is accumulated.  T x n_q_heads <= 2^30, B x
+ * n_kv_heads < 2^23.
  * Errors: INVALID_ARG, SHAPE, HIP. */
 int bdlora_kv_attend_prompt(bdlora_kv_t cache, const void* q, int64_t q_stride, int32_t T, const int32_t* q_starts, int32_t B,
                             const int32_t* table, int64_t table_stride, int32_t table_width, const int32_t* lens, int32_t window,

@@ -130,6 +130,9 @@ int append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const void* q_nor
             return api_fail(BDLORA_ERR_INVALID_ARG, "eps must be finite and not negative");
         if (n_seqs < 1) return api_fail(BDLORA_ERR_INVALID_ARG, "n_seqs must be positive");
         if (int rc = check_table(c, table, table_stride, table_width)) return rc;
+        // (a grid holds less than 2^24 workgroups of 256: T for queries, T x kv heads / 2 for blocks at most)
+        if (c->scales && (long long)T * (c->d.n_kv_heads + 2) > (1LL << 25) - 8)
+            return api_fail(BDLORA_ERR_SHAPE, "more than 2^25 - 8: T x (kv heads + 2)");
         Device guard(c->device);
         if (!guard.ok) return api_fail(BDLORA_ERR_HIP, "hipSetDevice failed");
         bdl::KvAppendArgs a;

@@ -201,6 +201,9 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
             }
     }
     if (bad) kv_error(a.c);
+    // (starts that do not ascend can name more rows than the grid is for, and a share
+    // that nobody brings would be waited for in the next call: nothing is cut then)
+    const int split = __any(bad) ? 0 : a.split;
     const int both = units[0] > 0.f && units[1] > 0.f ? 2 : 1;
     const float part_of[2] = {fmaxf(1.f, units[0] * heads / (float)(share_items(ROWS) / both)),
                               fmaxf(1.f, units[1] * heads / (float)(share_items(kNarrow) / both))};
@@ -215,7 +218,7 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
             for (int x = 0; x < C; ++x) {
                 if (x > 0 && c0 + 64 * x >= a.B) continue;
                 const unsigned tiles = p[x].narrow == (kind == 1) ? p[x].tiles : 0u;
-                unsigned parts = tiles ? parts_of((float)p[x].units, part_of[kind], kind, a.split) : 1u;
+                unsigned parts = tiles ? parts_of((float)p[x].units, part_of[kind], kind, split) : 1u;
                 const unsigned need = parts > 1 ? (unsigned)fminf((float)tiles * (float)parts * heads * (float)per, 1e6f) : 0u;
                 const unsigned slot_incl = slots + (unsigned)wave_incl_scan((int)need);
                 if (slot_incl > (unsigned)kKvPromptSlots) parts = 1;          // (what finds no slots is not cut)
@@ -385,7 +388,6 @@ struct Rows {
                 }
         }
     }
-    // output numbers of part dt of the row, and with the first its lse
     // output numbers of part dt of the row, and with the first its lse
     __device__ __forceinline__ void finish(const KvPromptArgs& a, int dt, const f32x16& v, float top, float total) const {
         const bool none = total == 0.f;

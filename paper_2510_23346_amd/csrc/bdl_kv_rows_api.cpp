@@ -58,6 +58,9 @@ int bdlora_kv_attend_prompt(bdlora_kv_t c, const void* q, int64_t q_stride, int3
         // (rows of a kv head, one for each token and query head, are counted in 32 bits)
         if ((long long)T * c->d.n_q_heads > 1LL << 30)
             return api_fail(BDLORA_ERR_SHAPE, "more than 2^30 rows: T x query heads");
+        // (and a grid holds less than 2^24 workgroups of 256)
+        if ((long long)B * c->d.n_kv_heads >= 1LL << 23)
+            return api_fail(BDLORA_ERR_SHAPE, "2^23 sequences' heads or more: B x kv heads");
         Device guard(c->device);
         if (!guard.ok) return api_fail(BDLORA_ERR_HIP, "hipSetDevice failed");
         bdl::KvPromptArgs a;

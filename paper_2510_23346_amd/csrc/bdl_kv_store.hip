@@ -237,7 +237,7 @@ template <int D>
 hipError_t store(const KvAppendArgs& a, hipStream_t s) {
     const int units = a.c.hq * (D / 16), rows = std::max(1, 256 / units);
     const long long q_groups = ((long long)a.T + rows - 1) / rows, blocks = ((long long)a.T * 2 * a.c.hkv + 3) / 4;
-    if (q_groups + blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (q_groups + blocks >= 1 << 24) return hipErrorInvalidValue;
     if (a.q_norm)
         kv_store_kernel<D, true><<<(int)(q_groups + blocks), 256, 0, s>>>(a, (int)q_groups, rows);
     else

@@ -91,6 +91,9 @@ int main() {
     app([](A& a) { a.eps = INFINITY; }, INV, "eps infinite");
     app([](A& a) { a.c = nullptr; }, INV, "null cache");
     app([&](A& a) { a.qkv = mem + 8; }, INV, "misaligned qkv");
+    app([](A& a) { a.T = (1 << 23) - 1; }, SH, "more tokens than a grid is for");
+    app([](A& a) { a.T = (1 << 23) - 2; }, HIP, "as many");
+    app([&](A& a) { a.c = &plain, a.T = 1 << 23; }, HIP, "to bf16");
 
     // sinks
     auto att = [&](bdlora_kv_t cc, int B, const int* starts, int sinks, int acc, int want, const char* what) {
@@ -143,6 +146,11 @@ int main() {
     pro([](P& x) { x.ts = x.tw = 1 << 25; }, SH, "more than 2^30 entries");
     pro([](P& x) { x.T = (1 << 27) + 1; }, SH, "more than 2^30 rows");
     pro([](P& x) { x.T = 1 << 27; }, HIP, "2^30 rows");
+    bdlora_kv many = c;
+    many.d.n_q_heads = many.d.n_kv_heads = 256;
+    many.d.max_seqs = 65535;
+    pro([&](P& x) { x.c = &many, x.qs = x.os = 256 * 128, x.B = 1 << 15; }, SH, "2^23 sequences' heads");
+    pro([&](P& x) { x.c = &many, x.qs = x.os = 256 * 128, x.B = (1 << 15) - 1; }, HIP, "fewer");
 
     // read
     struct R {

@@ -267,6 +267,22 @@ def test_invalid_arguments_on_the_device(torch):
     cache.close()
 
 
+def test_overlapping_rows_leave_the_next_call_right(torch):
+    # rows of many sequences on top of each other, more than q has: whatever that
+    # gives, the calls behind it, whose sequences are cut into stretches, are right
+    dc = DrawnCache([3000, 1100], 1, 64, 16, seed=13)
+    cache, table, lens = dc.device(n_q_heads=4, weights=False, max_seqs=600)
+    q, x = _queries(torch, 100, 4, 64, 2)
+    out = torch.zeros_like(q)
+    tables, lengths = table[:1].repeat(600, 1), lens[:1].repeat(600)
+    for rows in (100, 8):
+        cache.attend_prompt(q, _i32(torch, [0, rows] * 300 + [0]), tables, lengths, out)
+        assert cache.device_error() == 1
+        for new in ([100, 70], [3, 5]):
+            _prompt(torch, dc, new, 4, device=(cache, table, lens))
+    cache.close()
+
+
 def test_another_stream_and_graph_replays(torch):
     dc = DrawnCache([300, 120, 500], 2, 128, 64, seed=12, int8=True)
     cache, table, lens = dc.device(n_q_heads=8)
