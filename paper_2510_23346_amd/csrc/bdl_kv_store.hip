@@ -68,17 +68,15 @@ __device__ __forceinline__ void unpack_int8(const uint32_t (&w)[N / 4], Piece<N>
 
 constexpr float kLeast = 5.421010862427522e-20f;     // 2^-64
 
-// One block: token t (of an entry there is) and the tokens of its run behind it
+// One block: that of token t, entry i0 of row seq (which there is), and of the tokens
+// of its run behind it
 template <int D, bool NORM>
-__device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int kh, bool value) {
+__device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int seq, int i0, int kh, bool value) {
 #pragma clang fp contract(off)
     constexpr int N = D / 8;
-    const int l = threadIdx.x & 63, r = l >> 2, c = l & 3, cap = a.c.width << a.c.ps_shift;
-    // three trips to memory: where the token goes; the page, the run and its rows;
-    // what the block holds and the angles
-    const int seq = a.seqs[t], i0 = a.index[t], before_t = max(t - 1, 0), seq1 = a.seqs[before_t], i1 = a.index[before_t];
-    if (seq < 0 || seq >= a.n_seqs || i0 < 0 || i0 >= cap) return;
-    if (t > 0 && (i0 & (kKvBlock - 1)) && seq1 == seq && i1 == i0 - 1) return;     // not the run's first
+    const int l = threadIdx.x & 63, r = l >> 2, c = l & 3;
+    // (two trips to memory: the page, the run and its rows; what the block holds and
+    // the angles)
     const int j = r - (i0 & (kKvBlock - 1)), tok = min(t + max(j, 0), a.T - 1), d0 = N * c, d1 = D / 2 + N * c;
     const int page = a.c.table[(long long)seq * a.c.tstride + (i0 >> a.c.ps_shift)];
     const int seq_r = a.seqs[tok], index_r = a.index[tok], pos_r = a.positions[tok];
@@ -191,15 +189,31 @@ __device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int kh
     }
 }
 
-// Workgroups z = 0 take 256 / units tokens' queries, as append does; the others
-// (z > 0) four waves: of token x / 2 hkv .. the head and whether keys or values
-template <int D, bool NORM>
-__global__ __launch_bounds__(256) void kv_store_kernel(const KvAppendArgs a, int q_groups, int q_rows) {
+// The first `q_groups` workgroups take `q_rows` tokens' queries each, as append does.
+// A wave of the others has a head's keys or values of a token, and leaves if that is
+// not the first of a block's run.  MANY: of 16 tokens, `step` (1 more than a multiple of
+// 16) apart, so that runs that begin together have their firsts in different waves; each
+// lane looks at one
+template <int D, bool NORM, bool MANY>
+__global__ __launch_bounds__(256) void kv_store_kernel(const KvAppendArgs a, int q_groups, int q_rows, int step) {
 #pragma clang fp contract(off)
     if ((int)blockIdx.x >= q_groups) {
         const long long unit = (long long)(blockIdx.x - q_groups) * 4 + wave_id();
-        const int per = 2 * a.c.hkv, t = (int)(unit / per), u = (int)(unit - (long long)t * per);
-        if (t < a.T) store_block<D, NORM>(a, t, u >> 1, u & 1);
+        const int per = 2 * a.c.hkv, t0 = (int)(unit / per), u = (int)(unit - (long long)t0 * per), cap = a.c.width << a.c.ps_shift;
+        if (t0 >= step) return;
+        const int l = threadIdx.x & 63, t = MANY ? t0 + min(l, kKvBlock - 1) * step : t0, at_t = min(t, a.T - 1), before = max(at_t - 1, 0);
+        const int seq = a.seqs[at_t], at = a.index[at_t], seq1 = a.seqs[before], at1 = a.index[before];
+        bool first = seq >= 0 && seq < a.n_seqs && at >= 0 && at < cap;
+        if (t > 0 && (at & (kKvBlock - 1)) && seq1 == seq && at1 == at - 1) first = false;
+        if constexpr (MANY) {
+#pragma unroll 1
+            for (unsigned long long m = __ballot(first && l < kKvBlock && t < a.T); m; m &= m - 1) {
+                const int x = (int)__builtin_ctzll(m);
+                store_block<D, NORM>(a, t0 + x * step, __builtin_amdgcn_readlane(seq, x), __builtin_amdgcn_readlane(at, x), u >> 1, u & 1);
+            }
+        } else if (first) {
+            store_block<D, NORM>(a, t0, seq, at, u >> 1, u & 1);
+        }
         return;
     }
     constexpr int P = D / 16;
@@ -236,12 +250,22 @@ __global__ __launch_bounds__(256) void kv_store_kernel(const KvAppendArgs a, int
 template <int D>
 hipError_t store(const KvAppendArgs& a, hipStream_t s) {
     const int units = a.c.hq * (D / 16), rows = std::max(1, 256 / units);
-    const long long q_groups = ((long long)a.T + rows - 1) / rows, blocks = ((long long)a.T * 2 * a.c.hkv + 3) / 4;
+    const long long q_groups = ((long long)a.T + rows - 1) / rows, waves = (long long)a.T * 2 * a.c.hkv;
+    // 16 tokens a wave where waves for one each would wait for room, most of them to leave
+    // again; not where many tokens may be the only ones of their sequences, whose blocks
+    // such a wave stores one by one.  (Heads of 128, one token and 16 a wave: 8 prompts of
+    // 512 of one kv head 13.4 and 10.6 us, of 1024 21.7 and 17.0; of 8 kv heads 4 of 512
+    // 31 and 18, 4 of 1024 beside 192 single tokens 56 and 41, one of 10240 147 and 76, 2000
+    // single tokens 60 and 83; the 4 of 1024 beside 192, of one kv head, 14.3 and 18.6)
+    const bool many = (waves > 4096 && a.T >= 64LL * a.n_seqs) || (waves > 16384 && a.T >= 4LL * a.n_seqs);
+    const int step = many ? ((a.T + kKvBlock - 1) / kKvBlock + kKvBlock - 2) / kKvBlock * kKvBlock + 1 : a.T;
+    const long long blocks = ((long long)step * 2 * a.c.hkv + 3) / 4;
     if (q_groups + blocks >= 1 << 24) return hipErrorInvalidValue;
+    auto run = [&](auto kernel) { kernel<<<(int)(q_groups + blocks), 256, 0, s>>>(a, (int)q_groups, rows, step); };
     if (a.q_norm)
-        kv_store_kernel<D, true><<<(int)(q_groups + blocks), 256, 0, s>>>(a, (int)q_groups, rows);
+        many ? run(kv_store_kernel<D, true, true>) : run(kv_store_kernel<D, true, false>);
     else
-        kv_store_kernel<D, false><<<(int)(q_groups + blocks), 256, 0, s>>>(a, (int)q_groups, rows);
+        many ? run(kv_store_kernel<D, false, true>) : run(kv_store_kernel<D, false, false>);
     return hipGetLastError();
 }
 

@@ -133,6 +133,34 @@ def test_batch_sizes(torch, T):
     s.cache.close()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_prompts(torch, d):
+    # runs that begin anywhere in a block, single tokens and padding between them, a position outside in the middle of one
+    dc = DrawnCache([0, 5, 31, 0, 48], 2, d, 64, seed=d, int8=True, room=[1000, 901, 300, 17, 1])
+    s = Stored(torch, dc, 4, n_positions=1001)
+    seqs = [0] * 1000 + [-1] * 3 + [1] * 901 + [4] + [2] * 300 + [3] * 17 + [-1]
+    index = list(range(1000)) + [0, 1, 2] + list(range(5, 906)) + [48] + list(range(31, 331)) + list(range(17)) + [17]
+    positions = list(index)
+    positions[1500] = 1001
+    stored = [b >= 0 and positions[t] < 1001 for t, b in enumerate(seqs)]
+    assert len(seqs) == len(index) == 2223
+    s.append(seqs, index, positions, 1, stored=stored)
+    s.check(err=1)
+    s.cache.close()
+
+
+def test_many_heads_of_prompts_and_single_tokens(torch):
+    lens = [0, 70] + [3 + t % 40 for t in range(230)]
+    dc = DrawnCache(lens, 8, 64, 16, seed=6, int8=True, room=[400, 411] + [1] * 230)
+    s = Stored(torch, dc, 8, n_positions=500)
+    seqs = [0] * 400 + list(range(2, 100)) + [1] * 411 + list(range(100, 232))
+    index = list(range(400)) + lens[2:100] + list(range(70, 481)) + lens[100:]
+    for step in range(2):
+        s.append(seqs, index, index, step, size=1.0 + step)
+        s.check()
+    s.cache.close()
+
+
 def test_tokens_that_are_not_stored(torch):
     # positions and places outside, in the middle of a run; a page that is none; zeros
     dc = DrawnCache([0, 10, 20, 40], 1, 64, 16, seed=3, int8=True, room=40)
