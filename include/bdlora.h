@@ -477,8 +477,8 @@ int bdlora_last_path(bdlora_pool_t pool, int32_t* path);
  *
  * Device-side errors (a page number outside 0 .. n_pages - 1 under an entry
  * that is used, a length or index beyond the table's row, a position outside
- * the tables, a seq outside the table, rows that are not ascending) raise the cache's sticky error flag
- * (bdlora_kv_get_device_error); nothing outside the arrays is read or
+ * the tables, a seq outside the table, q_starts that do not ascend) raise the
+ * cache's sticky error flag (bdlora_kv_get_device_error); nothing outside the arrays is read or
  * written: the entry counts as not there, the length is cut to what the row
  * can name, the token is not stored.
  *
@@ -487,7 +487,7 @@ int bdlora_last_path(bdlora_pool_t pool, int32_t* path);
 typedef struct bdlora_kv* bdlora_kv_t;
 
 /* Cache formats: bf16, or 8 bits (e4m3) that stand for k_scale (v_scale)
- * times their value.  Queries, inputs and outputs are bf16 either way, and
+ * times their value.  Queries, inputs and outputs are bf16 in all formats, and
  * all sums and the softmax fp32. */
 #define BDLORA_KV_BF16     0
 #define BDLORA_KV_FP8_E4M3 1
@@ -533,8 +533,8 @@ int bdlora_kv_create_blocks(const bdlora_kv_desc* desc, void* k, void* v, float*
 /* Free the workspace (waits for the device's work). */
 int bdlora_kv_destroy(bdlora_kv_t cache);
 
-/* Bytes of one page (k and v and a block cache's scales, with `weights` weight and pos too) and of the
- * workspace.  Pure host function; either pointer may be null. */
+/* Bytes of one page (k and v and a block cache's scales, with `weights` weight
+ * and pos too) and of the workspace.  Pure host function; either pointer may be null. */
 int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_bytes, int64_t* workspace_bytes);
 
 /* Rotary embedding of T new tokens and their entry into the cache.

@@ -12,7 +12,9 @@
 // heads.  A wave's products are S^T = K Q^T and O^T = V^T P^T (32x32x16, bf16): a
 // row's scores lie in one lane (and the one 32 further), so that maximum and sum
 // need no exchange, and they are already those of the second product's operand.
-// The probabilities are rounded to bf16 for it (their sum is not).
+// The probabilities are rounded to bf16 for it (their sum is not): half a step of 2^-8
+// each, which the sum of many averages out.  Two bf16 numbers for each, as single
+// tokens have three, would take the second product twice, half as much time again.
 //
 // Wide tiles: a workgroup has 128 (or 64) rows, 32 a wave, whose four waves share
 // tiles of 64 entries in LDS, two of them in turn: one is worked on while the next
@@ -25,6 +27,16 @@
 // entries are cut into stretches for several workgroups.  They leave sums, maxima and
 // outputs in the workspace; the last one to come adds them, in the order of the
 // entries.
+//
+// Measured: one prompt of 8192 with 32 query heads of 128 on 8 kv heads 517 to 538 us
+// (two cards), 1.02 to 1.06 PFLOP/s, where a large matrix product has 1.25; the
+// matrix units are busy half of the time, at a clock that power holds near 2.0 GHz
+// (32 cycles a product beside 5.6 vector instructions, so what one wave does not
+// cover another one has to).  16384 with a window of 4096 beside 4 sinks, 8 heads on
+// one 263 to 272 us.  4 prompts of 1024 beside 192 single tokens, e4m3, 36 us; 8 of
+// 512, 4 heads on one, 16.4; 64 sequences of 5 new tokens behind 2100 entries each,
+// int8, 23.6: about 8 us are the chain to the first tile (starts and lengths, pages,
+// entries) and the end, and 8 more where stretches are joined.
 #include <type_traits>
 
 #include "bdl_kv_device.h"
@@ -1042,11 +1054,13 @@ hipError_t launch(KvPromptArgs a, hipStream_t s) {
     const long long G = a.c.hq / a.c.hkv, seqs = std::min(a.T, a.B);
     auto tiles = [&](int rows) { return (a.T * G / rows + seqs) * a.c.hkv; };
     // 64 rows a workgroup where 128 would leave compute units without, or with one long
-    // tile beside a short one.  (4 heads of 128 on one kv head, 64 and 128 rows: 8 prompts of
+    // tile beside a short one.  (Single tokens beside prompts are not counted in the second
+    // number.  4 heads of 128 on one kv head, 64 and 128 rows: 8 prompts of
     // 1024 29.0 and 30.4 us, 12 of them 46.8 and 42.3, 24 71.8 and 61.9; of 4096, 2 72.7 and
-    // 80.3, 4 107 and 119)
+    // 80.3, 4 107 and 119; 4 of 1024 beside 192 single tokens 28 and 35, with 8 heads 37 and
+    // 37, in e4m3 40 and 37.5)
     const long long wide = tiles(128);
-    const bool half = wide < 320 || (wide < 768 && a.T * G / 128 >= 64 * seqs);
+    const bool half = wide < 320 || a.T * G * a.c.hkv < 256 * 128 || (wide < 768 && a.T * G / 128 >= 64 * seqs);
     const long long items = half ? tiles(64) : wide;
     a.split = items < 1024;
     // (stretches are at most one a tile more than the items they were made for)

@@ -21,6 +21,11 @@ namespace {
 //
 // Rotation and norm are those of the bf16 cache, and queries are dealt with by
 // threads of the same launch as there.
+//
+// Bound by the trips to memory of an owner (which token, its run and page, then the
+// block and the angles) and the waves that find they are none: 4288 tokens of 8 + 1 + 1
+// heads of 128, 22 MB read and written, 10.9 to 11.8 us, where the bf16 cache's launch
+// takes 8.5; 10240 tokens of 32 + 8 + 8 heads, 235 MB, 76 us, 3.1 TB/s.
 template <int N>
 struct Piece {
     float x[N];
@@ -273,8 +278,8 @@ hipError_t store(const KvAppendArgs& a, hipStream_t s) {
 // Entries as bf16: the stored number times its scale, rounded once.  A thread
 // takes 8 numbers of a row (one 16-byte store, so that a wave's covers whole lines:
 // 32 bytes a thread 99 us where these take 91), of R rows in turn, whose loads are
-// in flight together.  Bound by its memory traffic: 278528 entries of two kv heads
-// of 128, 454 MB read and written, 91 us, 5.0 TB/s (a large copy 5.2).
+// in flight together.  Bound by its memory traffic: 293888 entries of two kv heads
+// of 128, 454 MB read and written, 90 us, 5.0 TB/s (a large copy 5.2).
 template <int D, int FMT, int R>
 __global__ __launch_bounds__(256) void kv_read_kernel(const KvReadArgs a) {
 #pragma clang fp contract(off)
