@@ -130,6 +130,12 @@ struct Prompt {
     int t0, n, len;
     unsigned tiles, units;
     bool narrow, bad;
+    // from n: the kind and number of its tiles
+    template <int ROWS>
+    __device__ __forceinline__ void count(int G) {
+        narrow = n * G <= kNarrow;
+        tiles = (unsigned)(n * G + (narrow ? kNarrow : ROWS) - 1) / (narrow ? kNarrow : ROWS);
+    }
 };
 
 template <int ROWS>
@@ -142,10 +148,9 @@ __device__ __forceinline__ Prompt prompt_of(const KvPromptArgs& a, int b, int G)
     p.n = t1 - p.t0;
     p.len = min(max(n, 0), cap);
     p.bad = p.t0 != u0 || t1 != u1 || p.len != n || p.n > p.len;
-    const int rows = b >= 0 && b < a.B ? p.n * G : 0;
-    p.narrow = rows <= kNarrow;
+    if (b < 0 || b >= a.B) p.n = 0;
+    p.count<ROWS>(G);
     const int size = p.narrow ? kNarrow : ROWS;
-    p.tiles = (unsigned)(rows + size - 1) / size;
     const Span s(a, p.len - p.n + (int)((max(p.tiles, 1u) - 1) * size / (unsigned)G), p.len - 1);
     p.units = p.tiles == 0 ? 0u : p.narrow ? (unsigned)(s.tiles(kNarrow) + NW - 1) / NW : (unsigned)s.tiles(kKeys);
     return p;
@@ -173,16 +178,31 @@ struct Item {
 
 // The workgroup's item; b -1: there is none.  All workgroups see the same plan.
 // Wide tiles come first; the last sequence's last tile, which sees most, before
-// the others
-template <int ROWS>
-__device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned item, int kvh) {
-    constexpr int C = 4;                // sequences a lane has at once (more are looked up again)
+// the others.  Up to kMine sequences each wave looks up by itself; of more, the first
+// HELD (from the last on) are looked up by the four waves together and kept in LDS, with
+// the tiles of each 64 of them.  (All looked up by each wave, again for each kind: 300
+// sequences of 16 tokens 27.5 us where these take 16, 1500 of 8 tokens 158 and 59)
+constexpr int kMine = 256;
+
+template <int ROWS, int HELD>
+__device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned item, int kvh, u32x4* held, int (*groups)[64], float2 (*stat)[32]) {
+    constexpr int C = kMine / 64;       // sequences a lane has at once
     const int l = threadIdx.x & 63, hkv = a.c.hkv;
     const float heads = (float)hkv;
+    const bool together = a.B > kMine;
     Prompt p[C];
     auto at = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < C; ++x) p[x] = prompt_of<ROWS>(a, a.B - 1 - c0 - 64 * x - l, G);
+    };
+    auto again = [&](int c0) __attribute__((always_inline)) {
+        if (c0 >= HELD) return at(c0);
+#pragma unroll
+        for (int x = 0; x < C; ++x) {
+            const u32x4 v = held[c0 + 64 * x + l];
+            p[x].t0 = (int)v[0], p[x].n = (int)v[1], p[x].len = (int)v[2], p[x].units = v[3];
+            p[x].count<ROWS>(G);
+        }
     };
     Item it;
     it.b = -1;
@@ -194,8 +214,18 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
     // units of work of either kind
     float units[2] = {0.f, 0.f};
     bool bad = false;
-    for (int c0 = 0; c0 < a.B; c0 += 64 * C) {
+    // (together: a wave's share of the sequences, the sums of all of them at the end)
+    const int w = wave_id();
+    for (int c0 = together ? kMine * w : 0; c0 < a.B; c0 += together ? kMine * NW : kMine) {
         at(c0);
+        if (together && c0 < HELD)
+#pragma unroll
+            for (int y = 0; y < C; ++y) {
+                held[c0 + 64 * y + l] = u32x4{(unsigned)p[y].t0, (unsigned)p[y].n, (unsigned)p[y].len, p[y].units};
+                const int n0 = wave_total(wave_incl_scan(p[y].narrow ? 0 : (int)p[y].tiles));
+                const int n1 = wave_total(wave_incl_scan(p[y].narrow ? (int)p[y].tiles : 0));
+                if (l == 0) groups[0][c0 / 64 + y] = n0, groups[1][c0 / 64 + y] = n1;
+            }
         float x[2] = {0.f, 0.f};
 #pragma unroll
         for (int y = 0; y < C; ++y) {
@@ -213,19 +243,60 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
             }
     }
     if (bad) kv_error(a.c);
+    if (together) {
+        if (l == 0) stat[w][0] = float2{units[0], units[1]};
+        const bool some = __any(bad);
+        if (l == 0) stat[w][1] = float2{some ? 1.f : 0.f, 0.f};
+        __syncthreads();
+        units[0] = units[1] = 0.f;
+#pragma unroll
+        for (int y = 0; y < NW; ++y) {
+            units[0] += stat[y][0].x, units[1] += stat[y][0].y;
+            bad |= stat[y][1].x != 0.f;
+        }
+    }
     // (starts that do not ascend can name more rows than the grid is for, and a share
     // that nobody brings would be waited for in the next call: nothing is cut then)
     const int split = __any(bad) ? 0 : a.split;
     const int both = units[0] > 0.f && units[1] > 0.f ? 2 : 1;
     const float part_of[2] = {fmaxf(1.f, units[0] * heads / (float)(share_items(ROWS) / both)),
                               fmaxf(1.f, units[1] * heads / (float)(share_items(kNarrow) / both))};
+    if (together && !split && a.B <= HELD) {
+        // nothing is cut: the group of 64 sequences, then the one of them
+        const bool in = 64 * l < (a.B + kMine - 1) / kMine * kMine;
+        unsigned left = item;
+#pragma unroll 1
+        for (int kind = 0; kind < 2; ++kind) {
+            const unsigned n = in ? (unsigned)groups[kind][l] : 0u, incl = (unsigned)wave_incl_scan((int)n);
+            const unsigned long long over = __ballot(incl > left);
+            if (over) {
+                const int g = __ffsll((long long)over) - 1;
+                left -= lane_of(incl - n, g);
+                Prompt q;
+                const u32x4 v = held[64 * g + l];
+                q.t0 = (int)v[0], q.n = (int)v[1], q.len = (int)v[2];
+                q.count<ROWS>(G);
+                const unsigned tiles = q.narrow == (kind == 1) ? q.tiles : 0u, upto = (unsigned)wave_incl_scan((int)tiles);
+                const int i = __ffsll((long long)__ballot(upto > left)) - 1;
+                it.b = a.B - 1 - 64 * g - i;
+                it.t0 = __builtin_amdgcn_readlane(q.t0, i);
+                it.n = __builtin_amdgcn_readlane(q.n, i);
+                it.len = __builtin_amdgcn_readlane(q.len, i);
+                it.narrow = kind == 1;
+                it.r0 = (int)((lane_of(upto, i) - 1 - left) * (kind ? kNarrow : ROWS));
+                return it;
+            }
+            left -= lane_of(incl, 63);
+        }
+        return it;
+    }
     unsigned before = 0, slots = 0;
 #pragma unroll 1
     for (int kind = 0; kind < 2; ++kind) {
         const unsigned per = kind ? 2 : ROWS / 16;                // slots of a share
 #pragma unroll 1
-        for (int c0 = 0; c0 < a.B; c0 += 64 * C) {
-            if (a.B > 64 * C) at(c0);
+        for (int c0 = 0; c0 < a.B; c0 += kMine) {
+            if (together) again(c0);
 #pragma unroll
             for (int x = 0; x < C; ++x) {
                 if (x > 0 && c0 + 64 * x >= a.B) continue;
@@ -1039,10 +1110,11 @@ template <int D, int FMT, bool PAGE, int RW>
 __global__ __launch_bounds__(NT, 2) void kv_prompt_kernel(const KvPromptArgs a) {
     __shared__ u32x4 lds[2][2][kKeys * D / 8];
     __shared__ float2 stat[NW][32];
-    __shared__ int flag;
+    __shared__ int flag, groups[2][64];
     const int hkv = a.c.hkv, G = a.c.hq / hkv, kvh = blockIdx.x % hkv;
-    const Item it = item_of<RW * 32>(a, G, blockIdx.x / hkv, kvh);
+    const Item it = item_of<RW * 32, 4 * kKeys * D / 8>(a, G, blockIdx.x / hkv, kvh, lds[0][0], groups, stat);
     if (it.b < 0) return;
+    if (a.B > kMine) __syncthreads();               // (LDS is for tiles from here on)
     if (it.narrow)
         narrow<D, FMT>(a, it, kvh, G, lds[0][0], stat, &flag);
     else
@@ -1062,7 +1134,7 @@ hipError_t launch(KvPromptArgs a, hipStream_t s) {
     const long long wide = tiles(128);
     const bool half = wide < 320 || a.T * G * a.c.hkv < 256 * 128 || (wide < 768 && a.T * G / 128 >= 64 * seqs);
     const long long items = half ? tiles(64) : wide;
-    a.split = items < 1024;
+    a.split = items < 1024 && (a.c.width << a.c.ps_shift) > 15 * kKeys;     // (shorter ones are not cut)
     // (stretches are at most one a tile more than the items they were made for)
     const int grid = (int)(items + (a.split ? share_items(half ? 64 : 128) + share_items(kNarrow) + 16 : 0));
     if (half)

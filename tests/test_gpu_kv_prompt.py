@@ -108,7 +108,7 @@ def test_group_sizes(torch, hq, hkv):
     _prompt(torch, dc, [20, 9, 1], hq, window=11, sinks=3, seed=hq)[0].close()
 
 
-@pytest.mark.parametrize("B", [1, 63, 64, 65, 200, 256, 257, 700])
+@pytest.mark.parametrize("B", [1, 63, 64, 65, 200, 256, 257, 700, 2048, 2100])
 def test_many_sequences(torch, B):
     rng = np.random.default_rng(B)
     lens = rng.integers(0, 90, B)
@@ -116,6 +116,17 @@ def test_many_sequences(torch, B):
     new[-1:] = lens[-1:]
     dc = DrawnCache(lens, 1, 64, 16, seed=B)
     _prompt(torch, dc, [int(x) for x in new], 4)[0].close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_ones_among_many_sequences(torch, d):
+    # (those of 2500 entries are cut into stretches)
+    lens = np.random.default_rng(d).integers(1, 60, 300)
+    new = np.minimum(lens, np.random.default_rng([d, 1]).integers(0, 30, 300))
+    for b, n in ((3, 4), (150, 40), (299, 1)):
+        lens[b], new[b] = 2500 + b, n
+    dc = DrawnCache(lens, 2, d, 16, seed=d)
+    _prompt(torch, dc, [int(x) for x in new], 6, behind=2)[0].close()
 
 
 @pytest.mark.parametrize("fmt", list(FORMATS))
