@@ -51,10 +51,11 @@ constexpr int NW = 4, NT = NW * 64;     // waves and threads of a workgroup, of 
 constexpr int kKeys = 64;               // entries of a wide tile
 constexpr int kNarrow = 32;             // rows, and entries of a wave's tile, of a narrow one
 
-// Stretches: as many as give this many workgroups work.  A share takes a slot of 16
-// rows' sums for each 16 rows, and half of the slots are for wide tiles where there
-// are both kinds
-constexpr int share_items(int rows) { return kKvPromptSlots / (rows / 16) / 2; }
+// Stretches: about as many as give this many workgroups work, two a compute unit (a
+// share takes a slot of the workspace for each 16 rows).  A wide tile's beginning counts
+// as this many units, the end of one that is cut as kJoin
+constexpr int kCutItems = 512, kCutNarrow = 384;
+constexpr float kEnds = 6.f, kJoin = 8.f;
 
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -125,17 +126,23 @@ __device__ __forceinline__ Tile tile_at(const Span& s, int size, int ct) {
 }
 
 // A sequence: its first row of q, new tokens, length; its tiles of rows and the
-// stretches' units (of 64 entries, narrow 128) of the last of them
+// stretches' units (of 64 entries, narrow 128) of the last of them and of the first
 struct Prompt {
     int t0, n, len;
-    unsigned tiles, units;
+    unsigned tiles, units, units0;
     bool narrow, bad;
-    // from n: the kind and number of its tiles
+    // what follows from n and len
     template <int ROWS>
-    __device__ __forceinline__ void count(int G) {
-        narrow = n * G <= kNarrow;
-        tiles = (unsigned)(n * G + (narrow ? kNarrow : ROWS) - 1) / (narrow ? kNarrow : ROWS);
+    __device__ __forceinline__ void count(const KvPromptArgs& a, int G) {
+        const int rows = n * G, size = rows <= kNarrow ? kNarrow : ROWS, at0 = len - n;
+        narrow = rows <= kNarrow;
+        tiles = (unsigned)(rows + size - 1) / size;
+        const Span s(a, at0 + (int)((max(tiles, 1u) - 1) * size / (unsigned)G), len - 1), s0(a, at0, at0 + (min(rows, size) - 1) / G);
+        units = tiles == 0 ? 0u : narrow ? (unsigned)(s.tiles(kNarrow) + NW - 1) / NW : (unsigned)s.tiles(kKeys);
+        units0 = tiles == 0 || narrow ? units : (unsigned)s0.tiles(kKeys);
     }
+    // of all tiles, about (a wide one's beginning and end take as long as kEnds units)
+    __device__ __forceinline__ float work() const { return (float)tiles * (0.5f * (float)(units + units0) + (narrow ? 0.f : kEnds)); }
 };
 
 template <int ROWS>
@@ -149,22 +156,44 @@ __device__ __forceinline__ Prompt prompt_of(const KvPromptArgs& a, int b, int G)
     p.len = min(max(n, 0), cap);
     p.bad = p.t0 != u0 || t1 != u1 || p.len != n || p.n > p.len;
     if (b < 0 || b >= a.B) p.n = 0;
-    p.count<ROWS>(G);
-    const int size = p.narrow ? kNarrow : ROWS;
-    const Span s(a, p.len - p.n + (int)((max(p.tiles, 1u) - 1) * size / (unsigned)G), p.len - 1);
-    p.units = p.tiles == 0 ? 0u : p.narrow ? (unsigned)(s.tiles(kNarrow) + NW - 1) / NW : (unsigned)s.tiles(kKeys);
+    p.template count<ROWS>(a, G);
     return p;
 }
 
-// Stretches of a tile of `units`, where `part` units each give all the workgroups
-// that the workspace has shares for work: no more than about the root of the units,
+// The last `tiles` of a sequence's tiles of rows are cut into `parts` stretches, where
+// `part` units each give all workgroups work: no more than about the root of the units,
 // since the last one reads all shares, and none of short tiles, since leaving and
 // joining takes about 8 us, and a unit 1 to 1.2.  (64 tokens of 4 heads behind 2048, 4096 and
 // 32768 entries: 24, 27 and 55 us; up to twice as many stretches 27, 33 and 75, none
-// 33, 56 and 380)
-__device__ __forceinline__ unsigned parts_of(float units, float part, int narrow, int split) {
-    if (!split || units < (narrow ? 8.f : 16.f)) return 1;
-    return max(1u, (unsigned)fminf(ceilf(units / part), (narrow ? 1.4f : 1.f) * __fsqrt_rn(units)));
+// 33, 56 and 380.)  Of a wide sequence those of more than a stretch's units are cut, and
+// into longer ones where the shares would take more than the sequence's `slots`.  (One
+// prompt of 2000, 4096, 6000 and 8192 tokens of 4 heads 26, 47, 68 and 109 us, not cut 29,
+// 62, 88 and 121; with no account of the tiles' ends 4 prompts of 2000 take 50 for 41)
+struct Cut {
+    unsigned tiles, parts;
+};
+
+__device__ __forceinline__ Cut cut_of(const Prompt& p, float part, float slots, float per, int split) {
+    const float units = (float)p.units, tiles = (float)p.tiles;
+    if (p.narrow) {
+        const unsigned parts = !split || units < 8.f ? 1u : max(1u, (unsigned)fminf(ceilf(units / part), 1.4f * __fsqrt_rn(units)));
+        return Cut{parts > 1 ? p.tiles : 0u, parts};
+    }
+    Cut c{0u, 1u};
+    if (!split || units < 16.f) return c;
+    float size = fmaxf(part, 1.5f * __fsqrt_rn(units));
+    bool done = false;
+#pragma unroll 1
+    for (int i = 0; i < 6 && __any(!done); ++i) {
+        const float parts = ceilf(units / size), over = units - fmaxf(size, 12.f), slope = units - (float)p.units0;
+        const float x = slope <= over ? tiles : ceilf(tiles * over / slope);
+        if (!done && (parts < 2.f || x * parts * per <= slots)) {
+            done = true;
+            if (parts >= 2.f && x > 0.f) c = Cut{(unsigned)x, (unsigned)parts};
+        }
+        size *= 1.4f;
+    }
+    return c;
 }
 
 // What a workgroup does: a tile of rows (r0 on) of sequence b, of its entries'
@@ -200,8 +229,8 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
 #pragma unroll
         for (int x = 0; x < C; ++x) {
             const u32x4 v = held[c0 + 64 * x + l];
-            p[x].t0 = (int)v[0], p[x].n = (int)v[1], p[x].len = (int)v[2], p[x].units = v[3];
-            p[x].count<ROWS>(G);
+            p[x].t0 = (int)v[0], p[x].n = (int)v[1], p[x].len = (int)v[2];
+            p[x].template count<ROWS>(a, G);
         }
     };
     Item it;
@@ -221,7 +250,7 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
         if (together && c0 < HELD)
 #pragma unroll
             for (int y = 0; y < C; ++y) {
-                held[c0 + 64 * y + l] = u32x4{(unsigned)p[y].t0, (unsigned)p[y].n, (unsigned)p[y].len, p[y].units};
+                held[c0 + 64 * y + l] = u32x4{(unsigned)p[y].t0, (unsigned)p[y].n, (unsigned)p[y].len, 0u};
                 const int n0 = wave_total(wave_incl_scan(p[y].narrow ? 0 : (int)p[y].tiles));
                 const int n1 = wave_total(wave_incl_scan(p[y].narrow ? (int)p[y].tiles : 0));
                 if (l == 0) groups[0][c0 / 64 + y] = n0, groups[1][c0 / 64 + y] = n1;
@@ -230,7 +259,7 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
 #pragma unroll
         for (int y = 0; y < C; ++y) {
             bad |= p[y].bad;
-            const float u = (float)p[y].tiles * (float)p[y].units;
+            const float u = p[y].work();
             x[0] += p[y].narrow ? 0.f : u;
             x[1] += p[y].narrow ? u : 0.f;
         }
@@ -259,8 +288,8 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
     // that nobody brings would be waited for in the next call: nothing is cut then)
     const int split = __any(bad) ? 0 : a.split;
     const int both = units[0] > 0.f && units[1] > 0.f ? 2 : 1;
-    const float part_of[2] = {fmaxf(1.f, units[0] * heads / (float)(share_items(ROWS) / both)),
-                              fmaxf(1.f, units[1] * heads / (float)(share_items(kNarrow) / both))};
+    const float part_of[2] = {fmaxf(1.f, units[0] * heads / (float)(kCutItems / both)) + kJoin,
+                              fmaxf(1.f, units[1] * heads / (float)(kCutNarrow / both))};
     if (together && !split && a.B <= HELD) {
         // nothing is cut: the group of 64 sequences, then the one of them
         const bool in = 64 * l < (a.B + kMine - 1) / kMine * kMine;
@@ -275,7 +304,7 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
                 Prompt q;
                 const u32x4 v = held[64 * g + l];
                 q.t0 = (int)v[0], q.n = (int)v[1], q.len = (int)v[2];
-                q.count<ROWS>(G);
+                q.template count<ROWS>(a, G);
                 const unsigned tiles = q.narrow == (kind == 1) ? q.tiles : 0u, upto = (unsigned)wave_incl_scan((int)tiles);
                 const int i = __ffsll((long long)__ballot(upto > left)) - 1;
                 it.b = a.B - 1 - 64 * g - i;
@@ -301,11 +330,12 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
             for (int x = 0; x < C; ++x) {
                 if (x > 0 && c0 + 64 * x >= a.B) continue;
                 const unsigned tiles = p[x].narrow == (kind == 1) ? p[x].tiles : 0u;
-                unsigned parts = tiles ? parts_of((float)p[x].units, part_of[kind], kind, split) : 1u;
-                const unsigned need = parts > 1 ? (unsigned)fminf((float)tiles * (float)parts * heads * (float)per, 1e6f) : 0u;
+                Cut cut{0u, 1u};
+                if (tiles) cut = cut_of(p[x], part_of[kind], (float)(kKvPromptSlots / both) * p[x].work() / units[kind], heads * (float)per, split);
+                const unsigned need = (unsigned)fminf((float)cut.tiles * (float)cut.parts * heads * (float)per, 1e6f);
                 const unsigned slot_incl = slots + (unsigned)wave_incl_scan((int)need);
-                if (slot_incl > (unsigned)kKvPromptSlots) parts = 1;          // (what finds no slots is not cut)
-                const unsigned incl = before + (unsigned)wave_incl_scan((int)(tiles * parts));
+                if (slot_incl > (unsigned)kKvPromptSlots) cut = Cut{0u, 1u};  // (what finds no slots is not cut)
+                const unsigned incl = before + (unsigned)wave_incl_scan((int)(tiles + cut.tiles * (cut.parts - 1)));
                 const unsigned long long over = __ballot(incl > item);
                 if (over) {
                     const int i = __ffsll((long long)over) - 1;
@@ -313,12 +343,17 @@ __device__ __forceinline__ Item item_of(const KvPromptArgs& a, int G, unsigned i
                     it.t0 = __builtin_amdgcn_readlane(p[x].t0, i);
                     it.n = __builtin_amdgcn_readlane(p[x].n, i);
                     it.len = __builtin_amdgcn_readlane(p[x].len, i);
-                    it.parts = lane_of(parts, i);
                     it.narrow = kind == 1;
-                    const unsigned z = lane_of(incl, i) - 1 - item, tile = z / it.parts;
-                    it.part = z - tile * it.parts;
+                    const unsigned z = lane_of(incl, i) - 1 - item, parts = lane_of(cut.parts, i), uncut = lane_of(tiles - cut.tiles, i);
+                    unsigned tile = z;
+                    if (z >= uncut) {
+                        const unsigned k = (z - uncut) / parts;
+                        it.parts = parts;
+                        it.part = z - uncut - k * parts;
+                        it.slot = (int)(lane_of(slot_incl - need, i) + (k * (unsigned)hkv + (unsigned)kvh) * parts * per);
+                        tile = uncut + k;
+                    }
                     it.r0 = (int)(tile * (kind ? kNarrow : ROWS));
-                    it.slot = (int)(lane_of(slot_incl - need, i) + (tile * (unsigned)hkv + (unsigned)kvh) * it.parts * per);
                     return it;
                 }
                 before = lane_of(incl, 63);
@@ -1135,8 +1170,9 @@ hipError_t launch(KvPromptArgs a, hipStream_t s) {
     const bool half = wide < 320 || a.T * G * a.c.hkv < 256 * 128 || (wide < 768 && a.T * G / 128 >= 64 * seqs);
     const long long items = half ? tiles(64) : wide;
     a.split = items < 1024 && (a.c.width << a.c.ps_shift) > 15 * kKeys;     // (shorter ones are not cut)
-    // (stretches are at most one a tile more than the items they were made for)
-    const int grid = (int)(items + (a.split ? share_items(half ? 64 : 128) + share_items(kNarrow) + 16 : 0));
+    // (a wide stretch takes slots, of which there are so many; narrow ones are at most one a
+    // tile more than the items they are made for)
+    const int grid = (int)(items + (a.split ? kKvPromptSlots / (half ? 4 : 8) + kCutNarrow + 16 : 0));
     if (half)
         kv_prompt_kernel<D, FMT, PAGE, 2><<<grid, NT, 0, s>>>(a);
     else
