@@ -28,14 +28,14 @@
 // outputs in the workspace; the last one to come adds them, in the order of the
 // entries.
 //
-// Measured: one prompt of 8192 with 32 query heads of 128 on 8 kv heads 517 to 538 us
-// (two cards), 1.02 to 1.06 PFLOP/s, where a large matrix product has 1.25; the
+// Measured: one prompt of 8192 with 32 query heads of 128 on 8 kv heads 517 to 560 us
+// (several cards), 0.98 to 1.06 PFLOP/s, where a large matrix product has 1.25; the
 // matrix units are busy half of the time, at a clock that power holds near 2.0 GHz
 // (32 cycles a product beside 5.6 vector instructions, so what one wave does not
 // cover another one has to).  16384 with a window of 4096 beside 4 sinks, 8 heads on
-// one 263 to 272 us.  4 prompts of 1024 beside 192 single tokens, e4m3, 36 us; 8 of
+// one 263 to 281 us.  4 prompts of 1024 beside 192 single tokens, e4m3, 36.5 us; 8 of
 // 512, 4 heads on one, 16.4; 64 sequences of 5 new tokens behind 2100 entries each,
-// int8, 23.6: about 8 us are the chain to the first tile (starts and lengths, pages,
+// int8, 24: about 8 us are the chain to the first tile (starts and lengths, pages,
 // entries) and the end, and 8 more where stretches are joined.
 #include <type_traits>
 

@@ -142,6 +142,31 @@ def test_a_long_prompt(torch):
     _prompt(torch, dc, [2100], 4)[0].close()
 
 
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1300, 70)])
+def test_prompts_whose_last_rows_are_cut_into_stretches(torch, fmt, d, window, sinks):
+    dc = DrawnCache([1700, 1300, 90], 1, d, 64, seed=d + window, **FORMATS[fmt])
+    _prompt(torch, dc, [1700, 300, 2], 4, window, sinks)[0].close()
+
+
+def test_pages_beyond_four_gigabytes(torch):
+    import paper_2510_23346_amd as bd
+    n_pages, page, d = 90_000, 256, 128
+    k = torch.zeros(n_pages, 1, page, d, dtype=torch.bfloat16, device="cuda")        # 5.9 GB each
+    v = torch.zeros_like(k)
+    dc = DrawnCache([700, 300], 1, d, page, seed=15, spare=0)
+    at = np.array([n_pages - 1, 0, n_pages - 3, 89_000, 66_000], np.int32)[:dc.n_pages]
+    for x, y in ((k, dc.K), (v, dc.V)):
+        x[torch.from_numpy(at).cuda().long()] = torch.from_numpy(y.view(np.int16)).cuda().view(torch.bfloat16)
+    named = (dc.table >= 0) & (dc.table < dc.n_pages)
+    table = _i32(torch, np.where(named, at[np.clip(dc.table, 0, dc.n_pages - 1)], -1))
+    cache = bd.KVCache(4, 1, d, n_pages, page, 2, k=k, v=v)
+    for new in ([300, 7], [700, 300]):
+        _prompt(torch, dc, new, 4, device=(cache, table, _i32(torch, dc.lens)))
+    cache.close()
+
+
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
 def test_scales(torch, scale):
     dc = DrawnCache([150, 30], 1, 64, 16, seed=5)
