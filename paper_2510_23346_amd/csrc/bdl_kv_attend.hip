@@ -401,12 +401,17 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) s[j] = mfma(buf[k_at<D>(j * 16 + lr, ks * 4 + lg)], q[ks], s[j]);
             }
-            if ((cur.lo[0] | cur.lo[1]) > 0 || (cur.n[0] & cur.n[1]) != 16) {
+            // (int8: what is attended to is taken times its block's scale here, since
+            // -infinity times a scale of 0, or one that vanishes beside the scores' own, is a NaN)
+            const bool cut = (cur.lo[0] | cur.lo[1]) > 0 || (cur.n[0] & cur.n[1]) != 16;
+            if (cut) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (FMT == kInt8) s[j][e] *= cur.ks[j];
                         if (4 * lg + e < cur.lo[j] || 4 * lg + e >= cur.n[j]) s[j][e] = -INFINITY;
+                    }
             }
             if constexpr (ACC) {
                 const Heads hd = heads_of(cur.h);
@@ -433,8 +438,8 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                 // (a block that is not there has read another's, which may be NaN)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    if (cur.n[j] == 0) cur.ks[j] = cur.vs[j] = 1.f;
-                    scale[j] = a.score_scale * cur.ks[j];
+                    if (cur.n[j] == 0) cur.vs[j] = 1.f;
+                    scale[j] = cut ? a.score_scale : a.score_scale * cur.ks[j];
                 }
             } else {
                 scale[0] = scale[1] = a.score_scale;
