@@ -419,11 +419,12 @@ struct Rows {
     // times the scales of an int8 cache's blocks (which may be NaN: what does not see
     // the block must not)
     __device__ __forceinline__ void mask(const KvPromptArgs& a, f32x16& s, const Tile& t, int e0, unsigned there, const float* ks) const {
-        asm volatile("");                       // (a branch: not done and thrown away where all are seen)
+        int hh = lh;
+        asm volatile("" : "+v"(hh));            // (a branch: not done and thrown away where all are seen; no registers across the tiles)
         const int to = min(t.hi - 1, p), from = a.window ? p - a.window + 1 : 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int e = e0 + 8 * (i / 4) + 4 * lh + i % 4;
+            const int e = e0 + 8 * (i / 4) + 4 * hh + i % 4;
             const bool sees = (e <= to) & (e >= t.lo) & ((e >= from) | (e < a.sinks)) & (bool)(there >> (i / 8) & 1);
             s[i] = sees ? FMT == kInt8 ? s[i] * ks[i / 8] : s[i] : -INFINITY;
         }
@@ -484,14 +485,32 @@ struct Rows {
                 o[dt] = mfma32(__builtin_bit_cast(u32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), pb[k], o[dt]);
             }
     }
-    // Infinities and NaN among `n` values of LDS, those of the entries from e0 on, are
-    // added to the rows that see them as they are (any probability times them is they)
-    __device__ __forceinline__ void poison(const KvPromptArgs& a, const u32x4* values, int n, const Tile& t, int e0, unsigned there) {
+    // the maximum follows the scores of 32 keys of LDS, rows r on, which stand for entries e0 on of tile t
+    __device__ __forceinline__ void follow_tile(const KvPromptArgs& a, const u32x4* keys, int r, const Tile& t, int e0, unsigned there) {
+        const float ones[2] = {1.f, 1.f};
+        int ln = l;
+        asm volatile("" : "+v"(ln));
+        // (registers: one read at a time)
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+            s = mfma32(keys[k_at<D>(r + (ln & 31), 2 * x + (ln >> 5))], q[x], s);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        mask(a, s, t, e0, there, ones);
+        const float top = top_of(s, a.score_scale, a.score_scale);
+        if (passes(top)) rescale(follow(top));
+    }
+    // Infinities and NaN among the values of LDS, rows k0 .. k1 - 1 of tile t, are added
+    // to the rows that see them as they are (any probability times them is they).  After
+    // the rows' maximum has followed the tile's scores: infinity times a factor that
+    // vanishes, or the 0 that stands for no maximum yet, is a NaN
+    __device__ __forceinline__ void poison(const KvPromptArgs& a, const u32x4* values, int k0, int k1, const Tile& t, unsigned there) {
         int hh = lh;
         asm volatile("" : "+v"(hh));
 #pragma unroll 1
-        for (int k = 0; k < n; ++k) {
-            const int e = e0 + k;
+        for (int k = k0; k < k1; ++k) {
+            const int e = t.e + k;
             const bool in = e <= min(t.hi - 1, p) && e >= t.lo && (!a.window || e > p - a.window || e < a.sinks) && (there >> (k / 16) & 1);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
@@ -766,6 +785,7 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
     const int all1 = nS + ((at0 + it.r0 / G + 1 - base) >> 6);
     const int all0 = nS + ((max(span.begin, a.window ? at0 + (it.r0 + rows - 1) / G - a.window + 1 : 0) - base + kKeys - 1) >> 6);
     auto edge = [&](int ct) __attribute__((always_inline)) { return FMT != kInt8 && (ct < all0 || ct >= all1); };
+    auto some_see = [&](int ct) __attribute__((always_inline)) { return busy && ct < past && (ct < nS || ct >= gone); };
     auto clean = [&](int buf, int ct) __attribute__((always_inline)) {
         u32x4* const values = lds[buf][1];
         uint32_t size = 0;
@@ -775,8 +795,12 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
         __syncthreads();
         if (!*flag) return;
         const Tile t = tile_at(span, kKeys, ct);
-        // (of the waves with the same rows one)
-        if (busy && half == 0) R.poison(a, values, kKeys, t, t.e, there);
+        if (some_see(ct)) {
+            const int h0 = RW == 4 ? 0 : half, h1 = RW == 4 ? 2 : half + 1;
+#pragma unroll 1
+            for (int h = h0; h < h1; ++h) R.follow_tile(a, lds[buf][0], 32 * h, t, t.e + 32 * h, there >> (2 * h));
+            R.poison(a, values, 32 * h0, 32 * h1, t, there);
+        }
         __syncthreads();
 #pragma unroll 1
         for (int i = 0; i < BUF / NT; ++i) values[i * NT + (int)threadIdx.x] = finite_only(values[i * NT + (int)threadIdx.x]);
@@ -881,7 +905,7 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
     };
     // Any tile: half by half
     auto any = [&](int buf, int ct) __attribute__((always_inline)) {
-        const bool some = busy && ct < past && (ct < nS || ct >= gone);
+        const bool some = some_see(ct);
         const bool late = FMT == kBf16 && some;     // the next tile's loads behind the first reads of this one
         if (!late) load(buf ^ 1, ct + 1);
         if (edge(ct)) clean(buf, ct);
@@ -1074,7 +1098,8 @@ __device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, in
 #pragma unroll 2
             for (int k = 0; k < BUF / 64; ++k) size = max_u16x2(size, size_of(values[k * 64 + l]));
             if (__any(infinite(size))) {
-                R.poison(a, values, kNarrow, t, t.e, here);
+                R.follow_tile(a, keys, 0, t, t.e, here);
+                R.poison(a, values, 0, kNarrow, t, here);
 #pragma unroll 1
                 for (int k = 0; k < BUF / 64; ++k) values[k * 64 + l] = finite_only(values[k * 64 + l]);
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

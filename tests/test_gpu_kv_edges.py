@@ -1,9 +1,10 @@
-"""Attention where a number of the cache is a zero scale: attend and attend_prompt
-give what the formula gives.  Tolerances as in
+"""Attention where a number of the cache is a zero scale or an infinity:
+attend and attend_prompt give what the formula gives.  Tolerances as in
 test_gpu_kv_prompt.py."""
 import numpy as np
 import pytest
 
+import workloads as wl
 from oracle import kv as okv
 from test_gpu_kv_prompt import _compare, _i32, _queries, torch  # noqa: F401  (torch: a fixture)
 from workloads.gpu import device_to_float
@@ -82,4 +83,116 @@ def test_single_tokens_over_a_cache_that_holds_nothing_yet(torch):  # noqa: F811
     cache.attend(q, table, lens, out, lse=lse)
     assert not out.any()
     assert np.allclose(lse.cpu().numpy(), np.array([0, np.log(16), np.log(33), -np.inf])[:, None], atol=2.0 ** -19)
+    cache.close()
+
+
+# ------------------------------------------------ infinite values
+
+def _expect(o, z, x, dc, b, bad, scale, seen, what):
+    """Rows of sequence b, whose value (entry e, column c) is bad[e, c]: rows that see
+    infinities of one sign in a column have it, of both or a NaN a NaN; all else
+    is right (their other numbers and lse too)."""
+    special = ~np.isfinite(dc.v[b][0])
+    v0 = np.where(special, 0.0, dc.v[b][0])[None]
+    s = seen.astype(np.float64)
+    plus, minus, nan = (s @ (special & m).astype(np.float64) > 0 for m in (bad == np.inf, bad == -np.inf, np.isnan(bad)))
+    ref, rlse, mag = okv.attend_rows(x, dc.k[b], v0, scale, seen)
+    n, d = v0.shape[1], v0.shape[2]
+    for h in range(x.shape[1]):
+        got = o[:, h]
+        size = np.where(seen, np.abs(x[:, h]) @ np.abs(dc.k[b][0]).T, 0).max(1)
+        es = ((d + 4) * 2.0 ** -24 * abs(scale) * size)[:, None]
+        tol = 2.0 ** -8 * np.abs(ref[:, h]) + (2.0 ** -8 + 4 * es + 2.0 ** -19 + n * 2.0 ** -24) * mag[:, h]
+        right = np.where(nan | (plus & minus), np.isnan(got),
+                         np.where(plus, got == np.inf, np.where(minus, got == -np.inf, np.abs(got - ref[:, h]) <= tol)))
+        assert right.all(), (what, h, np.argwhere(~right)[:6], got[~right][:6])
+        tol = 2 * es[:, 0] + 2.0 ** -19 + n * 2.0 ** -24 + 2.0 ** -23 * np.abs(np.where(np.isinf(rlse[:, h]), 0, rlse[:, h]))
+        some = seen.any(1)
+        assert (np.abs(z[some, h] - rlse[some, h]) <= tol[some]).all(), (what, h)
+
+
+def _put_values(dc, b, bad):
+    """bad: (entry, column, value) of sequence b."""
+    page, place = dc.where(b)
+    bits = {np.inf: 0x7F80, -np.inf: 0xFF80}
+    for e, c, x in bad:
+        dc.V[page[e], 0, place[e], c] = bits.get(x, 0x7FC0)
+        dc.v[b][0, e, c] = x
+
+
+# tokens, entries, window; heads: sequences of one tile, of several, of narrow and wide (64 rows) tiles, cut into stretches
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("new,length,window,hq", [(1, 1, 0, 4), (5, 20, 0, 4), (7, 150, 0, 4), (20, 20, 0, 1), (20, 20, 0, 4), (64, 64, 0, 4),
+                                                  (64, 64, 9, 4), (150, 150, 0, 4), (150, 150, 9, 4), (300, 310, 40, 4), (130, 2500, 0, 4),
+                                                  (4, 3000, 0, 4), (300, 900, 0, 20)])
+def test_rows_that_see_an_infinite_value_have_it(torch, d, page, new, length, window, hq):  # noqa: F811
+    dc = DrawnCache([length], 1, d, page, seed=length + d)
+    # the new tokens' first, middle and last, what the first token's window begins with, and an early one: each in columns of its own
+    entries = sorted({length - new, length - new + 2 * new // 3, length - 1, max(0, min(length - 1, length - new - window + 1)), length // 5})
+    bad = []
+    for i, e in enumerate(entries):
+        bad += [(e, 4 * i, np.inf), (e, 4 * i + 1, -np.inf), (e, 4 * i + 2, np.nan), (e, 40, np.inf if i % 2 else -np.inf)]
+    _put_values(dc, 0, bad)
+    cache, table, lens = dc.device(n_q_heads=hq, weights=False)
+    q, x = _queries(torch, new, hq, d, 3)
+    out, lse = torch.zeros_like(q), torch.zeros((new, hq), device="cuda")
+    cache.attend_prompt(q, _i32(torch, [0, new]), table, lens, out, window=window, lse=lse)
+    o, z = device_to_float(out).astype(np.float64).reshape(new, hq, d), lse.cpu().numpy()
+    _expect(o, z, x, dc, 0, dc.v[0][0], d ** -0.5, okv.sees(length, new, window), "prompt")
+    if new <= 64:
+        # the same rows as single tokens
+        own = np.arange(length - new, length)
+        one = dc.device(n_q_heads=hq, weights=False, max_seqs=new)[0]
+        one.attend(q, table.expand(new, -1).contiguous(), _i32(torch, own + 1), out, lse=lse,
+                   starts=_i32(torch, own - window + 1) if window else None)
+        o, z = device_to_float(out).astype(np.float64).reshape(new, hq, d), lse.cpu().numpy()
+        _expect(o, z, x, dc, 0, dc.v[0][0], d ** -0.5, okv.sees(length, new, window), "single")
+        one.close()
+    cache.close()
+
+
+@pytest.mark.parametrize("window", [0, 200])
+def test_infinite_values_of_a_long_prompt_of_many_heads(torch, window):  # noqa: F811
+    # tiles of 128 rows
+    new, hkv, G, d = 1300, 8, 4, 64
+    dc = DrawnCache([new], hkv, d, 64, seed=2)
+    page, place = dc.where(0)
+    for e, c, bits, value in ((0, 1, 0x7F80, np.inf), (63, 2, 0xFF80, -np.inf), (700, 3, 0x7F80, np.inf), (1299, 4, 0x7F80, np.inf)):
+        dc.V[page[e], :, place[e], c] = bits
+        dc.v[0][:, e, c] = value
+    cache, table, lens = dc.device(n_q_heads=hkv * G, weights=False)
+    q, x = _queries(torch, new, hkv * G, d, 3)
+    out, lse = torch.zeros_like(q), torch.zeros((new, hkv * G), device="cuda")
+    cache.attend_prompt(q, _i32(torch, [0, new]), table, lens, out, window=window, lse=lse)
+    o, z = device_to_float(out).astype(np.float64).reshape(new, hkv * G, d), lse.cpu().numpy()
+    seen = okv.sees(new, new, window)
+    for h in range(hkv):
+        one = type("", (), {"k": [dc.k[0][h:h + 1]], "v": [dc.v[0][h:h + 1]]})
+        r = slice(h * G, h * G + G)
+        _expect(o[:, r], z[:, r], x[:, r], one, 0, dc.v[0][h], d ** -0.5, seen, h)
+    cache.close()
+
+
+@pytest.mark.parametrize("new,length", [(5, 80), (20, 20), (64, 64), (100, 130), (100, 400)])
+def test_an_infinite_value_behind_scores_far_below_its_own(torch, new, length):  # noqa: F811
+    # the entries of the last new tokens score 150 above all before them (and the first
+    # of these stand in tiles of their own or in the same ones): what came before has no probability left
+    d, first = 64, length - (new + 1) // 2
+    dc = DrawnCache([length], 1, d, 16, seed=4)
+    page, place = dc.where(0)
+    dc.K[page, 0, place] = 0
+    dc.k[0][:] = 0
+    dc.K[page[first:], 0, place[first:], 0] = wl.bf16_round(np.full(length - first, 16.0))[0]
+    dc.k[0][0, first:, 0] = 16.0
+    _put_values(dc, 0, [(first, 3, np.inf), (length - 1, 4, -np.inf), (length - 1, 5, np.nan)])
+    q = torch.zeros((new, 2, d), dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 75.0
+    x = np.zeros((new, 2, d))
+    x[:, :, 0] = 75.0
+    cache, table, lens = dc.device(n_q_heads=2, weights=False)
+    out, lse = torch.zeros_like(q).flatten(1), torch.zeros((new, 2), device="cuda")
+    cache.attend_prompt(q.flatten(1), _i32(torch, [0, new]), table, lens, out, lse=lse)
+    o, z = device_to_float(out).astype(np.float64).reshape(new, 2, d), lse.cpu().numpy()
+    _expect(o, z, x, dc, 0, dc.v[0][0], d ** -0.5, okv.sees(length, new), "prompt")
     cache.close()
