@@ -68,12 +68,10 @@ __device__ __forceinline__ int v32_at(int r, int c) {
     return r * (D / 8) + (c ^ (D == 128 ? 4 * (r & 3) : 2 * (r & 2)));
 }
 
-// x y, but 0 where x is 0 whatever y
-__device__ __forceinline__ float times_legacy(float x, float y) {
-    float r;
-    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "s"(y), "v"(x));
-    return r;
-}
+// x y, but 0 where one of them is 0 whatever the other.  (The compiler's instruction and
+// not one of an asm statement: x is an exponential, which needs a pause before it is
+// used, and before asm statements the compiler puts none)
+extern "C" __device__ float bdl_mul_legacy(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
 
 // 64 pieces of 16 bytes, the lanes' at byte offsets `off` of a buffer, into LDS at
 // `to` (the wave's; lane l's lands 16 l bytes on).  Written out because the compiler
@@ -464,7 +462,7 @@ struct Rows {
                 const float f = FMT == kInt8 && k ? scale1 : scale0;
                 float x = exp2_(fmaf(s[8 * k + i], f, -mm)), y = exp2_(fmaf(s[8 * k + i + 1], f, -mm));
                 sum += x + y;
-                if constexpr (FMT == kInt8) x = times_legacy(x, vs[k]), y = times_legacy(y, vs[k]);
+                if constexpr (FMT == kInt8) x = bdl_mul_legacy(x, vs[k]), y = bdl_mul_legacy(y, vs[k]);
                 pb[k][i / 2] = pk_bf16(x, y);
             }
         // (computed here, beside the products that go on, and not where they are used)
