@@ -87,9 +87,8 @@ __device__ __forceinline__ unsigned lds_address(const void* p) {
 }
 
 __device__ __forceinline__ void copy_to_lds(u32x4 rsrc, unsigned off, unsigned at) {
-    // (the pause: a vector instruction may just have written the descriptor; the
-    // kernel has no other use of m0)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(rsrc) : "memory");
+    // (the pause: a vector instruction may just have written the descriptor)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(rsrc) : "m0", "memory");
 }
 
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }

@@ -40,3 +40,11 @@ def test_there_are_statements():
 def test_asm_statements_compute_nothing(file, code):
     for x in code.split("; "):
         assert re.match(r"(s_waitcnt|s_barrier|s_nop|s_mov_b32 m0|buffer_load_dwordx4 .* lds$)", x), (file, x)
+
+
+@pytest.mark.parametrize("file,code,whole", [(f, "; ".join(c), w) for f, c, w in _statements() if c])
+def test_what_statements_write_is_named(file, code, whole):
+    written = re.findall(r"s_mov_b32 (\w+),", code)
+    clobbers = whole.rsplit(":", 1)[1] if whole.count(":") >= 3 else ""
+    for r in written:
+        assert f'"{r}"' in clobbers, (file, whole)
