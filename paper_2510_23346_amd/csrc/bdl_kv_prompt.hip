@@ -86,10 +86,15 @@ __device__ __forceinline__ unsigned lds_address(const void* p) {
     return (unsigned)uni((int)(unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
 }
 
+// (m0 is named as written, so that the compiler keeps nothing there across it; its
+// warning is that it would not save one of its own there, which it has not)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_to_lds(u32x4 rsrc, unsigned off, unsigned at) {
     // (the pause: a vector instruction may just have written the descriptor)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(rsrc) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
