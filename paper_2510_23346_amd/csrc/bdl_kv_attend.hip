@@ -590,7 +590,7 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                     for (int z = 0; z < NW; ++z) y[z] = reinterpret_cast<const f32x4*>(lds)[piece(z) * BUF + dt * 64 + l];
 #pragma unroll
                     for (int z = 0; z < NW; ++z)
-                        if (st[z].x != 0.f) v += st[z].x * y[z];
+                        v = with_share(v, st[z].x, y[z]);
                     const int d = dt * 16 + 4 * lg;
                     if (ch_.whole) {
                         finish(b, hd.hq0 + lr, d, v, M, S);
@@ -706,7 +706,7 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                     for (int x = 0; x < kBatch; ++x) {
                         const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
                         ss += fx * ms[x].y;
-                        if (fx != 0.f) v += fx * y[x];
+                        v = with_share(v, fx, y[x]);
                     }
                 }
             };
@@ -734,7 +734,7 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                     const float2 y = fs[x * items + threadIdx.x];
                     const float fx = y.x == -INFINITY ? 0.f : exp2_(y.x - top);
                     ss += fx * y.y;
-                    if (fx != 0.f) v += fx * fv[x * items + threadIdx.x];
+                    v = with_share(v, fx, fv[x * items + threadIdx.x]);
                 }
             }
             if (in && g == 0) {

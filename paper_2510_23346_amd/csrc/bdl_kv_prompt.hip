@@ -527,6 +527,16 @@ struct Rows {
                 }
         }
     }
+    // A block of an int8 cache that stands for NaN, entries e0 on of tile t: rows that see
+    // one of them are NaN, also where its probability is 0
+    __device__ __forceinline__ void nan_block(const KvPromptArgs& a, const Tile& t, int e0) {
+        const int lo = max(t.lo, e0), to = min(min(t.hi - 1, p), e0 + 15), from = a.window ? p - a.window + 1 : 0;
+        const bool sees = max(lo, from) <= to || lo <= min(to, a.sinks - 1);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = sees ? NAN : o[dt][i];
+    }
     // output numbers of part dt of the row, and with the first its lse
     __device__ __forceinline__ void finish(const KvPromptArgs& a, int dt, const f32x16& v, float top, float total) const {
         const bool none = total == 0.f;
@@ -597,11 +607,10 @@ struct Shares {
             for (int x = 0; x < U; ++x) {
                 const float f = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
                 total += f * ms[x].y;
-                if (f != 0.f)
 #pragma unroll
-                    for (int z = 0; z < N; ++z)
+                for (int z = 0; z < N; ++z)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[z][i] += f * y[x][z][i / 4][i % 4];
+                    for (int i = 0; i < 16; ++i) v[z][i] = with_share(v[z][i], f, y[x][z][i / 4][i % 4]);
             }
         }
     }
@@ -710,7 +719,9 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
         blocks.turn(a, kvh, x0 + (l >> 2) < c1, t.e + 16 * (l & 3), t);
         look(x0 + 16);
     };
-    // of the tile being worked on: blocks that are there, and their scales
+    // of the tile being worked on: blocks that are there, and their scales.  (With a bit
+    // where a value's scale is NaN: such a tile is not one of the whole ones)
+    constexpr unsigned kNanBlock = 16u;
     unsigned there = 0, there_next = 0;
     float ks[4], vs[4], ks_next[4], vs_next[4];
 #pragma unroll
@@ -751,6 +762,7 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
             for (int k = 0; k < 4; ++k) {
                 ks_next[k] = __uint_as_float(lane_of(__float_as_uint(blocks.scale.x), l0 + k));
                 vs_next[k] = __uint_as_float(lane_of(__float_as_uint(blocks.scale.y), l0 + k));
+                if (vs_next[k] != vs_next[k]) there_next |= kNanBlock;
             }
     };
     constexpr int PIECES = 2 * LPT;
@@ -930,6 +942,10 @@ __device__ __forceinline__ void wide(const KvPromptArgs& a, const Item& it, int 
             if (R.passes(top)) R.rescale(R.follow(top));
             R.exponentials(s, f0, f1, v2, pb);
             R.add(values, 32 * h, pb, ln);
+            if (FMT == kInt8 && (there & kNanBlock))
+#pragma unroll 1
+                for (int k = 0; k < 2; ++k)
+                    if ((k ? v2[1] : v2[0]) != (k ? v2[1] : v2[0])) R.nan_block(a, t, t.e + 32 * h + 16 * k);
         }
     };
     constexpr std::integral_constant<int, 0> buf0{};
@@ -1118,6 +1134,10 @@ __device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, in
         u32x4 pb[2];
         R.exponentials(s, f0, f1, v2, pb);
         R.add(values, 0, pb, l);
+        if constexpr (FMT == kInt8)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (v2[k] != v2[k]) R.nan_block(a, t, t.e + 16 * k);
     }
     // the four waves' sums, each in its own part of LDS, added in order; wave dt has
     // part dt of the outputs
@@ -1148,9 +1168,8 @@ __device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, in
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x4 y = x[z * 2 * BUF + (4 * dt + i) * 64 + l];
-                if (f != 0.f)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[4 * i + k] += f * y[k];
+                for (int k = 0; k < 4; ++k) v[4 * i + k] = with_share(v[4 * i + k], f, y[k]);
             }
         }
     }

@@ -1,4 +1,4 @@
-"""Attention where a number of the cache is a zero scale or an infinity:
+"""Attention where a number of the cache is a zero scale, an infinity or a NaN:
 attend and attend_prompt give what the formula gives.  Tolerances as in
 test_gpu_kv_prompt.py."""
 import numpy as np
@@ -6,7 +6,7 @@ import pytest
 
 import workloads as wl
 from oracle import kv as okv
-from test_gpu_kv_prompt import _compare, _i32, _queries, torch  # noqa: F401  (torch: a fixture)
+from test_gpu_kv_prompt import FORMATS, _compare, _i32, _queries, torch  # noqa: F401  (torch: a fixture)
 from workloads.gpu import device_to_float
 from workloads.kv import DrawnCache
 
@@ -196,3 +196,70 @@ def test_an_infinite_value_behind_scores_far_below_its_own(torch, new, length): 
     o, z = device_to_float(out).astype(np.float64).reshape(new, 2, d), lse.cpu().numpy()
     _expect(o, z, x, dc, 0, dc.v[0][0], d ** -0.5, okv.sees(length, new), "prompt")
     cache.close()
+
+
+# ------------------------------------------------ NaN whose probability fp32 does not hold
+
+@pytest.mark.parametrize("fmt", list(FORMATS))
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at", [0, 40, 200])
+@pytest.mark.parametrize("new,length", [(1, 1200), (4, 1200), (60, 250), (130, 1200), (300, 1200)])
+def test_nan_values_without_probability_reach_all_rows_that_see_them(torch, fmt, d, at, new, length):  # noqa: F811
+    # every score is 0 but those of 64 entries around the NaN, which are 300 below: e^-300
+    # is 0 in fp32 (and 0 times NaN is NaN), in whole tiles too
+    dc = DrawnCache([length], 1, d, 16, seed=1, **FORMATS[fmt])
+    page, place = dc.where(0)
+    block = slice(at // 16 * 16, at // 16 * 16 + 16)
+    low = slice(at // 64 * 64, min(length, at // 64 * 64 + 64))
+    dc.K[page, 0, place] = 0
+    dc.k[0][:] = 0
+    if fmt == "int8":
+        _scales(dc, 0, 0, range(at // 64 * 4, -(-low.stop // 16)), 1.0)
+        dc.K[page[low], 0, place[low], 0] = -100
+        key = -100.0
+    elif fmt == "fp8":
+        dc.K[page[low], 0, place[low], 0] = okv.e4m3_encode(-448.0)
+        key = -448.0 * np.float64(np.float32(0.015))
+    else:
+        dc.K[page[low], 0, place[low], 0] = wl.bf16_round(np.full(low.stop - low.start, -100.0))[0]
+        key = -100.0
+    dc.k[0][0, low, 0] = key
+    if fmt == "int8":
+        _scales(dc, 0, 1, [at // 16], np.nan)
+    else:
+        dc.V[page[at], 0, place[at], 7] = {"bf16": 0x7FC0, "fp8": 0x7F}[fmt]
+        dc.v[0][0, at, 7] = np.nan
+    q = torch.zeros((new, 2, d), dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 3.0
+    scale = 300.0 / (3.0 * abs(key))
+    for window in (0, 100):
+        seen = okv.sees(length, new, window)
+        hit = seen[:, block].any(1) if fmt == "int8" else seen[:, at]
+        cache, table, lens = dc.device(n_q_heads=2, weights=False)
+        out, lse = torch.zeros_like(q).flatten(1), torch.zeros((new, 2), device="cuda")
+        cache.attend_prompt(q.flatten(1), _i32(torch, [0, new]), table, lens, out, window=window, scale=scale, lse=lse)
+        results = [("prompt", device_to_float(out), lse.cpu().numpy())]
+        own = np.arange(length - new, length)
+        one = dc.device(n_q_heads=2, weights=False, max_seqs=new)[0]
+        one.attend(q.flatten(1), table.expand(new, -1).contiguous(), _i32(torch, own + 1), out, lse=lse, scale=scale,
+                   starts=_i32(torch, own - window + 1) if window else None)
+        results.append(("single", device_to_float(out), lse.cpu().numpy()))
+        weight = np.where(seen, 1.0, 0.0)
+        weight[:, low] = 0.0                                      # (e^-300)
+        mean = weight @ np.nan_to_num(dc.v[0][0]) / np.maximum(weight.sum(1), 1)[:, None]
+        size = weight @ np.abs(np.nan_to_num(dc.v[0][0])) / np.maximum(weight.sum(1), 1)[:, None]
+        for what, o, z in results:
+            o = o.reshape(new, 2, d)
+            assert np.isnan(o[hit] if fmt == "int8" else o[hit][..., 7]).all(), (what, window)
+            assert np.isfinite(o[~hit]).all() and (fmt == "int8" or np.isfinite(np.delete(o[hit], 7, 2)).all()), (what, window)
+            # scores are 0 exactly: the sum of n ones, its logarithm to 2^-19; out: the sum's n 2^-24 and its rounding
+            some = weight.sum(1) > 0
+            assert np.abs(z[some] - np.log(weight.sum(1))[some, None]).max(initial=0) <= 2.0 ** -19 + length * 2.0 ** -24
+            rows = ~hit & some
+            # (attend_prompt over int8 rounds a probability times its block's scale to bf16: 1 is exact, 1 times
+            # the scale is off by up to half a step, 2^-8 of it, and so is each p |v| of the sum)
+            bits = 8 if what == "prompt" and fmt == "int8" else 15
+            tol = (2.0 ** -8 * np.abs(mean) + (2.0 ** -bits * 1.01 + length * 2.0 ** -24) * size)[rows][:, None]
+            assert (np.abs(o[rows] - mean[rows][:, None]) <= tol).all(), (what, window)
+        one.close()
+        cache.close()
