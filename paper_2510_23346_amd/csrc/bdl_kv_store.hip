@@ -16,8 +16,8 @@ namespace {
 // were there are rounded again, rint(q s_before / s).  (m / 127 and x / s are
 // products with the fp32 reciprocals.)  So a block has one owner: the wave of
 // the first token of its run, tokens of one sequence that follow each other in
-// the call and in the block.  It has all 16 rows of the block, those that are
-// new in registers, four lanes a row; its other tokens' waves leave.
+// the call and, with gaps or without, in the block.  It has all 16 rows of the block,
+// those that are new in registers, four lanes a row; its other tokens' waves leave.
 //
 // Rotation and norm are those of the bf16 cache, and queries are dealt with by
 // threads of the same launch as there.
@@ -82,20 +82,38 @@ __device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int se
     const int l = threadIdx.x & 63, r = l >> 2, c = l & 3;
     // (two trips to memory: the page, the run and its rows; what the block holds and
     // the angles)
-    const int j = r - (i0 & (kKvBlock - 1)), tok = min(t + max(j, 0), a.T - 1), d0 = N * c, d1 = D / 2 + N * c;
+    const int j = r - (i0 & (kKvBlock - 1)), d0 = N * c, d1 = D / 2 + N * c;
+    int tok = min(t + max(j, 0), a.T - 1);
     const int page = a.c.table[(long long)seq * a.c.tstride + (i0 >> a.c.ps_shift)];
-    const int seq_r = a.seqs[tok], index_r = a.index[tok], pos_r = a.positions[tok];
-    const uint16_t* const x = a.qkv + tok * a.qkv_stride + (a.c.hq + (value ? a.c.hkv : 0) + kh) * D;
-    Piece<N> y0 = load_piece<N>(x + d0), y1 = load_piece<N>(x + d1);
+    const int seq_r = a.seqs[tok], index_r = a.index[tok];
+    int pos_r = a.positions[tok];
+    const uint16_t* const x = a.qkv + (a.c.hq + (value ? a.c.hkv : 0) + kh) * D;
+    Piece<N> y0 = load_piece<N>(x + tok * a.qkv_stride + d0), y1 = load_piece<N>(x + tok * a.qkv_stride + d1);
     if ((unsigned)page >= (unsigned)a.c.n_pages) {
         kv_error(a.c);
         return;
     }
     const long long e0 = (((long long)page * a.c.hkv + kh) << a.c.ps_shift) + (i0 & ((1 << a.c.ps_shift) - 1) & ~(kKvBlock - 1));
-    // the row's token, if the run goes as far
-    const bool follows = j >= 0 && j < a.T - t && seq_r == seq && index_r == i0 + j;
+    // the lane's token, if the run goes as far: it is the row's where there are no gaps
+    const int index_1 = __shfl_up(index_r, 4);
+    const bool follows = j >= 0 && j < a.T - t && seq_r == seq && (index_r >> 4) == (i0 >> 4) && (j == 0 || index_r > index_1);
     const unsigned long long breaks = __ballot(j >= 0 && !follows);
-    const bool mine = follows && (breaks == 0 || l < (int)__builtin_ctzll(breaks)) && pos_r >= 0 && pos_r < a.n_positions;
+    bool has = follows && (breaks == 0 || l < (int)__builtin_ctzll(breaks));
+    if (__any(has && index_r != i0 + j)) {
+        // a run with gaps: each row looks for its token
+        const unsigned long long run = __ballot(has);
+        has = false;
+#pragma unroll 1
+        for (int k = i0 & (kKvBlock - 1); k < kKvBlock; ++k)
+            if ((run >> (4 * k) & 1) && (__builtin_amdgcn_readlane(index_r, 4 * k) & (kKvBlock - 1)) == r) {
+                has = true;
+                tok = t + k - (i0 & (kKvBlock - 1));
+            }
+        pos_r = a.positions[tok];
+        y0 = load_piece<N>(x + tok * a.qkv_stride + d0);
+        y1 = load_piece<N>(x + tok * a.qkv_stride + d1);
+    }
+    const bool mine = has && pos_r >= 0 && pos_r < a.n_positions;
     const int pos = mine ? pos_r : 0;
     const unsigned long long rows = __ballot(mine);
     if (rows == 0) return;
@@ -209,7 +227,7 @@ __global__ __launch_bounds__(256) void kv_store_kernel(const KvAppendArgs a, int
         const int l = threadIdx.x & 63, t = MANY ? t0 + min(l, kKvBlock - 1) * step : t0, at_t = min(t, a.T - 1), before = max(at_t - 1, 0);
         const int seq = a.seqs[at_t], at = a.index[at_t], seq1 = a.seqs[before], at1 = a.index[before];
         bool first = seq >= 0 && seq < a.n_seqs && at >= 0 && at < cap;
-        if (t > 0 && (at & (kKvBlock - 1)) && seq1 == seq && at1 == at - 1) first = false;
+        if (t > 0 && seq1 == seq && (at1 >> 4) == (at >> 4) && at1 < at) first = false;
         if constexpr (MANY) {
 #pragma unroll 1
             for (unsigned long long m = __ballot(first && l < kKvBlock && t < a.T); m; m &= m - 1) {
