@@ -30,6 +30,7 @@ constexpr int kv_part_floats(int D) { return kKvHeads * (D + 2); }
 
 // attention of many tokens: shares of up to 16 rows' sums in the same place
 constexpr int kKvPromptSlots = 1536;
+constexpr int kKvSlots = kKvPromptSlots > 2 * kKvAttendGrid ? kKvPromptSlots : 2 * kKvAttendGrid;
 
 // What every kernel knows of the cache and of the call's page table.  Pages
 // are [n_pages][hkv][1 << ps_shift] entries: K and V of D elements each,
@@ -58,6 +59,8 @@ struct KvAppendArgs {
     float k_inv, v_inv;   // e4m3 cache: 1 / scale
     const uint16_t *q_norm, *k_norm;   // [head size] each; null: no norm
     float eps;
+    int* owners;          // int8 caches: n_owners numbers, in the place of attention's shares; they may hold anything
+    unsigned n_owners;
 };
 
 struct KvReadArgs {
@@ -79,7 +82,7 @@ struct KvAttendArgs {
     int sinks;                  // first entries that are attended to before starts
     float* lse;                 // may be null
     int B;
-    float* part;                // [2 kKvAttendGrid][kv_part_floats(D)]
+    float* part;                // kKvSlots x kv_part_floats(D), 2 kKvAttendGrid used
     unsigned* count;            // kKvAttendCounts counters: zero between calls
     float* logits;              // accumulating: [n_pages][hq][page], products <q, k>
     float* lse2;                // accumulating: [B][hq], lse in those units

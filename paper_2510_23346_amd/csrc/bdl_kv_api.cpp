@@ -38,7 +38,7 @@ Parts layout(const bdlora_kv_desc& d, bool weights) {
     p.count = take(4LL * bdl::kKvCount * bdl::kKvAttendCounts);
     p.evict_count = take(weights ? 4LL * bdl::kKvCount * d.max_seqs * (d.n_kv_heads + 1) : 0);
     p.clear = at;
-    p.part = take((long long)std::max(2 * bdl::kKvAttendGrid, bdl::kKvPromptSlots) * bdl::kv_part_floats(d.head_dim) * 4);
+    p.part = take((long long)bdl::kKvSlots * bdl::kv_part_floats(d.head_dim) * 4);
     p.lse2 = take(weights ? 4LL * d.max_seqs * d.n_q_heads : 0);
     p.logits = take(weights ? 4LL * d.n_pages * d.n_q_heads * d.page_size : 0);
     p.total = at;
@@ -154,6 +154,8 @@ int append(bdlora_kv_t c, const void* qkv, int64_t qkv_stride, const void* q_nor
         a.q_norm = (const uint16_t*)q_norm;
         a.k_norm = (const uint16_t*)k_norm;
         a.eps = eps;
+        a.owners = (int*)c->part;
+        a.n_owners = (unsigned)(bdl::kKvSlots * bdl::kv_part_floats(c->d.head_dim));
         a.k_inv = 1.f / c->d.k_scale;
         a.v_inv = 1.f / c->d.v_scale;
         if (hipError_t e = bdl::launch_kv_append(a, c->d.head_dim, c->d.format == BDLORA_KV_FP8_E4M3, (hipStream_t)stream))

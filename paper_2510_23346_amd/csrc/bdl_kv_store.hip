@@ -19,6 +19,13 @@ namespace {
 // the call and, with gaps or without, in the block.  It has all 16 rows of the block,
 // those that are new in registers, four lanes a row; its other tokens' waves leave.
 //
+// Tokens of a block that do not stand so have owners that know nothing of each other,
+// and what the block holds is anything.  That is found out: an owner leaves its token's
+// number at the block's place in a.owners and takes the one it finds there, which is
+// an earlier call's, anything at all, or another owner's.  So it looks whether that
+// token, now, is of its block and not of its run.  (A cache of more blocks than there
+// are places, 3.2 million at head size 128, shares them, and an owner may not be found.)
+//
 // Rotation and norm are those of the bf16 cache, and queries are dealt with by
 // threads of the same launch as there.
 //
@@ -99,9 +106,10 @@ __device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int se
     const bool follows = j >= 0 && j < a.T - t && seq_r == seq && (index_r >> 4) == (i0 >> 4) && (j == 0 || index_r > index_1);
     const unsigned long long breaks = __ballot(j >= 0 && !follows);
     bool has = follows && (breaks == 0 || l < (int)__builtin_ctzll(breaks));
+    const unsigned long long run = __ballot(has);
+    const int tokens = __popcll(run) >> 2;
     if (__any(has && index_r != i0 + j)) {
         // a run with gaps: each row looks for its token
-        const unsigned long long run = __ballot(has);
         has = false;
 #pragma unroll 1
         for (int k = i0 & (kKvBlock - 1); k < kKvBlock; ++k)
@@ -113,6 +121,11 @@ __device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int se
         y0 = load_piece<N>(x + tok * a.qkv_stride + d0);
         y1 = load_piece<N>(x + tok * a.qkv_stride + d1);
     }
+    const bool asks = kh == 0 && value && l == 0;
+    int other = -1;
+    if (asks)
+        other = atomicExch(a.owners + (unsigned)((((unsigned long long)(unsigned)page << a.c.ps_shift) +
+                                                  (unsigned)(i0 & ((1 << a.c.ps_shift) - 1))) >> 4) % a.n_owners, t);
     const bool mine = has && pos_r >= 0 && pos_r < a.n_positions;
     const int pos = mine ? pos_r : 0;
     const unsigned long long rows = __ballot(mine);
@@ -210,6 +223,9 @@ __device__ __forceinline__ void store_block(const KvAppendArgs& a, int t, int se
         const int last = (63 - __builtin_clzll(rows)) >> 2;
         if (l == 0) atomicMax(a.lens + seq, (i0 & ~(kKvBlock - 1)) + last + 1);
     }
+    // (the run's tokens stand from t on)
+    if (asks && other >= 0 && other < a.T && (other < t || other >= t + tokens) && a.seqs[other] == seq && (a.index[other] >> 4) == (i0 >> 4))
+        kv_error(a.c);
 }
 
 // The first `q_groups` workgroups take `q_rows` tokens' queries each, as append does.
