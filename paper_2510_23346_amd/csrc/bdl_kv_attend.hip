@@ -571,6 +571,7 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
             if (lr < hd.n) {
                 float2 st[NW];
                 float M = -INFINITY, S = 0.f;
+                bool out = false;                                   // some are left out
 #pragma unroll
                 for (int z = 0; z < NW; ++z) st[z] = stat[piece(z)][lr];
 #pragma unroll
@@ -580,7 +581,9 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                 }
 #pragma unroll
                 for (int z = 0; z < NW; ++z) {
-                    st[z].x = st[z].x == -INFINITY ? 0.f : exp2_(st[z].x - M);
+                    const bool some = st[z].x != -INFINITY;
+                    st[z].x = some ? exp2_(st[z].x - M) : 0.f;
+                    out |= some && st[z].x == 0.f;
                     S += st[z].x * st[z].y;                         // (a NaN stays one)
                 }
 #pragma unroll 2
@@ -590,7 +593,12 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                     for (int z = 0; z < NW; ++z) y[z] = reinterpret_cast<const f32x4*>(lds)[piece(z) * BUF + dt * 64 + l];
 #pragma unroll
                     for (int z = 0; z < NW; ++z)
-                        v = with_share(v, st[z].x, y[z]);
+                        if (st[z].x != 0.f) v += st[z].x * y[z];
+                    if (out)
+#pragma unroll
+                        for (int z = 0; z < NW; ++z)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i] = keep_nan(v[i], y[z][i]);
                     const int d = dt * 16 + 4 * lg;
                     if (ch_.whole) {
                         finish(b, hd.hq0 + lr, d, v, M, S);
@@ -702,12 +710,19 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                     top = tn;
                     ss *= fo;
                     v *= fo;
+                    bool out = false;                               // some are left out
 #pragma unroll
                     for (int x = 0; x < kBatch; ++x) {
                         const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
                         ss += fx * ms[x].y;
-                        v = with_share(v, fx, y[x]);
+                        if (fx != 0.f) v += fx * y[x];
+                        out |= fx == 0.f && ms[x].x != -INFINITY;
                     }
+                    if (out)
+#pragma unroll
+                        for (int x = 0; x < kBatch; ++x)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i] = keep_nan(v[i], y[x][i]);
                 }
             };
             if (in) {
@@ -734,7 +749,12 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                     const float2 y = fs[x * items + threadIdx.x];
                     const float fx = y.x == -INFINITY ? 0.f : exp2_(y.x - top);
                     ss += fx * y.y;
-                    v = with_share(v, fx, fv[x * items + threadIdx.x]);
+                    const f32x4 z = fv[x * items + threadIdx.x];
+                    if (fx != 0.f)
+                        v += fx * z;
+                    else
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = keep_nan(v[i], z[i]);
                 }
             }
             if (in && g == 0) {

@@ -180,19 +180,10 @@ __device__ __forceinline__ float2 load_through2(__amdgpu_buffer_rsrc_t r, unsign
     return float2{__uint_as_float(v[0]), __uint_as_float(v[1])};
 }
 
-// A share's sums, x, times the factor of its maximum to those of a row, v.  Where that
-// is 0 they are nothing, infinities too; a NaN is one whatever its probability
-__device__ __forceinline__ float with_share(float v, float f, float x) {
-    if (f != 0.f) return v + f * x;
-    return x != x ? x : v;
-}
-
-__device__ __forceinline__ f32x4 with_share(f32x4 v, float f, f32x4 x) {
-    if (f != 0.f) return v + f * x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = x[i] != x[i] ? x[i] : v[i];
-    return v;
-}
+// Shares of a row are added times the factor of their maximum to the row's.  Where that
+// is 0 they are left out, since 0 times an infinity is a NaN; but a NaN among a share's
+// sums, x, is one of the row's, v, whatever its probability
+__device__ __forceinline__ float keep_nan(float v, float x) { return x != x ? x : v; }
 
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 

@@ -603,15 +603,25 @@ struct Shares {
             total *= fo;
 #pragma unroll
             for (int z = 0; z < N; ++z) v[z] *= fo;
+            bool out = false;                               // some are left out
 #pragma unroll
             for (int x = 0; x < U; ++x) {
                 const float f = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
                 total += f * ms[x].y;
+                out |= f == 0.f && ms[x].x != -INFINITY;
+                if (f != 0.f)
 #pragma unroll
-                for (int z = 0; z < N; ++z)
+                    for (int z = 0; z < N; ++z)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[z][i] = with_share(v[z][i], f, y[x][z][i / 4][i % 4]);
+                        for (int i = 0; i < 16; ++i) v[z][i] += f * y[x][z][i / 4][i % 4];
             }
+            if (out)
+#pragma unroll
+                for (int x = 0; x < U; ++x)
+#pragma unroll
+                    for (int z = 0; z < N; ++z)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[z][i] = keep_nan(v[z][i], y[x][z][i / 4][i % 4]);
         }
     }
 };
@@ -1134,10 +1144,10 @@ __device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, in
         u32x4 pb[2];
         R.exponentials(s, f0, f1, v2, pb);
         R.add(values, 0, pb, l);
-        if constexpr (FMT == kInt8)
-#pragma unroll
+        if (const float both = v2[0] + v2[1]; FMT == kInt8 && both != both)
+#pragma unroll 1
             for (int k = 0; k < 2; ++k)
-                if (v2[k] != v2[k]) R.nan_block(a, t, t.e + 16 * k);
+                if ((k ? v2[1] : v2[0]) != (k ? v2[1] : v2[0])) R.nan_block(a, t, t.e + 16 * k);
     }
     // the four waves' sums, each in its own part of LDS, added in order; wave dt has
     // part dt of the outputs
@@ -1168,8 +1178,12 @@ __device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, in
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x4 y = x[z * 2 * BUF + (4 * dt + i) * 64 + l];
+                if (f != 0.f)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[4 * i + k] = with_share(v[4 * i + k], f, y[k]);
+                    for (int k = 0; k < 4; ++k) v[4 * i + k] += f * y[k];
+                else
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[4 * i + k] = keep_nan(v[4 * i + k], y[k]);
             }
         }
     }
