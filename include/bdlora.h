@@ -617,8 +617,10 @@ int bdlora_kv_attend_sinks(bdlora_kv_t cache, const void* q, int64_t q_stride, i
  * and out, lse are as in bdlora_kv_attend, rows of `out` as those of q (they must
  * not overlap).  A row without an entry of its own (more rows than entries: error
  * flag) gives 0 and lse -infinity; rows of no sequence are left as they are.
- * Probabilities enter the sum over values as bf16 (8 significant bits), their
- * sum and lse do not.  Nothing is accumulated.  T x n_q_heads <= 2^30, B x
+ * Probabilities enter the sum over values with 24 bits, as in bdlora_kv_attend, for
+ * sequences of up to 32 rows (new tokens times query heads of a kv head: single
+ * and drafted tokens), and as bf16, 8 significant bits, for those of more; their
+ * sum and lse are fp32 in both.  Nothing is accumulated.  T x n_q_heads <= 2^30, B x
  * n_kv_heads < 2^23.
  * Errors: INVALID_ARG, SHAPE, HIP. */
 int bdlora_kv_attend_prompt(bdlora_kv_t cache, const void* q, int64_t q_stride, int32_t T, const int32_t* q_starts, int32_t B,

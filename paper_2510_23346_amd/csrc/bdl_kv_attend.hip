@@ -100,10 +100,6 @@ struct Line {
     }
 };
 
-// What is left of a number without its upper 16 bits, those of two numbers side
-// by side, and the smaller or larger one of each half
-__device__ __forceinline__ float below_bf16(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-
 // A tile: two blocks of 16 entries, each within one page, of one head of one
 // sequence
 struct Tile {

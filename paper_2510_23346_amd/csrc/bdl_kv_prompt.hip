@@ -12,9 +12,14 @@
 // heads.  A wave's products are S^T = K Q^T and O^T = V^T P^T (32x32x16, bf16): a
 // row's scores lie in one lane (and the one 32 further), so that maximum and sum
 // need no exchange, and they are already those of the second product's operand.
-// The probabilities are rounded to bf16 for it (their sum is not): half a step of 2^-8
-// each, which the sum of many averages out.  Two bf16 numbers for each, as single
-// tokens have three, would take the second product twice, half as much time again.
+// In wide tiles the probabilities are rounded to bf16 for it (their sum is not): half a
+// step of 2^-8 each, which the sum of many averages out: outputs are off by 0.0022 to
+// 0.0024 (root of the mean square, relative), 0.0017 of it their own rounding.  Two
+// bf16 numbers for each take the second product twice: 8192 tokens 733 us in place of
+// 539, 16384 with a window 373 for 274, 8 prompts of 512 17.8 for 16.4.  Narrow tiles,
+// single and drafted tokens, have three for each, all 24 bits, as the call for single
+// tokens has, so that a token's numbers do not depend on the call its batch takes (64
+// sequences of 5 tokens over int8 26.4 us in place of 24.3).
 //
 // Wide tiles: a workgroup has 128 (or 64) rows, 32 a wave, whose four waves share
 // tiles of 64 entries in LDS, two of them in turn: one is worked on while the next
@@ -472,20 +477,53 @@ struct Rows {
         // (computed here, beside the products that go on, and not where they are used)
         asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(sum));
     }
+    // part dt of 16 transposed values of LDS, rows r on
+    __device__ __forceinline__ u32x4 values_of(const u32x4* values, int r, int dt, int ln) const {
+        s16x4 v[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int at = v32_at<D>(r + 8 * x + 4 * (ln >> 5) + ((ln & 15) >> 2), 4 * dt + 2 * ((ln >> 4) & 1) + ((ln >> 1) & 1));
+            v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(reinterpret_cast<const short*>(values + at) + 4 * (ln & 1)));
+        }
+        return __builtin_bit_cast(u32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
     // out^T += V^T P^T over 32 values of LDS, rows r on
     __device__ __forceinline__ void add(const u32x4* values, int r, const u32x4 (&pb)[2], int ln) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                s16x4 v[2];
+            for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(values_of(values, r + 16 * k, dt, ln), pb[k], o[dt]);
+    }
+    // Exponentials and their product with 32 values of LDS, rows 0 on, where they are kept
+    // as three bf16 numbers whose sum they are, all 24 bits: each cut towards zero, what
+    // is left over is exact.  Where the first is not 0 the others are at least 2^-133, so
+    // that an infinite value gives an infinite sum and no NaN (int8 has none)
+    __device__ __forceinline__ void add_exponentials(const f32x16& s, float scale0, float scale1, const float* vs, const u32x4* values) {
+        const float mm = m == -INFINITY ? 0.f : m;
+        int ln = l;
+        asm volatile("" : "+v"(ln));                // (no addresses kept in registers across the tiles)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int at = v32_at<D>(r + 16 * k + 8 * x + 4 * (ln >> 5) + ((ln & 15) >> 2), 4 * dt + 2 * ((ln >> 4) & 1) + ((ln >> 1) & 1));
-                    v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(reinterpret_cast<const short*>(values + at) + 4 * (ln & 1)));
-                }
-                o[dt] = mfma32(__builtin_bit_cast(u32x4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7)), pb[k], o[dt]);
+        for (int k = 0; k < 2; ++k) {
+            u32x4 pb[3];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const float f = FMT == kInt8 && k ? scale1 : scale0;
+                float x = exp2_(fmaf(s[8 * k + i], f, -mm)), y = exp2_(fmaf(s[8 * k + i + 1], f, -mm));
+                sum += x + y;
+                if constexpr (FMT == kInt8) x = bdl_mul_legacy(x, vs[k]), y = bdl_mul_legacy(y, vs[k]);
+                const float x1 = below_bf16(x), y1 = below_bf16(y);
+                const uint32_t h = upper_halves(x, y), some = FMT == kInt8 ? 0u : min_u16x2(h, 0x00010001u);
+                pb[0][i / 2] = h;
+                pb[1][i / 2] = max_u16x2(upper_halves(x1, y1), some);
+                pb[2][i / 2] = max_u16x2(upper_halves(below_bf16(x1), below_bf16(y1)), some);
             }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const u32x4 v = values_of(values, 16 * k, dt, ln);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) o[dt] = mfma32(v, pb[n], o[dt]);
+            }
+        }
     }
     // the maximum follows the scores of 32 keys of LDS, rows r on, which stand for entries e0 on of tile t
     __device__ __forceinline__ void follow_tile(const KvPromptArgs& a, const u32x4* keys, int r, const Tile& t, int e0, unsigned there) {
@@ -1141,9 +1179,7 @@ __device__ __forceinline__ void narrow(const KvPromptArgs& a, const Item& it, in
         if (!whole) R.mask(a, s, t, t.e, here, k2);
         const float top = R.top_of(s, f0, f1);
         if (R.passes(top)) R.rescale(R.follow(top));
-        u32x4 pb[2];
-        R.exponentials(s, f0, f1, v2, pb);
-        R.add(values, 0, pb, l);
+        R.add_exponentials(s, f0, f1, v2, values);
         if (const float both = v2[0] + v2[1]; FMT == kInt8 && both != both)
 #pragma unroll 1
             for (int k = 0; k < 2; ++k)

@@ -263,3 +263,74 @@ def test_nan_values_without_probability_reach_all_rows_that_see_them(torch, fmt,
             assert (np.abs(o[rows] - mean[rows][:, None]) <= tol).all(), (what, window)
         one.close()
         cache.close()
+
+
+# ------------------------------------------------ bits of the probabilities
+
+@pytest.mark.parametrize("d,fmt", [(64, "bf16"), (128, "bf16"), (64, "fp8"), (128, "int8"), (64, "int8")])
+@pytest.mark.parametrize("new", [1, 2])
+def test_few_rows_keep_the_bits_of_32_in_the_sum_over_values(torch, d, fmt, new):  # noqa: F811
+    """Sequences of up to 32 rows (new tokens times query heads of a kv head), beside a
+    prompt of more.  Sums over values that all but cancel: one entry of probability
+    p (before the division) and value 1 (times 256 in e4m3) beside entries of
+    probability 1 whose values are minus the first and the next bits of p (8 in
+    bf16, 4 in e4m3, 6 and then 7 in int8, whose entries are of three blocks), so that
+    what is left is p's bits below about 2^-16.
+
+    Tolerance, as for single tokens: the score is one product, exact in fp32; its
+    scaling and the subtraction round numbers of at most 2 in units of log 2 (2^-24
+    each of it: 2^-23 in all), the exponential to 2^-23; a value's scale is a
+    power of 2; and the sum has at most 9 terms that are not 0, 2^-23 each: less than
+    2^-19 of sum p |v|, and the store's 2^-8 of the result.  (The sum of
+    probabilities, of 34 terms at most, errs by 34 2^-24 of the result.)"""
+    B, hq = 64, 16
+    n = 33 if fmt == "int8" else 5
+    rng = np.random.default_rng(d)
+    dc = DrawnCache([n] * B + [100], 1, d, 16, seed=1, **({"fp8": True} if fmt == "fp8" else {"int8": True} if fmt == "int8" else {}))
+    _, q = wl.bf16_round(rng.uniform(2.0, 9.0, (B, hq)))
+    steps = [2.0 ** -6, 2.0 ** -13, 2.0 ** -20]                         # int8: scales of the values' blocks
+    full = np.zeros((B, hq, d))
+    full[:, :, 0] = q
+    for b in range(B):
+        p = np.exp(-0.125 * q[b].astype(np.float64))
+        k, v = np.zeros((1, n, d)), np.zeros((1, n, d))
+        k[0, 1, 0] = -1.0
+        v[0, 1, :hq] = 256.0 if fmt == "fp8" else 1.0
+        rest = p * v[0, 1, 0]
+        for i, e in enumerate({"bf16": (0, 2), "fp8": (0, 2, 3, 4), "int8": (0, 16, 32)}[fmt]):
+            if fmt == "int8":
+                part = np.rint(rest / steps[i]) * steps[i]
+            else:
+                part = wl.bf16_round(rest)[1].astype(np.float64) if fmt == "bf16" else okv.e4m3_values()[okv.e4m3_encode(rest)]
+            v[0, e, :hq] = -part                                        # columns 0 .. hq - 1, one for each query head
+            rest = rest - part
+        dc.k[b], dc.v[b] = k, v
+        if fmt == "int8":
+            page, place = dc.where(b)
+            dc.S[page, 0, place // 16, 0] = 1.0
+            dc.S[page, 0, place // 16, 1] = np.asarray(steps)[np.arange(n) // 16]
+            dc.put(dc.K, b, k.astype(np.int8))
+            dc.put(dc.V, b, (v / np.asarray(steps)[np.arange(n) // 16][None, :, None]).astype(np.int8))
+        else:
+            bits = okv.e4m3_encode if fmt == "fp8" else (lambda x: wl.bf16_round(x)[0])
+            dc.put(dc.K, b, bits(k).astype(dc.K.dtype))
+            dc.put(dc.V, b, bits(v).astype(dc.V.dtype))
+    cache, table, dl = dc.device(n_q_heads=hq, weights=False)
+    rows = np.concatenate([np.repeat(full, new, 0), rng.standard_normal((100, hq, d))])
+    qd = torch.from_numpy(wl.bf16_round(rows.reshape(len(rows), hq * d))[0].view(np.int16)).cuda().view(torch.bfloat16)
+    out = torch.empty_like(qd)
+    begin = np.concatenate([np.arange(B + 1) * new, [B * new + 100]])
+    cache.attend_prompt(qd, _i32(torch, begin), table, dl, out, scale=0.125)
+    y = device_to_float(out).astype(np.float64).reshape(-1, hq, d)
+    for b in range(B):
+        for t in range(new):
+            m = n - new + t + 1
+            for h in range(hq):
+                p = np.exp(0.125 * (dc.k[b][0, :m] @ full[b, h]))
+                p /= p.sum()
+                ref, mag = p @ dc.v[b][0, :m], p @ np.abs(dc.v[b][0, :m])
+                tol = 2.0 ** -8 * np.abs(ref) + 2.0 ** -19 * mag
+                err = np.abs(y[b * new + t, h] - ref)
+                assert (err <= tol).all(), (b, t, h, "times the tolerance: %.2f" % (err[tol > 0] / tol[tol > 0]).max())
+    assert cache.device_error() == 0
+    cache.close()
