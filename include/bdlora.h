@@ -477,7 +477,8 @@ int bdlora_last_path(bdlora_pool_t pool, int32_t* path);
  *
  * Device-side errors (a page number outside 0 .. n_pages - 1 under an entry
  * that is used, a length or index beyond the table's row, a position outside
- * the tables, a seq outside the table, q_starts that do not ascend) raise the
+ * the tables, a seq outside the table, q_starts that do not ascend, tokens of one int8
+ * block that do not stand one after the other) raise the
  * cache's sticky error flag (bdlora_kv_get_device_error); nothing outside the arrays is read or
  * written: the entry counts as not there, the length is cut to what the row
  * can name, the token is not stored.
@@ -502,10 +503,14 @@ typedef struct bdlora_kv* bdlora_kv_t;
  * or to max(s, the scale before) where the block's first entry is not among
  * them, and stores rint(x / s) (both as products with the fp32 reciprocal).
  * Where the scale grows the entries that were there are rounded again, by up to
- * half a step each time.  The scales of a block whose first entry was never
- * appended must be valid (0 where it is new).  A block that has been given an
- * infinity or NaN stands for NaN, all of it.  Such a cache tracks no weights (it
- * does not accumulate or evict). */
+ * half a step each time.  It never shrinks but where the block begins anew: after
+ * tokens that are taken back (drafts that were refused) the block's other entries
+ * keep the coarser scale, until their keys and values, if the caller still has
+ * them, are appended again from the block's first entry on.  Scales that the caller
+ * sets are finite and not negative (0: the block's numbers are zeros), those of a
+ * block whose first entry was never appended too (0 where it is new).  A block that
+ * has been given an infinity or NaN stands for NaN, all of it.  Such a cache tracks
+ * no weights (it does not accumulate or evict).  (2 names no format.) */
 #define BDLORA_KV_INT8_BLOCK 3
 #define BDLORA_KV_BLOCK      16
 
@@ -553,7 +558,13 @@ int bdlora_kv_bytes(const bdlora_kv_desc* desc, int32_t weights, int64_t* page_b
  * null, and not the memory of seqs, index or positions, which are still read
  * while it changes): lens[seqs[t]] = max(lens[seqs[t]], index[t] + 1).  No two tokens of a call may become the same entry.  (Cache with a scale for
  * each block: those of one sequence that become entries of one block stand one
- * after the other in the call, by ascending entry; T x (n_kv_heads + 2) <= 2^25 - 8.)  A token whose position is outside the
+ * after the other in the call, by ascending entry, with gaps or without; where they
+ * do not, what the block holds is anything, and the error flag is raised (which a cache of more
+ * than 1.6 million blocks may miss).  T x (n_kv_heads + 2) <= 2^25 - 8.  A call of more
+ * than 2048 T x n_kv_heads is taken to be prompts', which is faster for these and
+ * slower for single tokens, where it has at least 64 tokens for each of the n_seqs
+ * rows of the table, one of more than 8192 where it has 4: rows of no use to the
+ * call are better left out of n_seqs.)  A token whose position is outside the
  * tables is not stored and its query row is zero.  Strides: multiples of 8;
  * qkv, q_out, cos, sin 16-byte aligned.
  * Errors: INVALID_ARG, SHAPE, HIP. */
@@ -591,7 +602,10 @@ int bdlora_kv_read(bdlora_kv_t cache, const int32_t* seqs, const int32_t* index,
  *     lse = log sum_j exp(s_j)
  * out: bf16 rows like q's (not overlapping what the call reads); lse: fp32
  * [B][n_q_heads], may be null.  Where no entry is left, or all scores are
- * -infinity, out is 0 and lse -infinity.  accumulate != 0 adds each entry's
+ * -infinity, out is 0 and lse -infinity.  A value that is a NaN makes its number of
+ * the rows that see it one, whatever its probability (but for a score of
+ * -infinity); an infinite one makes it infinite (where its probability is less than
+ * 2^-126 of the largest, it may count as nothing or give a NaN).  accumulate != 0 adds each entry's
  * p_j, summed over the query heads of its kv head, to its weight.  Results
  * do not depend on timing (bitwise equal from call to call).
  * q, out 16-byte aligned, strides multiples of 8.

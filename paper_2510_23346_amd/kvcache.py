@@ -185,7 +185,8 @@ class KVCache:
         ``k_norm`` (both or neither; bf16 ``[head_dim]``): every query and key
         head x is first taken to ``x / sqrt(mean(x^2) + eps)`` times them.  In a
         cache with a scale for each block, tokens of a sequence that become
-        entries of one block stand one after the other, by ascending entry."""
+        entries of one block stand one after the other, by ascending entry
+        (else that block holds anything, and ``device_error`` reports it)."""
         T = qkv.shape[0]
         qs = self._rows("qkv", qkv, T, self._qkvw)
         os_ = self._rows("q_out", q_out, T, self._qw)
@@ -240,7 +241,9 @@ class KVCache:
         ``lens[b]``.  The row of entry p sees the entries up to p, with
         ``window`` only the last so many of these, its own among them, and the
         first ``sinks``.  Into ``out`` (not q's memory; rows of no sequence stay
-        as they are); ``lse``: fp32 ``[T, n_q_heads]``."""
+        as they are); ``lse``: fp32 ``[T, n_q_heads]``.  Probabilities enter the
+        sum over values with 24 bits for sequences of up to 32 rows (new tokens
+        times query heads of a kv head), as in ``attend``, else as bf16."""
         T = q.shape[0]
         qs = self._rows("q", q, T, self._qw)
         os_ = self._rows("out", out, T, self._qw)
