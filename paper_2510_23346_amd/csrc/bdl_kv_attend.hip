@@ -709,10 +709,11 @@ __device__ __forceinline__ void attend(const KvAttendArgs& a) {
                     bool out = false;                               // some are left out
 #pragma unroll
                     for (int x = 0; x < kBatch; ++x) {
-                        const float fx = ms[x].x == -INFINITY ? 0.f : exp2_(ms[x].x - top);
+                        // (what saw nothing adds its zeros)
+                        const float fx = ms[x].x == -INFINITY ? 1.f : exp2_(ms[x].x - top);
                         ss += fx * ms[x].y;
                         if (fx != 0.f) v += fx * y[x];
-                        out |= fx == 0.f && ms[x].x != -INFINITY;
+                        out |= fx == 0.f;
                     }
                     if (out)
 #pragma unroll
