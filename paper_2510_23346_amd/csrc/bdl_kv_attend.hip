@@ -37,12 +37,12 @@
 // Integers with a scale for each block of 16 entries (a tile has two blocks) are
 // widened to bf16, which holds them exactly, on their way into LDS; the key's scale is
 // a factor of the block's scores, the value's of its probabilities.  64 sequences of up
-// to 8192 entries, 72 MB: 24.1 us beside 22.3 in e4m3, whose widening takes a third
+// to 8192 entries, 72 MB: 24.6 us beside 22.3 in e4m3, whose widening takes a third
 // of the vector instructions (1.5 a number against 0.5).
 //
 // Sinks: the first entries are tiles of their own before those of the window.  16
-// sequences of a window of 16384 beside 64, 135 MB, 30.5 us; 37 ragged ones of a window
-// of 300 beside 4, 7.8.
+// sequences of a window of 16384 beside 64, 135 MB, 31.1 us; 37 ragged ones of a window
+// of 300 beside 4, 8.5.
 #include "bdl_kv_device.h"
 
 namespace bdl {

@@ -28,10 +28,13 @@
 // every fourth tile of 32 entries each, through their own parts of LDS, and wait for
 // each other at the end only.
 //
-// Where there are few tiles of rows, or a long sequence among short ones, a tile's
-// entries are cut into stretches for several workgroups.  They leave sums, maxima and
-// outputs in the workspace; the last one to come adds them, in the order of the
-// entries.
+// Where there are few tiles of rows, or a long sequence among not too many short ones, a
+// tile's entries are cut into stretches for several workgroups.  They leave sums, maxima
+// and outputs in the workspace; the last one to come adds them, in the order of the
+// entries.  Calls of 1024 workgroups and more are not cut: there a long sequence's rows
+// stay with one workgroup a kv head (8 kv heads, 128 single tokens behind 2000 entries each and one
+// behind 32768: 511 us, where the 2000 everywhere take 212, and 119 of them and the long
+// one, which is cut, 218).
 //
 // Measured: one prompt of 8192 with 32 query heads of 128 on 8 kv heads 517 to 560 us
 // (several cards), 0.98 to 1.06 PFLOP/s, where a large matrix product has 1.25; the
@@ -40,7 +43,7 @@
 // cover another one has to).  16384 with a window of 4096 beside 4 sinks, 8 heads on
 // one 263 to 281 us.  4 prompts of 1024 beside 192 single tokens, e4m3, 36.5 us; 8 of
 // 512, 4 heads on one, 16.4; 64 sequences of 5 new tokens behind 2100 entries each,
-// int8, 24: about 8 us are the chain to the first tile (starts and lengths, pages,
+// int8, 26.4: about 8 us are the chain to the first tile (starts and lengths, pages,
 // entries) and the end, and 8 more where stretches are joined.
 #include <type_traits>
 
@@ -170,7 +173,7 @@ __device__ __forceinline__ Prompt prompt_of(const KvPromptArgs& a, int b, int G)
 // The last `tiles` of a sequence's tiles of rows are cut into `parts` stretches, where
 // `part` units each give all workgroups work: no more than about the root of the units,
 // since the last one reads all shares, and none of short tiles, since leaving and
-// joining takes about 8 us, and a unit 1 to 1.2.  (64 tokens of 4 heads behind 2048, 4096 and
+// joining takes about 8 us, and a unit 1 to 1.5.  (With one bf16 number a probability: 64 tokens of 4 heads behind 2048, 4096 and
 // 32768 entries: 24, 27 and 55 us; up to twice as many stretches 27, 33 and 75, none
 // 33, 56 and 380.)  Of a wide sequence those of more than a stretch's units are cut, and
 // into longer ones where the shares would take more than the sequence's `slots`.  (One
@@ -497,7 +500,9 @@ struct Rows {
     // Exponentials and their product with 32 values of LDS, rows 0 on, where they are kept
     // as three bf16 numbers whose sum they are, all 24 bits: each cut towards zero, what
     // is left over is exact.  Where the first is not 0 the others are at least 2^-133, so
-    // that an infinite value gives an infinite sum and no NaN (int8 has none)
+    // that an infinite value gives an infinite sum and no NaN (int8 has none).  (64 single
+    // tokens of 4 heads of 128 behind 2048, 4096 and 32768 entries each: bf16 26.2, 35.4
+    // and 204 us, int8 22.9, 29.6 and 130; one number 24.6, 33.2 and 199, 21.1, 26.5 and 112)
     __device__ __forceinline__ void add_exponentials(const f32x16& s, float scale0, float scale1, const float* vs, const u32x4* values) {
         const float mm = m == -INFINITY ? 0.f : m;
         int ln = l;

@@ -31,7 +31,7 @@ namespace {
 //
 // Bound by the trips to memory of an owner (which token, its run and page, then the
 // block and the angles) and the waves that find they are none: 4288 tokens of 8 + 1 + 1
-// heads of 128, 22 MB read and written, 10.9 to 11.8 us, where the bf16 cache's launch
+// heads of 128, 22 MB read and written, 11.3 to 12.6 us, where the bf16 cache's launch
 // takes 8.5; 10240 tokens of 32 + 8 + 8 heads, 235 MB, 76 us, 3.1 TB/s.
 template <int N>
 struct Piece {
